@@ -206,7 +206,7 @@ def _own(s, c, ctx):
         ctx.he_rmsnorm_q8(s["x"], s["codes"], s["scales"], EPS, residual=s["residual"], weight=s["weight"], sum_out=s["sum"])
         return {"codes": s["codes"], "scales": s["scales"], "sum": s["sum"]}
     if c["kind"] == "product":
-        ctx.he_matmul_q8(s["a"], s["a_scales"], s["w"], s["w_scales"], s["out"])
+        ctx.he_matmul_q8(s["a"], s["a_scales"], s["w"], s["w_scales"], s["out"], fast_sums=c["out"] != "f32")   # what is rounded to 16 bits needs no exact sums
         return {"out": s["out"]}
     if c["kind"] == "top":
         ctx.he_top_logits(s["z"], c["tau"], s["values"], s["index"], s["rest"])
