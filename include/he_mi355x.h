@@ -353,6 +353,114 @@ typedef struct {
 int32_t he_ca_ra_block(he_ctx* ctx, const he_block_plan* plan, const uint64_t* const* h_d_ct_in, uint64_t* const* h_d_ct_out);
 int32_t he_ws_query_ca_ra_block(const he_ctx* ctx, const he_block_plan* plan, uint64_t* h_bytes);
 
+/* ---- Plaintext side: a teacher's head and a student's loss.
+ *
+ * The networks whose layers the calls above evaluate have low-degree activations (Section 3.4) and are trained in the clear
+ * before their filters are encoded; the paper trains them by distillation (Section 4.1).  These calls are that step's operators
+ * on plain numbers: a teacher's last residual addition and norm with an output in 8 bits, its product with the class or
+ * vocabulary weights, its top logits, and the student's loss against them with its gradient.  They use a context for its
+ * stream, workspace and error text only, whatever its moduli; they do not count in he_counters.
+ *
+ *  - Elements are HE_F32, HE_BF16 or HE_F16; rows lie ld elements apart (the row's length <= ld <= 2^28) and need no more
+ *    alignment than their elements; at most 2^21 rows.  All arithmetic is in 32 bits, rounded once to nearest even where it is stored.
+ *  - 8 bits are e4m3 without infinities: largest value 448, 0x7f and 0xff not a number.  A row of codes has one float scale for
+ *    each 128 columns (the last of what is left); a value is its code times its scale.  Rows of codes start at multiples of
+ *    16 bytes (pointer and ld); the columns between the row's length and the next multiple of 16 are read but not used, so
+ *    the last row's have to be there too.
+ *  - Zero rows are valid: nothing is done. */
+typedef enum { HE_F32 = 0, HE_BF16 = 1, HE_F16 = 2 } he_dtype;
+
+/* h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight; per 128 columns scale = max|y| / 448 and code = e4m3(y / scale); a
+ * block of zeros has scale 0 and codes 0, one that holds an infinity or a NaN has a scale that is not finite.  d_sum receives h in
+ * the inputs' type (the norm takes it before that rounding).  d_residual and d_sum: both or neither; d_weight may be NULL (ones).
+ * d_sum may be d_x or d_residual (with the same ld); no output may overlap an input otherwise, or another output. */
+typedef struct {
+    uint32_t rows, dim;            /* dim from 1 to 65536 */
+    int32_t dtype;                 /* of x, residual, weight, sum */
+    float eps;                     /* >= 0 */
+    const void* d_x;
+    uint64_t ld_x;
+    const void* d_residual;
+    uint64_t ld_residual;
+    const void* d_weight;          /* [dim] */
+    void* d_sum;
+    uint64_t ld_sum;
+    uint8_t* d_codes;
+    uint64_t ld_codes;
+    float* d_scales;               /* ceil(dim/128) a row */
+    uint64_t ld_scales;
+} he_rmsnorm_plan;
+int32_t he_rmsnorm_q8(he_ctx* ctx, const he_rmsnorm_plan* plan);
+
+/* out[m][n] = sum over k of A[m][k] * W[n][k], values being codes times scales: A has a scale for each row and 128 columns, W one
+ * for each 128 rows and 128 columns ([ceil(N/128)][ceil(K/128)]).  out must not overlap an operand.  The products of a block are
+ * exact and summed in 32 bits. */
+typedef struct {
+    uint32_t m, n, k;              /* k from 1 to 2^20; m, n <= 2^20, m * n <= 2^33 */
+    int32_t out_dtype;
+    uint32_t fast_sums;            /* != 0: within a block of 128 columns the sums may be taken by the matrix instruction of 8-bit numbers, which
+                                      drops of a product what lies 13 binary orders below the largest product of its group of
+                                      columns: about 2e-5 of a typical result, well below what a result rounded to 16 bits loses */
+    const uint8_t* d_a;
+    uint64_t ld_a;
+    const float* d_a_scales;
+    uint64_t ld_a_scales;
+    const uint8_t* d_w;
+    uint64_t ld_w;
+    const float* d_w_scales;
+    uint64_t ld_w_scales;
+    void* d_out;
+    uint64_t ld_out;
+} he_matmul_plan;
+int32_t he_matmul_q8(he_ctx* ctx, const he_matmul_plan* plan);
+
+/* The k largest logits of every row in descending order, the lowest index first among equals (a NaN counts as larger than any
+ * number, -0 equals +0), and d_rest[row] = log of the sum over the row's OTHER logits z of exp(z / tau): -infinity where nothing
+ * but -infinity is left.  d_values, d_index: [rows][k], dense; d_rest may be NULL. */
+#define HE_TOP_MAX 128
+typedef struct {
+    uint32_t rows, vocab, k;       /* 1 <= k <= min(vocab, HE_TOP_MAX), vocab <= 2^20 */
+    int32_t dtype;
+    float tau;                     /* > 0 */
+    const void* d_z;
+    uint64_t ld_z;
+    float* d_values;
+    int32_t* d_index;
+    float* d_rest;
+} he_top_plan;
+int32_t he_top_logits(he_ctx* ctx, const he_top_plan* plan);
+
+/* Distillation from a teacher's top logits.  The teacher's distribution of a row is the softmax over its k values / tau and, if
+ * d_rest is given, d_rest (everything else as one outcome; he_top_logits at the same tau gives all three); the student's is the
+ * softmax of z / tau, its probability of the rest being that of all indices which the teacher does not name.  With P and Q those
+ * two and y the row's label
+ *   loss = (1 - alpha) tau^2 sum P log(P / Q) + alpha (log-sum-exp(z) - z[y]).
+ * Entries whose index is outside 0..vocab-1 are not there; an index that stands twice adds its probabilities.  Where nothing of
+ * the teacher is there, or it is -infinity throughout, the first term is 0.  A row whose label is negative is padding: loss and
+ * gradient 0.  So are those of a row whose student logits are all -infinity.  A label >= vocab is not there: the second term is 0.
+ * Without d_labels alpha has to be 0.
+ * he_distill_loss writes d_loss [rows], and d_stats if that is given; with d_grad it also writes, in the same pass over the
+ * logits, d_row_weights[row] times the gradient of the row's loss by z (in z's type; d_grad may be d_z with the same ld).
+ * he_distill_grad writes that gradient from the d_stats that he_distill_loss left for the same operands. */
+typedef struct {
+    uint32_t rows, vocab, k;       /* k from 1 to HE_TOP_MAX, vocab from 1 to 2^20 */
+    int32_t dtype;                 /* of z and of the gradient */
+    float tau, alpha;              /* tau > 0, 0 <= alpha <= 1 */
+    const void* d_z;
+    uint64_t ld_z;
+    const float* d_values;         /* [rows][k] */
+    const int32_t* d_index;        /* [rows][k] */
+    const float* d_rest;           /* [rows], or NULL */
+    const int32_t* d_labels;       /* [rows], or NULL */
+    float* d_loss;                 /* [rows] */
+    float* d_stats;                /* [rows][4] */
+    const float* d_row_weights;    /* [rows] */
+    void* d_grad;
+    uint64_t ld_grad;
+} he_distill_plan;
+int32_t he_distill_loss(he_ctx* ctx, const he_distill_plan* plan);
+int32_t he_distill_grad(he_ctx* ctx, const he_distill_plan* plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,7 @@ EXPORTS = [
     "he_ntt", "he_intt", "he_automorph", "he_evk_register", "he_keyswitch", "he_rotate_hoisted", "he_rotate_batch", "he_rotate",
     "he_conjugate", "he_ptct_mac", "he_add", "he_addpt", "he_mulct", "he_affine", "he_rescale", "he_conv2d", "he_raconv",
     "he_probe_alu", "he_build_id", "he_rotate_sum", "he_ws_query_raconv", "he_ca_ra_block", "he_ws_query_ca_ra_block", "he_ras", "he_ws_bytes", "he_ws_reserve", "he_ws_query_rotate_batch", "he_ws_query_conv2d", "he_rescale_noalloc", "he_ptct_mac_rot",
+    "he_rmsnorm_q8", "he_matmul_q8", "he_top_logits", "he_distill_loss", "he_distill_grad",
 ]
 
 
@@ -61,6 +62,34 @@ class BlockPlan(C.Structure):
                 ("n_ca", C.c_uint32), ("n_ra", C.c_uint32), ("level", C.c_uint32), ("group", C.c_uint32),
                 ("deferred_moddown", C.c_uint32), ("hoisted_ras", C.c_uint32), ("h_k_in", C.POINTER(C.c_uint64)),
                 ("h_d_w_ca", C.POINTER(C.c_void_p)), ("h_d_w_ra", C.POINTER(C.c_void_p))]
+
+
+_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # he_dtype
+_CODES = (torch.uint8, torch.float8_e4m3fn)
+
+
+class RmsNormPlan(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("dim", C.c_uint32), ("dtype", C.c_int32), ("eps", C.c_float), ("d_x", C.c_void_p), ("ld_x", C.c_uint64),
+                ("d_residual", C.c_void_p), ("ld_residual", C.c_uint64), ("d_weight", C.c_void_p), ("d_sum", C.c_void_p), ("ld_sum", C.c_uint64),
+                ("d_codes", C.c_void_p), ("ld_codes", C.c_uint64), ("d_scales", C.c_void_p), ("ld_scales", C.c_uint64)]
+
+
+class MatmulPlan(C.Structure):
+    _fields_ = [("m", C.c_uint32), ("n", C.c_uint32), ("k", C.c_uint32), ("out_dtype", C.c_int32), ("fast_sums", C.c_uint32), ("d_a", C.c_void_p), ("ld_a", C.c_uint64),
+                ("d_a_scales", C.c_void_p), ("ld_a_scales", C.c_uint64), ("d_w", C.c_void_p), ("ld_w", C.c_uint64),
+                ("d_w_scales", C.c_void_p), ("ld_w_scales", C.c_uint64), ("d_out", C.c_void_p), ("ld_out", C.c_uint64)]
+
+
+class TopPlan(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("vocab", C.c_uint32), ("k", C.c_uint32), ("dtype", C.c_int32), ("tau", C.c_float), ("d_z", C.c_void_p),
+                ("ld_z", C.c_uint64), ("d_values", C.c_void_p), ("d_index", C.c_void_p), ("d_rest", C.c_void_p)]
+
+
+class DistillPlan(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("vocab", C.c_uint32), ("k", C.c_uint32), ("dtype", C.c_int32), ("tau", C.c_float), ("alpha", C.c_float),
+                ("d_z", C.c_void_p), ("ld_z", C.c_uint64), ("d_values", C.c_void_p), ("d_index", C.c_void_p), ("d_rest", C.c_void_p),
+                ("d_labels", C.c_void_p), ("d_loss", C.c_void_p), ("d_stats", C.c_void_p), ("d_row_weights", C.c_void_p),
+                ("d_grad", C.c_void_p), ("ld_grad", C.c_uint64)]
 
 
 _lib = None
@@ -114,6 +143,11 @@ def load():
         "he_ws_query_conv2d": [vp, C.POINTER(ConvPlan), u64p],
         "he_rescale_noalloc": [vp, vp, u32, vp],
         "he_ptct_mac_rot": [vp, vp, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(u32), u32, u32, i32],
+        "he_rmsnorm_q8": [vp, C.POINTER(RmsNormPlan)],
+        "he_matmul_q8": [vp, C.POINTER(MatmulPlan)],
+        "he_top_logits": [vp, C.POINTER(TopPlan)],
+        "he_distill_loss": [vp, C.POINTER(DistillPlan)],
+        "he_distill_grad": [vp, C.POINTER(DistillPlan)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -141,6 +175,47 @@ def _need(t, n, what):
     """A buffer shorter than what the library will touch is the one mistake it cannot see itself."""
     if t.numel() < n:
         raise ValueError("%s holds %d elements, the call needs %d" % (what, t.numel(), n))
+
+
+def _rows(t, what, rows, cols, dtypes):
+    """Pointer and row pitch of a matrix of plain numbers whose rows are contiguous, given that it is what the call needs."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if t.dtype not in dtypes:
+        raise TypeError("%s must be %s, not %s" % (what, " or ".join(str(d) for d in dtypes), t.dtype))
+    if t.shape != (rows, cols):
+        raise ValueError("%s is %s, the call needs %s" % (what, tuple(t.shape), (rows, cols)))
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("%s: the elements of a row must be contiguous" % what)
+    return t.data_ptr(), max(ld, cols) if rows <= 1 else ld
+
+
+def _codes(t, what, rows, cols):
+    """The same for rows of codes, whose last row has to be there up to the next multiple of 16 bytes."""
+    ptr, ld = _rows(t, what, rows, cols, _CODES)
+    if rows <= 1:
+        ld = -(-max(ld, cols) // 16) * 16
+    if rows and t.untyped_storage().nbytes() - t.storage_offset() < (rows - 1) * ld + -(-cols // 16) * 16:
+        raise ValueError("%s: the last row ends before the next multiple of 16 bytes" % what)
+    return ptr, ld
+
+
+def _dense(t, what, shape, dtype):
+    """Pointer of a dense tensor of that shape and type; None stays None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
+        raise TypeError("%s must be a CUDA tensor of %s" % (what, dtype))
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be contiguous and %s, not %s" % (what, shape, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _matrix(t, what):
+    if not (isinstance(t, torch.Tensor) and t.dim() == 2):
+        raise TypeError("%s must be a matrix on the GPU" % what)
+    return t.shape
 
 
 def _u32arr(xs):
@@ -478,3 +553,60 @@ class HEContext:
         oa = (C.c_void_p * n_ca)(*[_dev(o).value for o in outs])
         self._ck(self._lib.he_ca_ra_block(self._h, C.byref(plan), ia, oa))
         return outs
+
+    # ---- plaintext side: a teacher's head and a student's loss
+    def he_rmsnorm_q8(self, x, codes, scales, eps, residual=None, weight=None, sum_out=None):
+        """Residual addition, root-mean-square norm and 8-bit output; x, residual, sum_out [rows][dim], codes uint8 or float8_e4m3fn."""
+        rows, dim = _matrix(x, "x")
+        t = (x.dtype,) if x.dtype in _DTYPE else tuple(_DTYPE)
+        dx, ldx = _rows(x, "x", rows, dim, t)
+        dr, ldr = _rows(residual, "residual", rows, dim, t) if residual is not None else (None, 0)
+        ds, lds = _rows(sum_out, "sum_out", rows, dim, t) if sum_out is not None else (None, 0)
+        dc, ldc = _codes(codes, "codes", rows, dim)
+        dk, ldk = _rows(scales, "scales", rows, -(-dim // 128), (torch.float32,))
+        plan = RmsNormPlan(rows, dim, _DTYPE[x.dtype], eps, dx, ldx, dr, ldr, _dense(weight, "weight", (dim,), x.dtype), ds, lds, dc, ldc, dk, ldk)
+        self._ck(self._lib.he_rmsnorm_q8(self._h, C.byref(plan)))
+        return codes
+
+    def he_matmul_q8(self, a, a_scales, w, w_scales, out, fast_sums=False):
+        """out [M][N] = A [M][K] times W [N][K] transposed, both codes with scales; fast_sums: sums of a block need not be exact in 32 bits."""
+        (m, k), (n, _) = _matrix(a, "a"), _matrix(w, "w")
+        da, lda = _codes(a, "a", m, k)
+        dw, ldw = _codes(w, "w", n, k)
+        kb = -(-k // 128)
+        dsa, ldsa = _rows(a_scales, "a_scales", m, kb, (torch.float32,))
+        dsw, ldsw = _rows(w_scales, "w_scales", -(-n // 128), kb, (torch.float32,))
+        do, ldo = _rows(out, "out", m, n, tuple(_DTYPE))
+        plan = MatmulPlan(m, n, k, _DTYPE[out.dtype], 1 if fast_sums else 0, da, lda, dsa, ldsa, dw, ldw, dsw, ldsw, do, ldo)
+        self._ck(self._lib.he_matmul_q8(self._h, C.byref(plan)))
+        return out
+
+    def he_top_logits(self, z, tau, values, index, rest=None):
+        """values, index [rows][k]: the k largest of every row of z in order; rest [rows]: log-sum-exp of the others / tau."""
+        (rows, vocab), (_, k) = _matrix(z, "z"), _matrix(values, "values")
+        dz, ldz = _rows(z, "z", rows, vocab, tuple(_DTYPE))
+        plan = TopPlan(rows, vocab, k, _DTYPE[z.dtype], tau, dz, ldz, _dense(values, "values", (rows, k), torch.float32),
+                       _dense(index, "index", (rows, k), torch.int32), _dense(rest, "rest", (rows,), torch.float32))
+        self._ck(self._lib.he_top_logits(self._h, C.byref(plan)))
+        return values, index, rest
+
+    def _distill_plan(self, z, values, index, rest, tau, labels, alpha, loss, stats, row_weights, grad):
+        (rows, vocab), (_, k) = _matrix(z, "z"), _matrix(values, "values")
+        dz, ldz = _rows(z, "z", rows, vocab, tuple(_DTYPE))
+        dg, ldg = _rows(grad, "grad", rows, vocab, (z.dtype,)) if grad is not None else (None, 0)
+        return DistillPlan(rows, vocab, k, _DTYPE[z.dtype], tau, alpha, dz, ldz, _dense(values, "values", (rows, k), torch.float32),
+                           _dense(index, "index", (rows, k), torch.int32), _dense(rest, "rest", (rows,), torch.float32),
+                           _dense(labels, "labels", (rows,), torch.int32), _dense(loss, "loss", (rows,), torch.float32),
+                           _dense(stats, "stats", (rows, 4), torch.float32), _dense(row_weights, "row_weights", (rows,), torch.float32), dg, ldg)
+
+    def he_distill_loss(self, z, values, index, rest, tau, loss, labels=None, alpha=0.0, stats=None, grad=None, row_weights=None):
+        """loss [rows] of the student's logits z against the teacher's top logits; with grad also row_weights times its gradient."""
+        plan = self._distill_plan(z, values, index, rest, tau, labels, alpha, loss, stats, row_weights, grad)
+        self._ck(self._lib.he_distill_loss(self._h, C.byref(plan)))
+        return loss
+
+    def he_distill_grad(self, z, values, index, rest, tau, stats, row_weights, grad, labels=None, alpha=0.0):
+        """row_weights times the gradient of the loss by z, from the statistics that he_distill_loss left."""
+        plan = self._distill_plan(z, values, index, rest, tau, labels, alpha, None, stats, row_weights, grad)
+        self._ck(self._lib.he_distill_grad(self._h, C.byref(plan)))
+        return grad

@@ -1,0 +1,206 @@
+"""GPU: the norm with 8-bit output and the product of 8-bit codes against their definitions in 64 bits.
+
+Tolerances.  A scale is a maximum times the inverse root of a mean: its relative error is half that of a sum of dim squares in
+32 bits (at most 64 additions in a row and a tree: 72 * 2^-24 / 2) and a few roundings: 4e-6.  A code is the nearest e4m3 number to
+a value that is itself that far off: half a step (2^-4 of it, 2^-10 among the smallest) times 1.001.  A product of K columns has
+at most 128 additions in a block and one a block, each off by 2^-24 of the sum of the terms' magnitudes, then one rounding."""
+import math
+
+import pytest
+import torch
+
+import plain_ref as R
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from he_inputs.params import config_params
+    from paper_2302_02407_amd.binding import HEContext
+    return HEContext.from_params(config_params(0))
+
+
+def rng(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def check_norm(x, res, w, eps, codes, scales, total, dtype):
+    y, want = R.norm(x, res, w, eps)
+    got, dim = scales.cpu().double(), x.shape[1]
+    assert ((got - want).abs() <= 4e-6 * want + 1e-43).all()
+    if res is not None:
+        assert torch.equal(total.cpu(), (x.float() + res.float()).to(dtype))
+    s = R.spread(scales.cpu(), dim)
+    v = torch.where(s > 0, y / s, 0.0)
+    c = codes.cpu().double()
+    assert ((c - v).abs() <= (v.abs() * 2.0 ** -4).clamp_min(2.0 ** -10) * 1.001).all()
+
+
+@pytest.mark.parametrize("rows,dim", [(1, 1), (1, 127), (3, 128), (2, 129), (5, 1001), (1, 4096), (33, 640), (2, 8191), (2, 16384), (1, 65536), (301, 72)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm(ctx, dtype, rows, dim):
+    g = rng(rows * 7 + dim)
+    for res, weight, extra, off in ((True, True, 0, 0), (False, False, 3, 1), (True, False, 5, 3), (False, True, 8, 0)):
+        draw = lambda n: (torch.randn((n, dim), generator=g) * torch.exp(torch.randn(dim, generator=g))).to(dtype)  # noqa: E731
+        x, r, w = draw(rows), draw(rows) if res else None, draw(1)[0] if weight else None
+        x[:, :dim // 3 // 128 * 128] = 0                     # blocks of zeros (with a residual they are not)
+        codes = R.code_rows(torch.zeros((rows, dim), dtype=R.F8), more=extra % 2)
+        scales, total = R.matrix(rows, -(-dim // 128), torch.float32, -(-dim // 128) + extra), R.matrix(rows, dim, dtype, dim + extra, off)
+        ctx.he_rmsnorm_q8(R.on_gpu(x, dim + extra, off), codes, scales, 1e-5, residual=R.on_gpu(r, dim + extra, off) if res else None,
+                          weight=w.cuda() if weight else None, sum_out=total if res else None)
+        check_norm(x, r, w, 1e-5, codes, scales, total, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_in_place_and_extremes(ctx, dtype):
+    g = rng(3)
+    x, r = torch.randn((9, 384), generator=g).to(dtype), torch.randn((9, 384), generator=g).to(dtype)
+    x[1], r[1] = 0, 0                                        # nothing but zeros: eps alone under the root
+    x[2], r[2] = x[2] * 2.0 ** -14, 0                        # small: eps counts
+    x[3, 5] = 1000
+    for onto in ("x", "residual"):
+        dx, dr = x.cuda(), r.cuda()
+        codes, scales = R.code_rows(torch.zeros((9, 384), dtype=R.F8)), torch.empty((9, 3), device="cuda")
+        total = dx if onto == "x" else dr
+        ctx.he_rmsnorm_q8(dx, codes, scales, 1e-6, residual=dr, sum_out=total)
+        check_norm(x, r, None, 1e-6, codes, scales, total, dtype)
+    assert (scales[1] == 0).all() and (codes[1].float() == 0).all()
+
+
+def test_norm_what_is_not_finite(ctx):
+    x = torch.randn((4, 300), generator=rng(4))
+    x[0, 130], x[1, 7], x[2, 299] = math.inf, math.nan, -math.inf
+    codes, scales = R.code_rows(torch.zeros((4, 300), dtype=R.F8)), torch.empty((4, 3), device="cuda")
+    ctx.he_rmsnorm_q8(x.cuda(), codes, scales, 1e-6)
+    s, c = scales.cpu(), codes.cpu().float()
+    assert s[1].isnan().all() and c[1].isnan().all()
+    assert not s[0, 1].isfinite() and c[0, 130].isnan() and not s[2, 2].isfinite() and c[2, 299].isnan()
+    check_norm(x[3:], None, None, 1e-6, codes[3:], scales[3:], None, torch.float32)
+
+
+def operands(m, n, k, seed):
+    g = rng(seed)
+    any_codes = lambda rows: torch.randint(0, 256, (rows, k), generator=g, dtype=torch.uint8)  # noqa: E731
+    a, w = [torch.where(c & 0x7f == 0x7f, 0, c).view(R.F8) for c in (any_codes(m), any_codes(n))]
+    sa, sw = torch.rand((m, -(-k // 128)), generator=g) + 0.01, torch.rand((-(-n // 128), -(-k // 128)), generator=g) + 0.01
+    return a, sa, w, sw
+
+
+def check_product(ctx, a, sa, w, sw, dtype, more=0, off=0):
+    m, n, k = a.shape[0], w.shape[0], a.shape[1]
+    kb = -(-k // 128)
+    out = R.matrix(m, n, dtype, n + more, off)
+    around = out.untyped_storage()
+    ctx.he_matmul_q8(R.code_rows(a, more), R.on_gpu(sa, kb + more), R.code_rows(w, more), R.on_gpu(sw, kb + more), out)
+    want, size = R.product(a, sa, w, sw)
+    got = out.cpu().double()
+    bound = size * ((128 + kb + 2) * 2.0 ** -24) + want.abs() * R.ULP[dtype] * 1.001 + (2.0 ** -25 if dtype == torch.float16 else 0)
+    big = want.abs() > 60000
+    if dtype == torch.float16:
+        got, want = torch.where(big, 0.0, got), torch.where(big, 0.0, want)
+    assert ((got - want).abs() <= bound).all(), float(((got - want).abs() / bound).max())
+    whole = torch.empty(0, dtype=dtype, device="cuda").set_(around)
+    assert int(whole.isnan().sum()) == whole.numel() - m * n          # nothing written outside the rows
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 10, 64), (1, 1000, 2048), (2, 17, 130), (15, 33, 127), (16, 128, 128), (17, 129, 129), (24, 1000, 512), (33, 250, 1040),
+                                   (64, 64, 16), (65, 300, 1000), (127, 1001, 391), (128, 256, 512), (130, 130, 2000), (200, 10, 4096), (257, 513, 640), (515, 1030, 256), (1, 3, 70000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_product(ctx, dtype, m, n, k):
+    check_product(ctx, *operands(m, n, k, m + n + k), dtype)
+
+
+@pytest.mark.parametrize("m", [1, 5, 20, 40, 70, 150, 300])
+def test_product_of_rows_further_apart(ctx, m):
+    for dtype, more, off in ((torch.float32, 1, 1), (torch.bfloat16, 3, 5), (torch.float16, 2, 2)):
+        check_product(ctx, *operands(m, 203, 333, m), dtype, more, off)
+
+
+@pytest.mark.parametrize("m", [1, 30, 140, 400])
+def test_product_picks_the_right_terms(ctx, m):
+    """Exact: one code in each row of W, powers of two, so that every result is one product."""
+    n, k = 300, 700
+    a, sa, _, _ = operands(m, n, k, 9)
+    sa, sw = torch.exp2(torch.randint(-3, 3, sa.shape, generator=rng(1)).float()), torch.exp2(torch.randint(-3, 3, (3, 6), generator=rng(2)).float())
+    at, w = (torch.arange(n) * 37) % k, torch.zeros((n, k))
+    w[torch.arange(n), at] = 2.0
+    out = torch.empty((m, n), device="cuda")
+    ctx.he_matmul_q8(R.code_rows(a), sa.cuda(), R.code_rows(w.to(R.F8)), sw.cuda(), out)
+    want, _ = R.product(a, sa, w, sw)
+    assert torch.equal(out.cpu().double(), want)
+
+
+@pytest.mark.parametrize("m", [1, 40, 300])
+def test_product_of_what_is_not_a_number(ctx, m):
+    """A NaN code spoils its row (or column) and nothing else; so does a scale that is not finite."""
+    a, sa, w, sw = operands(m, 260, 400, 5)
+    clean, _ = R.product(a, sa, w, sw)
+    a.view(torch.uint8)[m // 2, 399], w.view(torch.uint8)[130, 0], sw[2, 3] = 0x7f, 0xff, math.nan
+    out = torch.empty((m, 260), device="cuda")
+    ctx.he_matmul_q8(R.code_rows(a), sa.cuda(), R.code_rows(w), sw.cuda(), out)
+    bad = torch.zeros((m, 260), dtype=torch.bool)
+    bad[m // 2], bad[:, 130], bad[:, 256:] = True, True, True
+    assert torch.equal(out.cpu().isnan(), bad)
+    assert torch.allclose(out.cpu().double()[~bad], clean[~bad], rtol=1e-4, atol=1.0)
+
+
+def test_head_refusals(ctx):
+    from paper_2302_02407_amd.binding import HEError
+    z = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device="cuda")  # noqa: E731
+    x, codes, scales = z(4, 256), z(4, 256, dtype=R.F8), z(4, 2)
+
+    def refused(call, *a, **kw):
+        with pytest.raises((HEError, TypeError, ValueError)) as e:
+            call(*a, **kw)
+        assert not isinstance(e.value, HEError) or e.value.code == -1
+
+    refused(ctx.he_rmsnorm_q8, x, codes, scales, -1.0)
+    refused(ctx.he_rmsnorm_q8, x, codes, scales, math.nan)
+    refused(ctx.he_rmsnorm_q8, x, codes, scales, 0.0, residual=z(4, 256))                       # no room for the sum
+    refused(ctx.he_rmsnorm_q8, x, codes, scales, 0.0, sum_out=z(4, 256))
+    refused(ctx.he_rmsnorm_q8, x, codes, z(4, 1), 0.0)
+    refused(ctx.he_rmsnorm_q8, x, codes[:3], scales, 0.0)
+    refused(ctx.he_rmsnorm_q8, x.double(), codes, scales, 0.0)
+    refused(ctx.he_rmsnorm_q8, x, z(4, 264, dtype=R.F8)[:, :256], scales, 0.0)                  # rows off by 8 bytes
+    refused(ctx.he_rmsnorm_q8, x, x.view(torch.uint8).view(R.F8)[:, :256], scales, 0.0)         # codes in the input's memory
+    refused(ctx.he_rmsnorm_q8, x, codes, x[:, :2], 0.0)
+    room = z(5, 256)
+    refused(ctx.he_rmsnorm_q8, room[:4], codes, scales, 0.0, residual=z(4, 256), sum_out=room[1:])
+    refused(ctx.he_rmsnorm_q8, x[:, ::2], codes[:, :128], z(4, 1), 0.0)
+    ctx.he_rmsnorm_q8(x[:0], codes[:0], scales[:0], 0.0)                                        # no rows: fine
+    w, sw, out = z(100, 256, dtype=R.F8), z(1, 2), z(4, 100)
+    refused(ctx.he_matmul_q8, codes, scales, w[:, :240], sw, out)
+    refused(ctx.he_matmul_q8, codes, scales, w, z(2, 2), out)
+    refused(ctx.he_matmul_q8, codes, z(4, 3), w, sw, out)
+    refused(ctx.he_matmul_q8, codes, scales, w, sw, out[:, :99])
+    refused(ctx.he_matmul_q8, codes.float(), scales, w, sw, out)
+    refused(ctx.he_matmul_q8, z(4, 260, dtype=R.F8)[:, 4:], scales, w, sw, out)
+    refused(ctx.he_matmul_q8, codes, scales, w, sw, w.view(torch.float32)[:4, :0].new_zeros(0))
+    refused(ctx.he_matmul_q8, codes, scales, w, sw, w.view(torch.bfloat16)[:4, :100])           # output in an operand
+    refused(ctx.he_matmul_q8, z(64, dtype=R.F8)[:50].view(1, 50)[:, :49], z(1, 1), z(3, 64, dtype=R.F8)[:, :49], z(1, 1), z(1, 3, dtype=torch.float64))
+    refused(ctx.he_matmul_q8, z(49, dtype=R.F8).view(1, 49), z(1, 1), z(3, 64, dtype=R.F8)[:, :49], z(1, 1), z(1, 3))   # last row cut short
+    ctx.he_matmul_q8(codes[:0], scales[:0], w, sw, out[:0])
+    torch.cuda.synchronize()
+
+
+def test_head_on_a_stream_of_its_own(ctx):
+    from he_inputs.params import config_params
+    from paper_2302_02407_amd.binding import HEContext
+    side = torch.cuda.Stream()
+    other = HEContext.from_params(config_params(0), stream=side)
+    g = rng(8)
+    x = torch.randn((64, 512), generator=g).cuda()
+    a, sa, w, sw = operands(64, 300, 512, 12)
+    w, sw = R.code_rows(w), sw.cuda()
+    outs = []
+    torch.cuda.synchronize()
+    for c in (ctx, other):
+        codes, scales, out = R.code_rows(torch.zeros((64, 512), dtype=R.F8)), torch.zeros((64, 4), device="cuda"), torch.zeros((64, 300), device="cuda")
+        torch.cuda.synchronize()
+        c.he_rmsnorm_q8(x, codes, scales, 1e-6)
+        c.he_matmul_q8(codes, scales, w, sw, out)
+        c.he_sync()
+        outs.append(out)
+    assert torch.equal(*outs)
