@@ -396,7 +396,7 @@ int32_t he_rmsnorm_q8(he_ctx* ctx, const he_rmsnorm_plan* plan);
  * for each 128 rows and 128 columns ([ceil(N/128)][ceil(K/128)]).  out must not overlap an operand.  The products of a block are
  * exact and summed in 32 bits. */
 typedef struct {
-    uint32_t m, n, k;              /* k from 1 to 2^20; m, n <= 2^20, m * n <= 2^33 */
+    uint32_t m, n, k;              /* k from 1 to 2^20; m, n <= 2^20, m * n <= 2^33; ld_a, ld_w <= 2^23 */
     int32_t out_dtype;
     uint32_t fast_sums;            /* != 0: within a block of 128 columns the sums may be taken by the matrix instruction of 8-bit numbers, which
                                       drops of a product what lies 13 binary orders below the largest product of its group of

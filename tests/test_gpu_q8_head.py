@@ -118,6 +118,28 @@ def test_product_of_rows_further_apart(ctx, m):
         check_product(ctx, *operands(m, 203, 333, m), dtype, more, off)
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 130, 640), (70, 300, 130), (129, 260, 1000), (300, 700, 2048), (513, 257, 384)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_product_with_fast_sums(ctx, dtype, m, n, k):
+    """A product may lose 2^-13 of the largest of its group of columns, at most its block's: 128 * 2^-13 of that a block.  Of normal values
+    in a group of at least 8 the losses are independent and mostly far smaller: 1e-4 of the result in the 2-norm."""
+    g = rng(m + n)
+    a, w = [torch.randn((r, k), generator=g).mul_(60).clamp_(-448, 448).to(R.F8) for r in (m, n)]
+    _, sa, _, sw = operands(m, n, k, 4)
+    out = R.matrix(m, n, dtype, n + 3, 1)
+    ctx.he_matmul_q8(R.code_rows(a), sa.cuda(), R.code_rows(w), sw.cuda(), out, fast_sums=True)
+    want, size = R.product(a, sa, w, sw)
+    most = lambda x, sx: torch.stack([b.double().abs().amax(dim=1) for b in x.split(128, dim=1)], dim=1) * sx.double()  # noqa: E731
+    loss = 128 * 2.0 ** -13 * most(a, sa) @ most(w, sw.repeat_interleave(128, dim=0)[:n]).T
+    if dtype == torch.float16:                               # beyond what f16 holds: infinities, as in the other test of products
+        beyond = want.abs() > 65600
+        assert torch.equal(out.cpu().double()[beyond], want[beyond].sign() * math.inf)
+        out, want = out.cpu().masked_fill(want.abs() > 60000, 0.0), want.masked_fill(want.abs() > 60000, 0.0)
+    d = out.cpu().double() - want
+    assert (d.abs() <= loss + size * ((128 + sa.shape[1] + 2) * 2.0 ** -24) + want.abs() * R.ULP[dtype] * 1.001).all()
+    assert d.norm() <= (1e-4 + R.ULP[dtype]) * want.norm()
+
+
 @pytest.mark.parametrize("m", [1, 30, 140, 400])
 def test_product_picks_the_right_terms(ctx, m):
     """Exact: one code in each row of W, powers of two, so that every result is one product."""
