@@ -81,8 +81,13 @@ template <class T> __global__ __launch_bounds__(64) void matmul_q8_kernel(GemmAr
 // (the second operand's), so a block's sums need one factor a lane and square: 16 multiply-adds beside the 2 matrix instructions (64 passes
 // each) that made them.
 //
-// The 16-byte piece c of row r lies at piece c ^ (r & 7): the lanes of a fragment read take the same piece of consecutive rows, and any
-// eight of them cover all banks.
+// The 16-byte piece c of row r lies at piece c ^ (r / 2 & 7): the lanes of a fragment read take the same piece of consecutive rows, and any
+// sixteen of them, two rows of 128 bytes to a line of all 64 banks, cover every bank once.  The fills are spread over the first half of a
+// block's squares: all at once they wait for the cache's 64 bytes a cycle and hold the wavefront's matrix instructions back.
+//
+// 8192 x 32768 x 4096 to bf16 1.08 ms (2030 TFLOP/s), exact sums to f32 2.15 ms (1020).  With no fills at all (on what lies there)
+// the first takes 0.91 ms; the matrix instructions alone are 45% of its cycles, the multiply-adds 30%, and of the two kinds about half can
+// run at a time (a pair of the first and 16 of the second take 172 cycles, not 130, with two wavefronts to a unit).
 typedef const __attribute__((address_space(1))) void* gptr;
 typedef __attribute__((address_space(3))) void* lptr;
 
@@ -96,7 +101,7 @@ template <int WN, int WM, int TN, int TM> struct Tile {
 __device__ __forceinline__ v16f zero16() { return v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}; }
 // Pieces c and c + 1 of row r (r0 = the row's first byte)
 __device__ __forceinline__ v8i fragment(const uint8_t* r0, uint32_t c, uint32_t r) {
-    const v4i lo = *(const v4i*)(r0 + ((c ^ (r & 7)) << 4)), hi = *(const v4i*)(r0 + (((c + 1) ^ (r & 7)) << 4));
+    const v4i lo = *(const v4i*)(r0 + ((c ^ (r >> 1 & 7)) << 4)), hi = *(const v4i*)(r0 + (((c + 1) ^ (r >> 1 & 7)) << 4));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -116,7 +121,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
     using raw = typename T::raw;
     using G = Tile<WN, WM, TN, TM>;
     extern __shared__ __align__(1024) uint8_t lds[];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 31, g = lane >> 5;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane & 31, g = lane >> 5;
     const uint32_t wn = wave % WN, wm = wave / WN;
     uint32_t n0, m0;
     if (!tile_of((a.n + G::BN - 1) / G::BN, (a.m + G::BM - 1) / G::BM, n0, m0)) return;
@@ -125,20 +130,20 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
     const uint32_t blocks = (a.k + 127) / 128;
 
     // a wavefront fills eight rows at a time: lane i the piece i % 8 of row i / 8
-    constexpr int WAVES = WN * WM, FW = G::BN / 8 / WAVES, FA = G::BM / 8 / WAVES;
+    constexpr int WAVES = WN * WM, FW = G::BN / 8 / WAVES, FA = G::BM / 8 / WAVES, FILLS = FW + FA;
     const uint8_t *w0 = a.w + n0 * a.ld_w, *a0 = a.a + m0 * a.ld_a;
-    const uint32_t piece = (lane & 7) ^ (lane >> 3);
-    uint32_t off[FW + FA];                               // ld <= 2^23: 256 rows stay below 2^31
+    const uint32_t piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+    uint32_t off[FILLS];                               // ld <= 2^23: 256 rows stay below 2^31
 #pragma unroll
-    for (int f = 0; f < FW + FA; f++) {
+    for (int f = 0; f < FILLS; f++) {
         const uint32_t r = ((f < FW ? f : f - FW) * WAVES + wave) * 8 + (lane >> 3);
         off[f] = f < FW ? min(r, a.n - 1 - n0) * (uint32_t)a.ld_w : min(r, a.m - 1 - m0) * (uint32_t)a.ld_a;
     }
-    auto fill = [&](uint32_t b) {
+    auto fill = [&](uint32_t b, int from, int end) {
         const uint32_t at = b * 128 + piece * 16, in = at < a.k ? at : 0;          // past the end: anything that is there, cleared below
         uint8_t* to = lds + (b & 1) * G::BYTES + wave * 1024;
 #pragma unroll
-        for (int f = 0; f < FW + FA; f++)
+        for (int f = from; f < end; f++)
             __builtin_amdgcn_global_load_lds((gptr)((f < FW ? w0 : a0) + (off[f] + in)), (lptr)(to + f * WAVES * 1024), 16, 0, 0);
     };
     float* scales = (float*)(lds + 2 * G::BYTES);
@@ -151,9 +156,9 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0;
 
-    fill(0);
+    fill(0, 0, FILLS);
     for (uint32_t b = 0; b < blocks; b++) {
-        if ((b & 7) == 0) {                              // scales of the next eight blocks, one row of A a few threads
+        if ((b & 7) == 0) {                              // scales of the next eight blocks
             float* to = scales + (b >> 3 & 1) * 8 * G::BM;
             for (uint32_t i = tid; i < 8 * G::BM; i += G::THREADS) {
                 const uint32_t r = i / 8, c = b + i % 8;
@@ -163,12 +168,12 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
         const float swb = sw[b];
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (b + 1 < blocks) fill(b + 1);
+        if (!FAST && b + 1 < blocks) fill(b + 1, 0, FILLS);
         uint8_t* buf = lds + (b & 1) * G::BYTES;
         if (b + 1 == blocks && (a.k & 127)) {            // columns past the end become zeros, in both operands
             const uint32_t left = a.k & 127;
             for (uint32_t i = tid; i < (G::BN + G::BM) * 8; i += G::THREADS) {
-                const uint32_t r = i >> 3, c = (i & 7) ^ (r & 7);
+                const uint32_t r = i >> 3, c = (i & 7) ^ (r >> 1 & 7);
                 v4i* p = (v4i*)(buf + i * 16);
                 if (16 * c + 16 > left) *p = 16 * c < left ? keep(*p, (int)(left - 16 * c)) : v4i{0, 0, 0, 0};
             }
@@ -191,10 +196,12 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
                 for (int h = 0; h < 2; h++) wf[h] = fragment(wb + i * 4096, 4 * h + 2 * g, l);
 #pragma unroll
                 for (int j = 0; j < TM; j++) {
+                    if (i < 2 && b + 1 < blocks) fill(b + 1, (i * TM + j) * FILLS / 4, (i * TM + j + 1) * FILLS / 4);
                     v16f p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[0], af[j][0], zero16(), 0, 0, 0, 0, 0, 0);
                     p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[1], af[j][1], p, 0, 0, 0, 0, 0, 0);
 #pragma unroll
                     for (int e = 0; e < 16; e++) acc[i][j][e] += p[e] * s[j];
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         } else {
@@ -203,7 +210,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
             for (int j = 0; j < TM; j++)
 #pragma unroll
                 for (int c = 0; c < 4; c++) {
-                    const v4i v = *(const v4i*)(ab + j * 4096 + (((2 * c + g) ^ (l & 7)) << 4));
+                    const v4i v = *(const v4i*)(ab + j * 4096 + (((2 * c + g) ^ (l >> 1 & 7)) << 4));
                     af[j][2 * c] = halves(v[0], v[1]);
                     af[j][2 * c + 1] = halves(v[2], v[3]);
                 }
@@ -212,7 +219,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
                 v16f p[TM];
 #pragma unroll
                 for (int c = 0; c < 4; c++) {
-                    const v4i v = *(const v4i*)(wb + i * 4096 + (((2 * c + g) ^ (l & 7)) << 4));
+                    const v4i v = *(const v4i*)(wb + i * 4096 + (((2 * c + g) ^ (l >> 1 & 7)) << 4));
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
                         const v8h wf = halves(v[2 * h], v[2 * h + 1]);
