@@ -47,6 +47,40 @@ template <int WAVES, class F> __device__ __forceinline__ float group_reduce(floa
 template <int WAVES> __device__ __forceinline__ float group_sum(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return a + b; }); }
 template <int WAVES> __device__ __forceinline__ float group_max(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return fmaxf(a, b); }); }
 
+// Sixteen bytes of a row that starts anywhere its elements may: N numbers from p on, of which `left` are the row's; the others are `fill`
+template <class T> struct Vec {
+    using raw = typename T::raw;
+    static constexpr int N = 16 / sizeof(raw);
+    raw r[N];
+    __device__ __forceinline__ void load(const raw* p, uint32_t left, float fill) {
+        if (left >= (uint32_t)N) __builtin_memcpy(r, p, 16);
+        else
+#pragma unroll
+            for (int i = 0; i < N; i++) r[i] = (uint32_t)i < left ? p[i] : from_float<T>(fill);
+    }
+    __device__ __forceinline__ void store(raw* p, uint32_t left) const {
+        if (left >= (uint32_t)N) __builtin_memcpy(p, r, 16);
+        else
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                if ((uint32_t)i < left) p[i] = r[i];
+    }
+    __device__ __forceinline__ float operator[](int i) const { return to_float<T>(r[i]); }
+};
+
+// Maximum over a wavefront, the same in all lanes: within rows of 16 lanes by rotations, then over the four rows
+template <int CTRL> __device__ __forceinline__ float rotated(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+__device__ __forceinline__ float wave_max_dpp(float v) {
+    v = fmaxf(v, rotated<0x128>(v));      // row_ror:8, 4, 2, 1
+    v = fmaxf(v, rotated<0x124>(v));
+    v = fmaxf(v, rotated<0x122>(v));
+    v = fmaxf(v, rotated<0x121>(v));
+    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+
 // Calls f with the type of `dtype` (an he_dtype that has been checked)
 template <class F> static inline void with_dtype(int32_t dtype, F&& f) {
     if (dtype == HE_F32) f(f32_t{});
