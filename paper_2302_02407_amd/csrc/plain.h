@@ -47,38 +47,65 @@ template <int WAVES, class F> __device__ __forceinline__ float group_reduce(floa
 template <int WAVES> __device__ __forceinline__ float group_sum(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return a + b; }); }
 template <int WAVES> __device__ __forceinline__ float group_max(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return fmaxf(a, b); }); }
 
-// Sixteen bytes of a row that starts anywhere its elements may: N numbers from p on, of which `left` are the row's; the others are `fill`
+// Sixteen bytes of a row, which may start anywhere its elements may
 template <class T> struct Vec {
     using raw = typename T::raw;
     static constexpr int N = 16 / sizeof(raw);
-    raw r[N];
-    __device__ __forceinline__ void load(const raw* p, uint32_t left, float fill) {
-        if (left >= (uint32_t)N) __builtin_memcpy(r, p, 16);
-        else
-#pragma unroll
-            for (int i = 0; i < N; i++) r[i] = (uint32_t)i < left ? p[i] : from_float<T>(fill);
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const raw* p) { __builtin_memcpy(w, p, 16); }
+    __device__ __forceinline__ void store(raw* p) const { __builtin_memcpy(p, w, 16); }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (N == 4) return __builtin_bit_cast(float, w[i]);
+        else if constexpr (__is_same(T, bf16_t)) return __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i / 2] >> 16 * (i & 1)));
     }
-    __device__ __forceinline__ void store(raw* p, uint32_t left) const {
-        if (left >= (uint32_t)N) __builtin_memcpy(p, r, 16);
-        else
-#pragma unroll
-            for (int i = 0; i < N; i++)
-                if ((uint32_t)i < left) p[i] = r[i];
+    __device__ __forceinline__ void set(int i, float v) {
+        const raw r = from_float<T>(v);
+        if constexpr (N == 4) w[i] = r;
+        else w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (uint32_t)r << 16 : (w[i / 2] & 0xffff0000u) | r;
     }
-    __device__ __forceinline__ float operator[](int i) const { return to_float<T>(r[i]); }
 };
 
-// Maximum over a wavefront, the same in all lanes: within rows of 16 lanes by rotations, then over the four rows
-template <int CTRL> __device__ __forceinline__ float rotated(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+// A row of n >= N elements in pieces of 16 bytes, without a branch on the way to a load: piece v starts at base(v), the last one, and any
+// past it, where it still lies in the row.  The elements of those that belong to the piece before, or to nothing, are those below
+// v * N.
+template <class T> struct Row {
+    using raw = typename T::raw;
+    static constexpr uint32_t N = Vec<T>::N;
+    const raw* p;
+    uint32_t n;
+    __device__ __forceinline__ uint32_t pieces() const { return (n + N - 1) / N; }
+    __device__ __forceinline__ uint32_t base(uint32_t v) const { return min(v * N, n - N); }
+    __device__ __forceinline__ Vec<T> load(uint32_t v) const {
+        Vec<T> x;
+        x.load(p + base(v));
+        return x;
+    }
+};
+
+// Numbers as integers in their order, and back (NaN lies beyond the infinity of its sign)
+__device__ __forceinline__ int32_t ordered(float v) {
+    const int32_t b = __builtin_bit_cast(int32_t, v);
+    return b ^ (b >> 31 & 0x7fffffff);
 }
-__device__ __forceinline__ float lane_value(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
-__device__ __forceinline__ float wave_max_dpp(float v) {
-    v = fmaxf(v, rotated<0x128>(v));      // row_ror:8, 4, 2, 1
-    v = fmaxf(v, rotated<0x124>(v));
-    v = fmaxf(v, rotated<0x122>(v));
-    v = fmaxf(v, rotated<0x121>(v));
-    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+__device__ __forceinline__ float unordered(int32_t k) { return __builtin_bit_cast(float, k ^ (k >> 31 & 0x7fffffff)); }
+
+// Maximum or minimum of integers over a wavefront, the same in all lanes: rotations within rows of 16 lanes, then the four rows in scalars.
+// (Of floats every step would cost two more instructions, which make a signalling NaN a quiet one.)
+template <int CTRL> __device__ __forceinline__ int32_t rotated(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ int32_t wave_max(int32_t v) {
+    v = max(v, rotated<0x128>(v));        // row_ror:8, 4, 2, 1
+    v = max(v, rotated<0x124>(v));
+    v = max(v, rotated<0x122>(v));
+    v = max(v, rotated<0x121>(v));
+    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+// Minimum over each row of 16 lanes
+__device__ __forceinline__ int32_t row_min(int32_t v) {
+    v = min(v, rotated<0x128>(v));
+    v = min(v, rotated<0x124>(v));
+    v = min(v, rotated<0x122>(v));
+    return min(v, rotated<0x121>(v));
 }
 
 // Calls f with the type of `dtype` (an he_dtype that has been checked)

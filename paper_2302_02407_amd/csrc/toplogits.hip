@@ -25,12 +25,14 @@ __device__ __forceinline__ u64 place_of(float z, uint32_t i) { return (u64)order
 // An element's place in the order is one number of 64 bits, its key above the complement of its index, all different.
 
 template <int THREADS> struct TopShared {
-    static constexpr int ROOM = 2048;          // elements that can be set aside
-    u64 found[ROOM];
-    float dropped[ROOM];
+    static constexpr int ROOM = THREADS == 1024 ? 1024 : 512, KEEP = 512;
+    uint4 aside[ROOM];                         // 16 bytes of the row each, and which
+    uint32_t which[ROOM];                      // index of the first of its elements, and above 24 bits how many are another's
+    u64 keep[KEEP], more;
     uint32_t bins[256];
-    float tw[2][THREADS / 64], room[THREADS / 64];
-    uint32_t digit, left, got;
+    int32_t tw[2][THREADS / 64];
+    float room[THREADS / 64];
+    uint32_t digit, left, got, kept;
 };
 
 // A row by reading it as often as it takes: the k-th largest place is found a digit of 8 bits at a time, from the row's counts of that digit
@@ -68,15 +70,15 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
     for (uint32_t i = t; i < a.vocab; i += THREADS) {
         const float v = to_float<T>(z[i]);
         const u64 c = place_of(v, i);
-        if (c >= prefix) s.found[atomicAdd(&s.got, 1u)] = c;    // exactly k
+        if (c >= prefix) s.keep[atomicAdd(&s.got, 1u)] = c;     // exactly k
         else most = fmaxf(most, v);
     }
     most = group_max<THREADS / 64>(most, s.room);
     __syncthreads();
     if (t < a.k) {
-        const u64 c = s.found[t];
+        const u64 c = s.keep[t];
         uint32_t place = 0;
-        for (uint32_t j = 0; j < a.k; j++) place += s.found[j] > c;
+        for (uint32_t j = 0; j < a.k; j++) place += s.keep[j] > c;
         const uint32_t i = ~(uint32_t)c;
         a.values[row * a.k + place] = to_float<T>(z[i]);
         a.index[row * a.k + place] = (int32_t)i;
@@ -92,106 +94,132 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
     if (t == 0) a.rest[row] = at == INFINITY ? sum : logf(sum) + at / a.tau;
 }
 
-// One row a work group, read once, 16 bytes a lane at a time.  Elements from a threshold on are set aside in LDS, the others go into their
-// lane's sum against its running maximum.  The threshold is one that at least k elements reach: every wavefront has r = ceil(k / wavefronts)
-// lanes whose largest element so far reaches its r-th largest lane's, and the smallest of those over the wavefronts is it.  It is taken
-// anew after 0, 1, 2, 4, 8 ... pieces of the row, so that of a row in no particular order some k (1 + ln(pieces)) elements are set
-// aside.  At the end each of them counts how many of them come before it: the first k are the result, in order, the others join the
-// sum, by their place in that order so that the same row gives the same bits.  An element of -infinity can only be among the
-// first k if its index is below k: of the first k elements at most as many are larger as there are larger ones at all.
+// One row a work group, read once, 16 bytes a lane at a time.  Pieces of 16 bytes with an element that reaches a threshold are set aside in
+// LDS, the elements of the others go into their lane's sum against its running maximum.  The threshold is one that at least k
+// elements reach: every wavefront has r = ceil(k / wavefronts) lanes whose largest element so far reaches its r-th largest lane's, and the
+// smallest of those over the wavefronts is it.  It is taken anew after 0, 2, 6, 14 ... turns, so that of a row in no particular order a
+// few times k (1 + ln(turns)) pieces are set aside, and once more at the end.  Of the elements that reach the last one each counts how
+// many come before it: the first k are the result, in order.  The others join the sum as whole multiples of 2^-44 of the rest's largest
+// term, in any order the same number.  An element of -infinity can only be among the first k if its index is below k: of the first k
+// elements at most as many are larger as there are larger ones at all.
 template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void top_logits_kernel(TopArgs a) {
     using raw = typename T::raw;
-    constexpr int N = Vec<T>::N, WAVES = THREADS / 64, ROOM = TopShared<THREADS>::ROOM;
+    constexpr int N = Vec<T>::N, WAVES = THREADS / 64, ROOM = TopShared<THREADS>::ROOM, KEEP = TopShared<THREADS>::KEEP;
     __shared__ TopShared<THREADS> s;
     const u64 row = blockIdx.x;
     const raw* z = (const raw*)a.z + row * a.ld_z;
     const uint32_t t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const uint32_t vecs = (a.vocab + N - 1) / N, pieces = (vecs + THREADS - 1) / THREADS;
+    if (a.vocab < (uint32_t)N) return exact_row<T, THREADS>(a, s, row);
+    const Row<T> in{z, a.vocab};
+    const uint32_t vecs = in.pieces(), turns = (vecs + THREADS - 1) / THREADS;
     const uint32_t full = min((uint32_t)WAVES, vecs / 64), r = full ? (a.k + full - 1) / full : 65;
     const float c = HE_LOG2E / a.tau;
-    auto load = [&](uint32_t v) {
-        Vec<T> x;
-        const uint32_t at = v * N;
-        x.load(z + at, at < a.vocab ? a.vocab - at : 0, -INFINITY);
-        return x;
-    };
-    if (t == 0) s.got = 0;
+    if (t == 0) s.got = s.kept = 0, s.more = 0;
     float m = -3e38f, sum = 0, high = -INFINITY, least = -INFINITY;
-    Vec<T> next = load(t);
-    for (uint32_t p = 0; p < pieces; p++) {
-        const Vec<T> x = next;
-        if (p + 1 < pieces) next = load((p + 1) * THREADS + t);
+    auto raise = [&](int32_t* tw) {
+        int32_t w = ordered(high), best = INT32_MIN;
+        if (r <= 64)
+            for (uint32_t i = 0; i < r; i++) {
+                best = wave_max(w);
+                if (lane == (uint32_t)__builtin_ctzll(__ballot(w == best))) w = INT32_MIN;
+            }
+        if (lane == 0) tw[wave] = wave < full ? best : INT32_MAX;
+        __syncthreads();
+        const int32_t all = __builtin_amdgcn_readfirstlane(row_min(tw[lane % WAVES]));
+        least = r <= 64 ? fmaxf(unordered(all), -INFINITY) : -INFINITY;      // no NaN: lanes that have run out
+    };
+    auto turn = [&](uint32_t p, Vec<T>& buf) {           // two buffers in turn, each refilled as soon as it is taken
+        const uint32_t v = p * THREADS + t;
+        const uint32_t base = in.base(v), past = v * N - base;       // elements of it that are another piece's
+        Vec<T> x = buf;
+        buf = in.load(v + 2 * THREADS);
         float e[N];
 #pragma unroll
         for (int i = 0; i < N; i++) e[i] = x[i];
+        if (past)
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                if ((uint32_t)i < past) x.set(i, e[i] = -INFINITY);
         float mx = e[0];
 #pragma unroll
         for (int i = 1; i < N; i++) mx = fmaxf(mx, e[i]);
         high = fmaxf(high, mx);
-        if ((p & (p - 1)) == 0) {
-            float w = high, best = -INFINITY;
-            if (r <= 64)
-                for (uint32_t i = 0; i < r; i++) {
-                    best = wave_max_dpp(w);
-                    const uint64_t who = __ballot(w == best);
-                    if (lane == (uint32_t)__builtin_ctzll(who | 1ull << 63)) w = -INFINITY;
-                }
-            float* tw = s.tw[p ? __builtin_ctz(p) + 1 & 1 : 0];
-            if (lane == 0) tw[wave] = wave < full ? best : INFINITY;
-            __syncthreads();
-            least = tw[0];
+        if (((p + 1) & (p + 2)) == 0) raise(s.tw[__builtin_ctz(p + 2) & 1]);
+        if (!(mx < least) && (mx != -INFINITY || base < a.k)) {
+            const uint32_t to = atomicAdd(&s.got, 1u);
+            if (to < ROOM) {
+                s.aside[to] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+                s.which[to] = base | min(past, 15u) << 24;
+            }
+        } else {
+            if (mx > m) {
+                sum *= exp2_fast((m - mx) * c);
+                m = mx;
+            }
+            const float mc = m == -3e38f ? 0.0f : m * c;     // nothing but -infinity so far
 #pragma unroll
-            for (int i = 1; i < WAVES; i++) least = fminf(least, tw[i]);
-            if (r > 64) least = -INFINITY;
+            for (int i = 0; i < N; i++) sum += exp2_fast(fmaf(e[i], c, -mc));
         }
-        if (__any(!(mx < least))) {
-            const uint32_t at = (p * THREADS + t) * N;
-#pragma unroll
-            for (int i = 0; i < N; i++)
-                if (!(e[i] < least)) {
-                    if (e[i] != -INFINITY || at + i < a.k) {
-                        const uint32_t to = atomicAdd(&s.got, 1u);
-                        if (to < ROOM) s.found[to] = place_of(e[i], at + i);
-                    }
-                    e[i] = -INFINITY;
-                }
-            mx = e[0];
-#pragma unroll
-            for (int i = 1; i < N; i++) mx = fmaxf(mx, e[i]);
-        }
-        if (__any(mx > m)) {
-            const float to = fmaxf(m, mx);
-            sum *= exp2_fast((m - to) * c);
-            m = to;
-        }
-        const float mc = m == -3e38f ? 0.0f : m * c;     // nothing but -infinity so far
-#pragma unroll
-        for (int i = 0; i < N; i++) sum += exp2_fast(fmaf(e[i], c, -mc));
+    };
+    Vec<T> one = in.load(t), two = in.load(THREADS + t);
+    for (uint32_t p = 0; p < turns; p += 2) {
+        turn(p, one);
+        if (p + 1 < turns) turn(p + 1, two);
     }
-    __syncthreads();
+    __syncthreads();                                     // all is set aside, and the slots of tw have been read
     const uint32_t got = s.got;
     if (got > ROOM || __syncthreads_or(sum != sum)) return exact_row<T, THREADS>(a, s, row);
-    for (uint32_t i = t; i < got; i += THREADS) {
-        const u64 mine = s.found[i];
+    raise(s.tw[0]);
+    float most = m;
+    for (uint32_t i = t; i < got * N; i += THREADS) {
+        const float v = to_float<T>(((const raw*)s.aside)[i]);
+        const uint32_t which = s.which[i / N], at = (which & 0xffffff) + i % N;
+        if (!(v < least) && i % N >= which >> 24) {
+            const uint32_t to = atomicAdd(&s.kept, 1u);
+            if (to < KEEP) s.keep[to] = place_of(v, at);
+        } else most = fmaxf(most, v);
+    }
+    __syncthreads();
+    const uint32_t kept = s.kept;
+    if (kept > KEEP) return exact_row<T, THREADS>(a, s, row);
+    u64 over[KEEP / 256];                                // what this thread looks after and is not among the first k, 0: nothing
+    constexpr int Q = KEEP > THREADS ? KEEP / THREADS : 1;
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const uint32_t i = q * THREADS + t;
+        over[q] = 0;
+        if (i >= kept) continue;
+        const u64 mine = s.keep[i];
         uint32_t place = 0;
-        for (uint32_t j = 0; j < got; j++) place += s.found[j] > mine;
-        const float v = value_of((uint32_t)(mine >> 32));
+        for (uint32_t j = 0; j < kept; j++) place += s.keep[j] > mine;
         if (place < a.k) {
-            a.values[row * a.k + place] = to_float<T>(z[~(uint32_t)mine]);      // as it stands there: -0, the NaN's bits
-            a.index[row * a.k + place] = (int32_t)~(uint32_t)mine;
+            const uint32_t at = ~(uint32_t)mine;
+            a.values[row * a.k + place] = to_float<T>(z[at]);          // as it stands there: -0, the NaN's bits
+            a.index[row * a.k + place] = (int32_t)at;
+        } else {
+            over[q] = mine;
+            most = fmaxf(most, value_of((uint32_t)(mine >> 32)));
         }
-        s.dropped[place] = v;
     }
     if (!a.rest) return;
-    __syncthreads();
-    for (uint32_t i = a.k + t; i < got; i += THREADS) {
-        const float v = s.dropped[i], to = fmaxf(m, v);
-        sum = sum * exp2_fast((m - to) * c) + (v == INFINITY ? INFINITY : v == -INFINITY ? 0.0f : exp2_fast((v - to) * c));
-        m = to;
+    bool lost = false;                                   // a NaN among the rest
+    most = group_max<WAVES>(most, s.room);
+    u64 more = 0;
+    auto add = [&](float v) {
+        lost = lost || v != v;
+        if (v != -INFINITY && most != INFINITY) more += (u64)(exp2_fast((v - most) * c) * 0x1p44f);
+    };
+    for (uint32_t i = t; i < got * N; i += THREADS) {
+        const float v = to_float<T>(((const raw*)s.aside)[i]);
+        if (v < least) add(v);
     }
-    const float most = group_max<WAVES>(m, s.room);
-    sum = group_sum<WAVES>(sum == 0.0f ? 0.0f : most == INFINITY ? sum : sum * exp2_fast((m - most) * c), s.room);
-    if (t == 0) a.rest[row] = most == INFINITY ? INFINITY : logf(sum) + most / a.tau;
+#pragma unroll
+    for (int q = 0; q < Q; q++)
+        if (over[q]) add(value_of((uint32_t)(over[q] >> 32)));
+    if (more) atomicAdd((unsigned long long*)&s.more, (unsigned long long)more);
+    sum = group_sum<WAVES>(most == INFINITY ? 0.0f : sum * exp2_fast((m - most) * c), s.room);
+    lost = __syncthreads_or(lost);
+    if (t == 0) a.rest[row] = lost ? NAN : most == INFINITY ? INFINITY : logf(sum + (float)s.more * 0x1p-44f) + most / a.tau;
 }
 
 extern "C" int32_t he_top_logits(he_ctx* ctx, const he_top_plan* p) {
