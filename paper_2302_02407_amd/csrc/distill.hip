@@ -1,10 +1,11 @@
 // Distillation loss against a teacher's top logits, mixed with the label's cross entropy, and its gradient.
 //
-// Of a row's logits z the indices that the teacher names are few: they and the label are handled one a thread, and the pass over the
-// row sums the others against their own maximum m: S = sum exp((z - m)/tau), S1 = sum exp(z - m).  The rest's probability then keeps
-// its relative accuracy however small it is.  With the sums over all, Z and Z1 (against the same m), the gradient at an index that
-// the teacher does not name is
-//   exp((z - m)/tau) * (1 - alpha) tau (1/Z - P_rest/S) + exp(z - m) * alpha/Z1,
+// Of a row's logits z the indices that the teacher names are few: they and the label are handled apart, and the pass over the row
+// sums the others.  The rest's probability then keeps its relative accuracy however small it is.  With c = log2(e) / tau all sums are of
+// 2^(c z - R) for a reference R that is a number of its own, near c times the largest z: the difference is one multiply-add with one
+// rounding, so nothing is lost where logits are large.  With S the sum over the indices that are not named, Z over all, and S1, Z1 the
+// same at temperature 1 (reference R1), the gradient at an index that is not named is
+//   2^(c z - R) * (1 - alpha) tau (1/Z - P_rest/S) + 2^(log2(e) z - R1) * alpha/Z1,
 // two factors a row.  Where no rest is given (P_rest = 0) nothing has to be told apart and the pass sums over all.
 #include "plain.h"
 
@@ -19,147 +20,295 @@ struct DistillArgs {
     float tau, alpha;
 };
 
+// A sum of powers of two against its reference: value * 2^ref
+struct Sum {
+    float ref, value;
+};
+#define NOTHING -3e38f     // the reference of a sum without a term
+__device__ __forceinline__ float ref_or_0(float r) { return r == NOTHING ? 0.0f : r; }
+__device__ __forceinline__ void raise(Sum& s, float ref) {
+    if (ref > s.ref) {
+        s.value *= exp2_fast(s.ref - ref);
+        s.ref = ref;
+    }
+}
+// Over a wavefront, then over the work group (room: 2 floats a wavefront; a barrier before it is used again is the caller's)
+__device__ __forceinline__ Sum wave_total(Sum s) {
+    const float r = wave_max(s.ref);
+    return {r, wave_sum(s.value == 0.0f ? 0.0f : s.value * exp2_fast(s.ref - r))};
+}
+template <int WAVES> __device__ __forceinline__ Sum total_of(const Sum* w) {
+    Sum s = w[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; i++) s.ref = fmaxf(s.ref, w[i].ref);
+    s.value = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; i++) s.value += w[i].value == 0.0f ? 0.0f : w[i].value * exp2_fast(w[i].ref - s.ref);
+    return s;
+}
+
 // What a row's threads share
-struct RowShared {
-    float t[HE_TOP_MAX], zt[HE_TOP_MAX], p[HE_TOP_MAX];   // the teacher's value / tau, the student's logit, the teacher's probability
-    int32_t at[HE_TOP_MAX];                               // index, -1: not there
-    float room[16];
+template <int WAVES> struct RowShared {
+    int32_t at[HE_TOP_MAX];         // the teacher's indices, -1: not there
+    struct Entry {
+        float t, z, p;              // value / tau, the student's logit, probability
+        int32_t first;              // there, and the first with its index
+    } entry[HE_TOP_MAX];
+    float label_z;
+    float teacher[5];               // P_rest, log of the sum over all (against the largest), log P_rest, the largest, whether anything is there
+    int32_t put_at[HE_TOP_MAX + 1]; // where the gradient is written last, -1: nowhere; the label at the end
+    float put[HE_TOP_MAX + 1];
+    Sum part[2][WAVES];
+    float factor[4];                // R, R1, and the factors of the two powers
 };
 
-// Maximum and sums over the indices that the teacher names: thread j < k holds entry j
-struct Named {
-    bool live;        // entry j is there and the first with its index
-    float z;          // student's logit
-};
+// The teacher's entries of a row and what goes with them, by one wavefront, entry lane + 64 u; in LDS until the sums are there
+template <class T, int WAVES> __device__ __forceinline__ void named_entries(const DistillArgs& a, RowShared<WAVES>& s, u64 row, const typename T::raw* z, uint32_t lane) {
+    int32_t at[2];
+    float t[2], zt[2], x[2];
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+        const uint32_t j = lane + 64 * u;
+        at[u] = -1;
+        t[u] = zt[u] = -INFINITY;
+        if (j < a.k) {
+            const int32_t i = a.index[row * a.k + j];
+            if (i >= 0 && (uint32_t)i < a.vocab) {
+                at[u] = i;
+                t[u] = a.values[row * a.k + j] / a.tau;
+                zt[u] = to_float<T>(z[i]);
+            }
+        }
+        s.at[j] = at[u];
+    }
+    const float r = a.rest ? a.rest[row] : -INFINITY, high = fmaxf(wave_max(fmaxf(t[0], t[1])), r), most = high == -INFINITY ? 0.0f : high;
+#pragma unroll
+    for (int u = 0; u < 2; u++) x[u] = exp2_fast((t[u] - most) * HE_LOG2E);
+    const float xr = exp2_fast((r - most) * HE_LOG2E), top = wave_sum(x[0] + x[1]), all = top + xr, all_log = logf(all);
+    const bool any = !(all == 0.0f);
+    wave_sync();
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+        const uint32_t j = lane + 64 * u;
+        bool first = at[u] >= 0;
+        if (first)
+            for (uint32_t i = 0; i < j; i++)
+                if (s.at[i] == at[u]) first = false;
+        s.entry[j] = {t[u], zt[u], any ? x[u] / all : 0.0f, first};
+    }
+    if (lane == 0) {
+        s.teacher[0] = any ? xr / all : 0.0f;
+        s.teacher[1] = all_log;
+        s.teacher[2] = xr >= top ? -log1pf(top / xr) : r - most - all_log;     // where the rest has nearly all, what it lacks
+        s.teacher[3] = most;
+        s.teacher[4] = any ? 1.0f : 0.0f;
+    }
+    wave_sync();
+}
 
-// LOSS: writes the loss (and the statistics); GRAD: writes the gradient.  GRAD alone takes m, S, S1 from the statistics.
-template <class T, bool LOSS, bool GRAD, bool REST> __global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
+// One row a work group.  LOSS: writes the loss (and the statistics); GRAD: writes the gradient; REST: the rest counts as one outcome.
+// GRAD alone takes the sums from the statistics.  The row is read twice, 16 bytes a lane: once for the sums (against each lane's running
+// reference) and once for the gradient, the second time from the caches: what the rows of all work groups at work hold (at most 512 of
+// 256 KiB) stays in the last level's 256 MiB.
+template <class T, class R_, int THREADS, bool LOSS, bool GRAD, bool REST> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void distill_kernel(DistillArgs a) {
     using raw = typename T::raw;
-    __shared__ RowShared s;
+    constexpr int N = Vec<T>::N, WAVES = THREADS / 64;
+    __shared__ RowShared<WAVES> s;
     extern __shared__ uint32_t named[];                   // REST: a bit for each index that the teacher names
     const u64 row = blockIdx.x;
-    const uint32_t t = threadIdx.x;
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const raw* z = (const raw*)a.z + row * a.ld_z;
     raw* grad = (raw*)a.grad + row * a.ld_grad;
+    const R_ in{z, a.vocab};
+    const uint32_t turns = (in.pieces() + THREADS - 1) / THREADS;
     const int32_t label = a.labels ? a.labels[row] : 0;
-    const float weight = GRAD ? a.weights[row] : 0.0f;
     if (a.labels && label < 0) {
         if (LOSS && t == 0) a.loss[row] = 0;
         if (LOSS && a.stats && t < 4) a.stats[row * 4 + t] = 0;
-        if (GRAD) for (uint32_t i = t; i < a.vocab; i += 256) grad[i] = 0;
+        if (GRAD)
+            for (uint32_t p = 0; p < turns; p++) in.store(grad, p * THREADS + t, Vec<T>{{0, 0, 0, 0}});
         return;
     }
-    const float inv_tau = 1.0f / a.tau, c = HE_LOG2E / a.tau;
     const uint32_t words = (a.vocab + 31) / 32;
-    if (REST) for (uint32_t i = t; i < words; i += 256) named[i] = 0;
-    float tv = -INFINITY, zt = -INFINITY;
-    int32_t at = -1;
-    if (t < a.k) {
-        at = a.index[row * a.k + t];
-        if (at < 0 || (uint32_t)at >= a.vocab) at = -1;
-        if (at >= 0) {
-            tv = a.values[row * a.k + t] / a.tau;
-            zt = to_float<T>(z[at]);
+    const float c = HE_LOG2E / a.tau;
+    const bool ce_on = a.alpha > 0.0f && a.labels && (uint32_t)label < a.vocab, two = ce_on && a.tau != 1.0f;
+    Vec<T> one = in.load(t), two_ = in.load(THREADS + t);
+    if (REST && LOSS) {
+        for (uint32_t i = t; i < words; i += THREADS) named[i] = 0;
+        __syncthreads();
+    }
+    if (wave == 0) {
+        named_entries<T, WAVES>(a, s, row, z, lane);
+        if (REST && LOSS)
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+                if (const int32_t at = s.at[lane + 64 * u]; at >= 0) atomicOr(&named[at >> 5], 1u << (at & 31));
+        if (lane == 0 && ce_on) s.label_z = to_float<T>(z[label]);
+    }
+    Sum S = {NOTHING, 0}, S1 = {NOTHING, 0};
+    if (LOSS) {
+        if (REST) __syncthreads();
+        auto turn = [&](uint32_t p, Vec<T>& buf) {
+            const uint32_t v = p * THREADS + t, base = in.base(v), past = v * N - base;
+            float x[N];
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = buf[i];
+            buf = in.load(v + 2 * THREADS);
+            uint32_t out = 0;
+            if (REST) {
+                out = named[base >> 5] >> (base & 31);
+                if (past && (base & 31) > 32 - N && (base >> 5) + 1 < words) out |= named[(base >> 5) + 1] << (32 - (base & 31));   // across two words
+            }
+            out &= (1u << N) - 1;
+            if (past) out |= (1u << min(past, (uint32_t)N)) - 1;
+            if (out)
+#pragma unroll
+                for (int i = 0; i < N; i++)
+                    if (out >> i & 1) x[i] = -INFINITY;
+            float most = x[0];
+#pragma unroll
+            for (int i = 1; i < N; i++) most = fmaxf(most, x[i]);
+            if (!(most > HE_MASKED)) most = -INFINITY;
+            raise(S, most * c);
+            const float R = ref_or_0(S.ref);
+#pragma unroll
+            for (int i = 0; i < N; i++) S.value += exp2_fast(fmaf(x[i], c, -R));
+            if (two) {
+                raise(S1, most * HE_LOG2E);
+                const float R1 = ref_or_0(S1.ref);
+#pragma unroll
+                for (int i = 0; i < N; i++) S1.value += exp2_fast(fmaf(x[i], HE_LOG2E, -R1));
+            }
+        };
+        for (uint32_t p = 0; p < turns; p += 2) {
+            turn(p, one);
+            if (p + 1 < turns) turn(p + 1, two_);
         }
-        s.at[t] = at;
-        s.t[t] = tv;
-        s.zt[t] = zt;
-    }
-    __syncthreads();
-    bool first = at >= 0;                                 // the first entry with its index
-    if (t < a.k && at >= 0) {
-        for (uint32_t j = 0; j < t; j++) first = first && s.at[j] != at;
-        if (REST) atomicOr(&named[at >> 5], 1u << (at & 31));
-    }
-    // the teacher: P_j, P_rest
-    const float tr = REST ? a.rest[row] : -INFINITY;
-    const float tm = fmaxf(group_max<4>(tv, s.room), tr), tm0 = tm == -INFINITY ? 0.0f : tm;
-    const float et = exp2_fast((tv - tm0) * HE_LOG2E), er = exp2_fast((tr - tm0) * HE_LOG2E);
-    const float ttop = group_sum<4>(et, s.room), tall = ttop + er;
-    const bool taught = !(tall == 0.0f);
-    const float p = taught ? et / tall : 0.0f, pr = taught ? er / tall : 0.0f;
-    if (t < a.k) s.p[t] = p;
-    __syncthreads();
-    const bool kl_on = taught && a.alpha < 1.0f, ce_on = a.alpha > 0.0f && a.labels && (uint32_t)label < a.vocab;
-    const float zl = ce_on ? to_float<T>(z[label]) : 0.0f;
-    // the student's indices that are not named (all of them without a rest)
-    float m, S, S1;
-    if (LOSS) {
-        m = -INFINITY;
-        for (uint32_t i = t; i < a.vocab; i += 256)
-            if (!REST || !(named[i >> 5] >> (i & 31) & 1)) m = fmaxf(m, to_float<T>(z[i]));
-        m = group_max<4>(m, s.room);
-    } else {
-        m = a.stats[row * 4];
-        S = a.stats[row * 4 + 1];
-        S1 = a.stats[row * 4 + 2];
-    }
-    const float m0 = m == -INFINITY ? 0.0f : m;
-    if (LOSS) {
-        S = S1 = 0;
-        for (uint32_t i = t; i < a.vocab; i += 256)
-            if (!REST || !(named[i >> 5] >> (i & 31) & 1)) {
-                const float d = to_float<T>(z[i]) - m0;
-                S += exp2_fast(d * c);
-                S1 += exp2_fast(d * HE_LOG2E);
-            }
-        S = group_sum<4>(S, s.room);
-        S1 = group_sum<4>(S1, s.room);
-    }
-    // all: against M, the larger of the two maxima
-    const float mt = group_max<4>(REST ? zt : -INFINITY, s.room), M = fmaxf(m, mt), M0 = M == -INFINITY ? 0.0f : M;
-    const float top = group_sum<4>(REST && first ? exp2_fast((zt - M0) * c) : 0.0f, s.room);
-    const float top1 = group_sum<4>(REST && first ? exp2_fast((zt - M0) * HE_LOG2E) : 0.0f, s.room);
-    const float down = exp2_fast((m0 - M0) * c), down1 = exp2_fast((m0 - M0) * HE_LOG2E);
-    const float Z = top + S * down, Z1 = top1 + S1 * down1;
-    const bool dead = Z == 0.0f;                          // nothing but -infinity
-    if (LOSS) {
-        const float term = p > 0.0f ? p * ((tv - tm0 - logf(tall)) - ((zt - M0) * inv_tau - logf(Z))) : 0.0f;
-        float kl = group_sum<4>(term, s.room);
-        if (t == 0) {
-            if (REST && pr > 0.0f) {
-                const float lp = er >= ttop ? -log1pf(ttop / er) : tr - tm0 - logf(tall);
-                const float lq = S * down >= top ? -log1pf(top / (S * down)) : (m0 - M0) * inv_tau + logf(S) - logf(Z);
-                kl += pr * (lp - lq);
-            }
-            float loss = 0;
-            if (kl_on && !dead) loss = (1.0f - a.alpha) * a.tau * a.tau * kl;
-            if (ce_on && !dead) loss += a.alpha * (logf(Z1) - (zl - M0));
-            a.loss[row] = loss;
-            if (a.stats) {
-                a.stats[row * 4] = m;
-                a.stats[row * 4 + 1] = S;
-                a.stats[row * 4 + 2] = S1;
-                a.stats[row * 4 + 3] = 0;
-            }
+        if (GRAD) {                                       // on their way while the sums are joined
+            one = in.load(t);
+            two_ = in.load(THREADS + t);
         }
-    }
-    if (GRAD) {
-        const float wk = kl_on && !dead ? weight * (1.0f - a.alpha) * a.tau : 0.0f, wc = ce_on && !dead ? weight * a.alpha : 0.0f;
-        const float fk = dead ? 0.0f : wk * (down / Z - (S > 0.0f ? pr / S : 0.0f)), fc = dead ? 0.0f : wc * (down1 / Z1);
-        for (uint32_t i = t; i < a.vocab; i += 256) {
-            const float d = to_float<T>(z[i]) - m0;
-            const float g = (fk != 0.0f ? fk * exp2_fast(d * c) : 0.0f) + (fc != 0.0f ? fc * exp2_fast(d * HE_LOG2E) : 0.0f);
-            grad[i] = from_float<T>(g);
+        S = wave_total(S);
+        if (two) S1 = wave_total(S1);
+        if (lane == 0) {
+            s.part[0][wave] = S;
+            s.part[1][wave] = S1;
         }
         __syncthreads();
-        // the named indices and the label, each by one thread
-        if (t < a.k && first) {
-            float q = 0;
-            for (uint32_t j = 0; j < a.k; j++) q += s.at[j] == at ? s.p[j] : 0.0f;
-            float g = dead ? 0.0f : wk * (exp2_fast((zt - M0) * c) / Z - q) + wc * (exp2_fast((zt - M0) * HE_LOG2E) / Z1);
-            if (ce_on && at == label) g -= wc;
-            grad[at] = from_float<T>(g);
+    }
+    if (wave == 0) {
+        if (LOSS) {
+            S = total_of<WAVES>(s.part[0]);
+            S1 = two ? total_of<WAVES>(s.part[1]) : S;
+        } else {
+            S = {a.stats[row * 4], a.stats[row * 4 + 1]};
+            S1 = {a.stats[row * 4 + 2], a.stats[row * 4 + 3]};
         }
-        if (ce_on && t == 255) {
-            bool alone = true;
-            for (uint32_t j = 0; j < a.k; j++) alone = alone && s.at[j] != label;
-            if (alone && !dead) {
-                const float d = zl - m0;
-                grad[label] = from_float<T>((fk != 0.0f ? fk * exp2_fast(d * c) : 0.0f) + fc * exp2_fast(d * HE_LOG2E) - wc);
+        struct {
+            int32_t at[2];
+            float t[2], z[2], p[2];
+            bool first[2];
+        } e;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const auto& n = s.entry[lane + 64 * u];
+            e.at[u] = s.at[lane + 64 * u];
+            e.t[u] = n.t;
+            e.z[u] = n.z;
+            e.p[u] = n.p;
+            e.first[u] = n.first;
+        }
+        const float rest = s.teacher[0], all_log = s.teacher[1], rest_log = s.teacher[2], teacher_most = s.teacher[3], zl = ce_on ? s.label_z : 0.0f;
+        // all: against the larger of the reference and the named logits' largest
+        const float c1 = two ? HE_LOG2E : c, zt = fmaxf(REST && e.first[0] ? e.z[0] : -INFINITY, REST && e.first[1] ? e.z[1] : -INFINITY), zm = wave_max(zt);
+        const float M = !(zm > HE_MASKED) ? S.ref : fmaxf(S.ref, zm * c), M1 = !(zm > HE_MASKED) ? S1.ref : fmaxf(S1.ref, zm * c1);
+        const float R = ref_or_0(M), R1 = ref_or_0(M1);
+        float x[2], x1[2];
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            x[u] = e.at[u] >= 0 ? exp2_fast(fmaf(e.z[u], c, -R)) : 0.0f;
+            x1[u] = e.at[u] >= 0 ? exp2_fast(fmaf(e.z[u], c1, -R1)) : 0.0f;
+        }
+        const float top = wave_sum(REST ? (e.first[0] ? x[0] : 0.0f) + (e.first[1] ? x[1] : 0.0f) : 0.0f);
+        const float top1 = wave_sum(REST ? (e.first[0] ? x1[0] : 0.0f) + (e.first[1] ? x1[1] : 0.0f) : 0.0f);
+        const float down = exp2_fast(S.ref - M), down1 = exp2_fast(S1.ref - M1), others = S.value * down;
+        const float Z = top + others, Z1 = top1 + S1.value * down1;
+        const bool dead = Z == 0.0f;                      // nothing but -infinity
+        const bool kl_on = s.teacher[4] != 0.0f && a.alpha < 1.0f && !dead, ce = ce_on && !dead;
+        if (LOSS) {
+            const float log_z = logf(Z);
+            float term = 0;
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+                if (e.p[u] > 0.0f) term += e.p[u] * ((e.t[u] - teacher_most - all_log) - (fmaf(e.z[u], c, -R) * HE_LN2 - log_z));
+            float kl = wave_sum(term);
+            if (REST && rest > 0.0f) {
+                const float lq = others >= top ? -log1pf(top / others) : (S.ref - M) * HE_LN2 + logf(S.value) - log_z;
+                kl += rest * (rest_log - lq);
+            }
+            if (lane == 0) {
+                float loss = kl_on ? (1.0f - a.alpha) * a.tau * a.tau * kl : 0.0f;
+                if (ce) loss += a.alpha * (logf(Z1) - fmaf(zl, c1, -R1) * HE_LN2);
+                a.loss[row] = loss;
+                if (a.stats) {
+                    a.stats[row * 4] = S.ref;
+                    a.stats[row * 4 + 1] = S.value;
+                    a.stats[row * 4 + 2] = S1.ref;
+                    a.stats[row * 4 + 3] = S1.value;
+                }
+            }
+        }
+        if (GRAD) {
+            const float weight = a.weights[row], wk = kl_on ? weight * (1.0f - a.alpha) * a.tau : 0.0f, wc = ce ? weight * a.alpha : 0.0f;
+            float fk = dead ? 0.0f : wk * (down / Z - (S.value > 0.0f ? rest / S.value : 0.0f)), fc = dead ? 0.0f : wc * (down1 / Z1);
+            const float label_power = ce ? exp2_fast(fmaf(zl, c1, -ref_or_0(S1.ref))) : 0.0f, label_power_k = ce ? exp2_fast(fmaf(zl, c, -ref_or_0(S.ref))) : 0.0f;
+            const bool alone = __all(e.at[0] != label && e.at[1] != label);
+            if (lane == 0) {
+                s.factor[0] = ref_or_0(S.ref);
+                s.factor[1] = ref_or_0(S1.ref);
+                s.factor[2] = two ? fk : fk + fc;         // one temperature: one power
+                s.factor[3] = fc;
+                s.put_at[HE_TOP_MAX] = ce && alone ? label : -1;
+                s.put[HE_TOP_MAX] = (fk != 0.0f ? fk * label_power_k : 0.0f) + fc * label_power - wc;
+            }
+            // what stands at the named indices, and at the label's if it is none of them, is written once all else is
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const uint32_t j = lane + 64 * u;
+                float q = 0;
+                if (e.first[u])
+                    for (uint32_t i = 0; i < a.k; i++) q += s.at[i] == e.at[u] ? s.entry[i].p : 0.0f;
+                float g = dead ? 0.0f : wk * (x[u] / Z - q) + wc * (x1[u] / Z1);
+                if (ce && e.at[u] == label) g -= wc;
+                s.put_at[j] = e.first[u] ? e.at[u] : -1;
+                s.put[j] = g;
             }
         }
     }
+    if (!GRAD) return;
+    __syncthreads();
+    const float R = s.factor[0], R1 = s.factor[1], fk = s.factor[2], fc = s.factor[3];
+    auto turn = [&](uint32_t p, Vec<T>& buf) {
+        const uint32_t v = p * THREADS + t;
+        const Vec<T> x = buf;
+        buf = in.load(v + 2 * THREADS);
+        float y[N];
+#pragma unroll
+        for (int i = 0; i < N; i++) y[i] = fk * exp2_fast(fmaf(x[i], c, -R));
+        if (two)
+#pragma unroll
+            for (int i = 0; i < N; i++) y[i] = fmaf(fc, exp2_fast(fmaf(x[i], HE_LOG2E, -R1)), y[i]);
+        Vec<T> g;
+        g.set(y);
+        in.store(grad, v, g);
+    };
+    for (uint32_t p = 0; p < turns; p += 2) {
+        turn(p, one);
+        if (p + 1 < turns) turn(p + 1, two_);
+    }
+    __syncthreads();
+    for (uint32_t i = t; i <= HE_TOP_MAX; i += THREADS)
+        if (s.put_at[i] >= 0) grad[s.put_at[i]] = from_float<T>(s.put[i]);
 }
 
 static int32_t check(he_ctx* ctx, const he_distill_plan* p, const char* who) {
@@ -200,14 +349,22 @@ static int32_t check_operands(he_ctx* ctx, const he_distill_plan* p, const char*
     return HE_OK;
 }
 
+template <class R> struct Of { using type = R; };
 template <bool LOSS, bool GRAD> static void launch(he_ctx* ctx, const he_distill_plan* p) {
     const DistillArgs a = {p->d_z, p->d_values, p->d_rest, p->d_row_weights, p->d_index, p->d_labels, p->d_loss, p->d_stats, p->d_grad, p->ld_z, p->ld_grad,
                            p->vocab, p->k, p->tau, p->alpha};
-    const uint32_t lds = p->d_rest ? (p->vocab + 31) / 32 * 4 : 0;
+    const uint32_t lds = p->d_rest && LOSS ? (p->vocab + 31) / 32 * 4 : 0;
     with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        if (p->d_rest) distill_kernel<T, LOSS, GRAD, true><<<p->rows, 256, lds, ctx->stream>>>(a);
-        else distill_kernel<T, LOSS, GRAD, false><<<p->rows, 256, 0, ctx->stream>>>(a);
+        auto go = [&](auto threads, auto row) {
+            constexpr int THREADS = decltype(threads)::value;
+            using R = typename decltype(row)::type;
+            if (p->d_rest) distill_kernel<T, R, THREADS, LOSS, GRAD, true><<<p->rows, THREADS, lds, ctx->stream>>>(a);
+            else distill_kernel<T, R, THREADS, LOSS, GRAD, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
+        };
+        if (p->vocab < (uint32_t)Vec<T>::N) go(std::integral_constant<int, 64>{}, Of<ShortRow<T>>{});
+        else if ((uint64_t)p->vocab * dtype_bytes(p->dtype) > 32768) go(std::integral_constant<int, 1024>{}, Of<Row<T>>{});
+        else go(std::integral_constant<int, 256>{}, Of<Row<T>>{});
     });
 }
 

@@ -3,10 +3,13 @@
 #ifndef HE_PLAIN_H
 #define HE_PLAIN_H
 
+#include <type_traits>
+
 #include "he_internal.h"
 
 #define HE_LOG2E 1.44269504088896340736f
 #define HE_LN2 0.69314718055994530942f
+#define HE_MASKED -0x1p126f      // a logit from here down counts as -infinity in a sum (the lowest number of a type, times log2(e), is none)
 
 struct f32_t { using raw = uint32_t; };
 struct bf16_t { using raw = uint16_t; };
@@ -22,6 +25,12 @@ template <> __device__ __forceinline__ uint16_t from_float<bf16_t>(float v) { re
 template <> __device__ __forceinline__ uint16_t from_float<f16_t>(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, -inf -> 0
+
+// What the lanes of a wavefront have written to LDS is there for its other lanes after this
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) {
 #pragma unroll
@@ -59,6 +68,24 @@ template <class T> struct Vec {
         else if constexpr (__is_same(T, bf16_t)) return __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
         else return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i / 2] >> 16 * (i & 1)));
     }
+    __device__ __forceinline__ void set(const float* v) {
+        if constexpr (N == 4)
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = __builtin_bit_cast(uint32_t, v[i]);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                typedef float f2 __attribute__((ext_vector_type(2)));
+                const f2 p = {v[2 * i], v[2 * i + 1]};
+                if constexpr (__is_same(T, bf16_t)) {
+                    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+                    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, b2));
+                } else {
+                    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+                    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, h2));
+                }
+            }
+    }
     __device__ __forceinline__ void set(int i, float v) {
         const raw r = from_float<T>(v);
         if constexpr (N == 4) w[i] = r;
@@ -80,6 +107,37 @@ template <class T> struct Row {
         Vec<T> x;
         x.load(p + base(v));
         return x;
+    }
+    // Piece v of a row that is written: all of it, or of a last one what is its own
+    __device__ __forceinline__ void store(raw* to, uint32_t v, const Vec<T>& x) const {
+        const uint32_t at = base(v), past = v * N - at;
+        if (past == 0) x.store(to + at);
+        else
+#pragma unroll
+            for (uint32_t i = 0; i < N; i++)
+                if (i >= past) to[at + i] = from_float<T>(x[i]);
+    }
+};
+// The same of a row of fewer than N elements: piece 0 with -infinity after them
+template <class T> struct ShortRow {
+    using raw = typename T::raw;
+    static constexpr uint32_t N = Vec<T>::N;
+    const raw* p;
+    uint32_t n;
+    __device__ __forceinline__ uint32_t pieces() const { return 1; }
+    __device__ __forceinline__ uint32_t base(uint32_t) const { return 0; }
+    __device__ __forceinline__ Vec<T> load(uint32_t) const {
+        float x[N];
+#pragma unroll
+        for (uint32_t i = 0; i < N; i++) x[i] = i < n ? to_float<T>(p[i]) : -INFINITY;
+        Vec<T> v;
+        v.set(x);
+        return v;
+    }
+    __device__ __forceinline__ void store(raw* to, uint32_t v, const Vec<T>& x) const {
+#pragma unroll
+        for (uint32_t i = 0; i < N; i++)
+            if (v == 0 && i < n) to[i] = from_float<T>(x[i]);
     }
 };
 
