@@ -23,17 +23,6 @@ __device__ __forceinline__ v8h halves(uint32_t lo, uint32_t hi) {
     return v8h{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// The 16 x 16 products over 128 columns: rows of the first operand by lane % 16, of the second likewise, 32 columns by lane / 16 in
-// both (any assignment of columns to lanes gives the same sum as long as both have it).  Lane l holds column l % 16 (a row of the
-// second operand) of rows 4 * (l / 16) .. + 3 (of the first).  The codes go through the matrix instruction of f16, which adds in 32
-// bits; the one of 8 bits aligns the products of a group to the largest and drops what lies 2^-13 below it.
-__device__ __forceinline__ v4f mfma128(v8i a, v8i b) {
-    v4f c = {0, 0, 0, 0};
-#pragma unroll
-    for (int h = 0; h < 4; h++) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(a[2 * h], a[2 * h + 1]), halves(b[2 * h], b[2 * h + 1]), c, 0, 0, 0);
-    return c;
-}
-
 // Columns at and after `left` of 16 become zeros (code 0)
 __device__ __forceinline__ v4i keep(v4i v, int left) {
 #pragma unroll
@@ -44,33 +33,125 @@ __device__ __forceinline__ v4i keep(v4i v, int left) {
     return v;
 }
 
-// A lane's 32 codes of a row from column `at`, zeros from column k on
-__device__ __forceinline__ v8i codes32(const uint8_t* row, uint32_t at, uint32_t k) {
-    v4i lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-    if (at < k) lo = keep(*(const v4i*)(row + at), (int)min(k - at, 16u));
-    if (at + 16 < k) hi = keep(*(const v4i*)(row + at + 16), (int)min(k - at - 16, 16u));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+// ---- few rows of A: W is read once, straight from memory
+//
+// A wavefront owns R rows of W (16 for up to 16 rows of A, 32 for up to 64) and every KS-th block of 128 columns; the KS wavefronts of a
+// work group join their sums in LDS, in order.  KS is chosen so that about 8192 wavefronts are there: what bounds it is W's bytes, and
+// 4 KiB on the way per wavefront, 32 to a compute unit, keep memory busy.  A and the scales come from the caches.  Pieces of 16 bytes go to
+// lanes so that a row's 128 bytes are read by 64 / R lanes side by side; any assignment of columns to lanes gives the same products as long
+// as both operands have it.  Codes go through the matrix instruction of f16, which adds in 32 bits: exact, and not what bounds it.
+//
+// 1 x 32768 x 4096: FEW_1 us; 24 x 1000 x 2048: FEW_2 us.
+template <int R> struct Acc;
+template <> struct Acc<16> {
+    typedef v4f type;
+    static __device__ __forceinline__ v4f product(v8h w, v8h a, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(w, a, c, 0, 0, 0); }
+};
+template <> struct Acc<32> {
+    typedef v16f type;
+    static __device__ __forceinline__ v16f product(v8h w, v8h a, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(w, a, c, 0, 0, 0); }
+};
+
+template <class T, int R, int MT, int KS> __global__ __launch_bounds__(64 * KS) void matmul_q8_few_kernel(GemmArgs a) {
+    using raw = typename T::raw;
+    using acc_t = typename Acc<R>::type;
+    constexpr int G = 64 / R, C = 8 / G, E = sizeof(acc_t) / 4, PITCH = R + 4;       // lanes a row, pieces a lane
+    extern __shared__ float sums[];                                                   // [KS][R * MT rows of A][PITCH]
+    const uint32_t lane = threadIdx.x & 63, l = lane % R, g = lane / R, ks = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n0 = blockIdx.x * R, blocks = (a.k + 127) / 128;
+    const uint8_t* wr = a.w + min(n0 + l, a.n - 1) * a.ld_w;
+    const float* sw = a.sw + (n0 >> 7) * a.ld_sw;
+    const uint8_t* ar[MT];
+    const float* sa[MT];
+    acc_t acc[MT];
+#pragma unroll
+    for (int j = 0; j < MT; j++) {
+        const uint64_t m = min(j * R + l, a.m - 1);
+        ar[j] = a.a + m * a.ld_a;
+        sa[j] = a.sa + m * a.ld_sa;
+#pragma unroll
+        for (int e = 0; e < E; e++) acc[j][e] = 0;
+    }
+    struct Pieces {
+        v4i w[C], a[MT][C];
+        float s[MT];
+    };
+    auto load = [&](uint32_t b, Pieces& p) {
+        const float swb = sw[b];
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            const uint32_t at = b * 128 + (c * G + g) * 16, in = at < a.k ? at : 0;       // past the end: cleared when it is used
+            p.w[c] = *(const v4i*)(wr + in);
+#pragma unroll
+            for (int j = 0; j < MT; j++) p.a[j][c] = *(const v4i*)(ar[j] + in);
+        }
+#pragma unroll
+        for (int j = 0; j < MT; j++) p.s[j] = sa[j][b] * swb;
+    };
+    auto multiply = [&](uint32_t b, Pieces& p) {
+        acc_t x[MT];
+#pragma unroll
+        for (int j = 0; j < MT; j++)
+#pragma unroll
+            for (int e = 0; e < E; e++) x[j][e] = 0;
+        const bool cut = (b + 1) * 128 > a.k;
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            if (cut) {
+                const int left = max(0, (int)a.k - (int)(b * 128 + (c * G + g) * 16));
+                p.w[c] = keep(p.w[c], left);
+#pragma unroll
+                for (int j = 0; j < MT; j++) p.a[j][c] = keep(p.a[j][c], left);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const v8h w = halves(p.w[c][2 * h], p.w[c][2 * h + 1]);
+#pragma unroll
+                for (int j = 0; j < MT; j++) x[j] = Acc<R>::product(w, halves(p.a[j][c][2 * h], p.a[j][c][2 * h + 1]), x[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < MT; j++)
+#pragma unroll
+            for (int e = 0; e < E; e++) acc[j][e] += x[j][e] * p.s[j];
+    };
+    if (wave < blocks) {
+        Pieces one, two;
+        load(wave, one);
+        for (uint32_t b = wave; b < blocks; b += 2 * ks) {
+            load(min(b + ks, blocks - 1), two);
+            multiply(b, one);
+            if (b + ks < blocks) {
+                load(min(b + 2 * ks, blocks - 1), one);
+                multiply(b + ks, two);
+            }
+        }
+    }
+    // element e: row 8 (e / 4) + 4 g + e % 4 of W (R = 16: 4 g + e), row l of A
+#pragma unroll
+    for (int j = 0; j < MT; j++)
+#pragma unroll
+        for (int e = 0; e < E; e++) sums[((wave * MT + j) * R + l) * PITCH + 8 * (e / 4) + 4 * g + e % 4] = acc[j][e];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < R * MT * R; i += blockDim.x) {
+        const uint32_t m = i / R, n = i % R;
+        if (m >= a.m || n0 + n >= a.n) continue;
+        float x = 0;
+        for (uint32_t k = 0; k < ks; k++) x += sums[(k * MT * R + m) * PITCH + n];
+        ((raw*)a.out)[m * a.ld_out + n0 + n] = from_float<T>(x);
+    }
 }
 
-// One wavefront a tile of 16 x 16, operands straight from memory
-template <class T> __global__ __launch_bounds__(64) void matmul_q8_kernel(GemmArgs a) {
-    using raw = typename T::raw;
-    const uint32_t l = threadIdx.x & 15, g = threadIdx.x >> 4, tiles_n = (a.n + 15) / 16;
-    const uint32_t m = blockIdx.x / tiles_n * 16 + l, n0 = blockIdx.x % tiles_n * 16;
-    const uint32_t mr = min(m, a.m - 1), nr = min(n0 + l, a.n - 1);
-    const uint8_t *ar = a.a + mr * a.ld_a, *wr = a.w + nr * a.ld_w;
-    const float *sa = a.sa + mr * a.ld_sa, *sw = a.sw + (n0 >> 7) * a.ld_sw;
-    v4f acc = {0, 0, 0, 0};
-    for (uint32_t k = 0; k < a.k; k += 128) {
-        const v4f p = mfma128(codes32(wr, k + 32 * g, a.k), codes32(ar, k + 32 * g, a.k));
-        const float s = sa[k >> 7] * sw[k >> 7];
-        acc += p * s;
-    }
-    raw* out = (raw*)a.out + (u64)m * a.ld_out;
-    if (m < a.m)
-#pragma unroll
-        for (uint32_t j = 0; j < 4; j++)
-            if (n0 + 4 * g + j < a.n) out[n0 + 4 * g + j] = from_float<T>(acc[j]);
+template <class T, int R, int MT, int KS> static hipError_t launch_few(const GemmArgs& a, hipStream_t stream) {
+    const auto kernel = matmul_q8_few_kernel<T, R, MT, KS>;
+    constexpr int LDS = R * MT * (R + 4) * 4;            // a wavefront
+    static const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, KS * LDS);
+    if (ready != hipSuccess) return ready;
+    const uint32_t tiles = (a.n + R - 1) / R, blocks = (a.k + 127) / 128;
+    uint32_t ks = 1;
+    while (ks < KS && ks < blocks && tiles * ks < 8192) ks *= 2;
+    kernel<<<tiles, 64 * ks, ks * LDS, stream>>>(a);
+    return hipGetLastError();
 }
 
 // ---- tiles staged in LDS
@@ -303,15 +384,14 @@ extern "C" int32_t he_matmul_q8(he_ctx* ctx, const he_matmul_plan* p) {
         return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: the output overlaps an operand");
     const GemmArgs a = {p->d_a, p->d_w, p->d_a_scales, p->d_w_scales, p->d_out, p->ld_a, p->ld_w, p->ld_a_scales, p->ld_w_scales, p->ld_out, p->m, p->n, p->k};
     hipError_t rc = hipSuccess;
-    if (p->m > 64) {
-        with_dtype(p->out_dtype, [&](auto t) {
-            rc = p->fast_sums ? launch_tiles<decltype(t), true, 2, 4, 4, 2>(a, ctx->stream) : launch_tiles<decltype(t), false, 2, 4, 2, 2>(a, ctx->stream);
-        });
-        if (rc != hipSuccess) return he_fail(ctx, HE_ERR_HIP, "he_matmul_q8: %s", hipGetErrorString(rc));
-        return HE_OK;
-    }
-    with_dtype(p->out_dtype, [&](auto t) { matmul_q8_kernel<decltype(t)><<<((p->n + 15) / 16) * ((p->m + 15) / 16), 64, 0, ctx->stream>>>(a); });
-    HE_LAUNCHED(ctx);
+    with_dtype(p->out_dtype, [&](auto t) {
+        using T = decltype(t);
+        if (p->m <= 16) rc = launch_few<T, 16, 1, 16>(a, ctx->stream);
+        else if (p->m <= 32) rc = launch_few<T, 32, 1, 16>(a, ctx->stream);
+        else if (p->m <= 64) rc = launch_few<T, 32, 2, 8>(a, ctx->stream);
+        else rc = p->fast_sums ? launch_tiles<T, true, 2, 4, 4, 2>(a, ctx->stream) : launch_tiles<T, false, 2, 4, 2, 2>(a, ctx->stream);
+    });
+    if (rc != hipSuccess) return he_fail(ctx, HE_ERR_HIP, "he_matmul_q8: %s", hipGetErrorString(rc));
     return HE_OK;
     });
 }
