@@ -413,6 +413,8 @@ typedef struct {
     uint64_t ld_out;
 } he_matmul_plan;
 int32_t he_matmul_q8(he_ctx* ctx, const he_matmul_plan* plan);
+/* Workspace of a product with these m, n, k (0 for most: only where the sum's axis is cut in parts). */
+int32_t he_ws_query_matmul_q8(const he_ctx* ctx, const he_matmul_plan* plan, uint64_t* h_bytes);
 
 /* The k largest logits of every row in descending order, the lowest index first among equals (a NaN counts as larger than any
  * number, -0 equals +0), and d_rest[row] = log of the sum over the row's OTHER logits z of exp(z / tau): -infinity where nothing

@@ -20,7 +20,7 @@ EXPORTS = [
     "he_ntt", "he_intt", "he_automorph", "he_evk_register", "he_keyswitch", "he_rotate_hoisted", "he_rotate_batch", "he_rotate",
     "he_conjugate", "he_ptct_mac", "he_add", "he_addpt", "he_mulct", "he_affine", "he_rescale", "he_conv2d", "he_raconv",
     "he_probe_alu", "he_build_id", "he_rotate_sum", "he_ws_query_raconv", "he_ca_ra_block", "he_ws_query_ca_ra_block", "he_ras", "he_ws_bytes", "he_ws_reserve", "he_ws_query_rotate_batch", "he_ws_query_conv2d", "he_rescale_noalloc", "he_ptct_mac_rot",
-    "he_rmsnorm_q8", "he_matmul_q8", "he_top_logits", "he_distill_loss", "he_distill_grad",
+    "he_rmsnorm_q8", "he_matmul_q8", "he_top_logits", "he_distill_loss", "he_distill_grad", "he_ws_query_matmul_q8",
 ]
 
 
@@ -145,6 +145,7 @@ def load():
         "he_ptct_mac_rot": [vp, vp, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(u32), u32, u32, i32],
         "he_rmsnorm_q8": [vp, C.POINTER(RmsNormPlan)],
         "he_matmul_q8": [vp, C.POINTER(MatmulPlan)],
+        "he_ws_query_matmul_q8": [vp, C.POINTER(MatmulPlan), u64p],
         "he_top_logits": [vp, C.POINTER(TopPlan)],
         "he_distill_loss": [vp, C.POINTER(DistillPlan)],
         "he_distill_grad": [vp, C.POINTER(DistillPlan)],
@@ -580,6 +581,11 @@ class HEContext:
         plan = MatmulPlan(m, n, k, _DTYPE[out.dtype], 1 if fast_sums else 0, da, lda, dsa, ldsa, dw, ldw, dsw, ldsw, do, ldo)
         self._ck(self._lib.he_matmul_q8(self._h, C.byref(plan)))
         return out
+
+    def he_ws_query_matmul_q8(self, m, n, k):
+        v = C.c_uint64()
+        self._ck(self._lib.he_ws_query_matmul_q8(self._h, C.byref(MatmulPlan(m, n, k)), C.byref(v)))
+        return v.value
 
     def he_top_logits(self, z, tau, values, index, rest=None):
         """values, index [rows][k]: the k largest of every row of z in order; rest [rows]: log-sum-exp of the others / tau."""

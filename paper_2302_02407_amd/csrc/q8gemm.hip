@@ -14,6 +14,8 @@ struct GemmArgs {
     void* out;
     u64 ld_a, ld_w, ld_sa, ld_sw, ld_out;
     uint32_t m, n, k;
+    uint32_t per;      // tiles: blocks of 128 columns a part of the sum's axis takes
+    u64 part;          // ... and elements from one part's results to the next's
 };
 
 // Eight codes as f16: exact, an e4m3 number has 4 bits of mantissa and 18 binary orders.
@@ -33,87 +35,65 @@ __device__ __forceinline__ v4i keep(v4i v, int left) {
     return v;
 }
 
-// ---- few rows of A: W is read once, straight from memory
+// ---- up to 16 rows of A: W is read once, straight from memory
 //
-// A wavefront owns R rows of W (16 for up to 16 rows of A, 32 for up to 64) and every KS-th block of 128 columns; the KS wavefronts of a
-// work group join their sums in LDS, in order.  KS is chosen so that about 8192 wavefronts are there: what bounds it is W's bytes, and
-// 4 KiB on the way per wavefront, 32 to a compute unit, keep memory busy.  A and the scales come from the caches.  Pieces of 16 bytes go to
-// lanes so that a row's 128 bytes are read by 64 / R lanes side by side; any assignment of columns to lanes gives the same products as long
-// as both operands have it.  Codes go through the matrix instruction of f16, which adds in 32 bits: exact, and not what bounds it.
+// A wavefront owns NT times 16 rows of W and every KS-th block of 128 columns; the KS wavefronts of a work group join their sums in LDS, in
+// order.  KS is chosen so that about 8192 wavefronts are there: what bounds it is W's bytes, and the pieces on the way of 32
+// wavefronts to a compute unit keep memory busy.  A and the scales come from the caches, A's pieces once for the NT tiles.  Pieces of 16
+// bytes go to lanes so that four lanes side by side read 64 bytes of a row; any assignment of columns to lanes gives the same products as
+// long as both operands have it.  Codes go through the matrix instruction of f16, which adds in 32 bits: exact, and not what bounds it.
 //
-// 1 x 32768 x 4096: FEW_1 us; 24 x 1000 x 2048: FEW_2 us.
-template <int R> struct Acc;
-template <> struct Acc<16> {
-    typedef v4f type;
-    static __device__ __forceinline__ v4f product(v8h w, v8h a, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(w, a, c, 0, 0, 0); }
-};
-template <> struct Acc<32> {
-    typedef v16f type;
-    static __device__ __forceinline__ v16f product(v8h w, v8h a, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(w, a, c, 0, 0, 0); }
-};
-
-template <class T, int R, int MT, int KS> __global__ __launch_bounds__(64 * KS) void matmul_q8_few_kernel(GemmArgs a) {
+// 1 x 32768 x 4096: 28.7 us (4.7 TB/s).
+template <class T, int NT> __global__ __launch_bounds__(1024) void matmul_q8_few_kernel(GemmArgs a) {
     using raw = typename T::raw;
-    using acc_t = typename Acc<R>::type;
-    constexpr int G = 64 / R, C = 8 / G, E = sizeof(acc_t) / 4, PITCH = R + 4;       // lanes a row, pieces a lane
-    extern __shared__ float sums[];                                                   // [KS][R * MT rows of A][PITCH]
-    const uint32_t lane = threadIdx.x & 63, l = lane % R, g = lane / R, ks = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t n0 = blockIdx.x * R, blocks = (a.k + 127) / 128;
-    const uint8_t* wr = a.w + min(n0 + l, a.n - 1) * a.ld_w;
-    const float* sw = a.sw + (n0 >> 7) * a.ld_sw;
-    const uint8_t* ar[MT];
-    const float* sa[MT];
-    acc_t acc[MT];
+    constexpr int PITCH = 20;
+    extern __shared__ float sums[];                                                   // [KS][NT][16 rows of A][PITCH]
+    const uint32_t lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, ks = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t n0 = blockIdx.x * (16 * NT), blocks = (a.k + 127) / 128, m = min(l, a.m - 1);
+    const uint8_t *wr[NT], *ar = a.a + m * a.ld_a;
+    const float *sw = a.sw + (n0 >> 7) * a.ld_sw, *sa = a.sa + m * a.ld_sa;
+    v4f acc[NT];
 #pragma unroll
-    for (int j = 0; j < MT; j++) {
-        const uint64_t m = min(j * R + l, a.m - 1);
-        ar[j] = a.a + m * a.ld_a;
-        sa[j] = a.sa + m * a.ld_sa;
-#pragma unroll
-        for (int e = 0; e < E; e++) acc[j][e] = 0;
+    for (int i = 0; i < NT; i++) {
+        wr[i] = a.w + min(n0 + 16 * i + l, a.n - 1) * a.ld_w;
+        acc[i] = v4f{0, 0, 0, 0};
     }
     struct Pieces {
-        v4i w[C], a[MT][C];
-        float s[MT];
+        v4i w[NT][2], a[2];
+        float s;
     };
     auto load = [&](uint32_t b, Pieces& p) {
-        const float swb = sw[b];
 #pragma unroll
-        for (int c = 0; c < C; c++) {
-            const uint32_t at = b * 128 + (c * G + g) * 16, in = at < a.k ? at : 0;       // past the end: cleared when it is used
-            p.w[c] = *(const v4i*)(wr + in);
+        for (int c = 0; c < 2; c++) {
+            const uint32_t at = b * 128 + (c * 4 + g) * 16, in = at < a.k ? at : 0;       // past the end: cleared when it is used
 #pragma unroll
-            for (int j = 0; j < MT; j++) p.a[j][c] = *(const v4i*)(ar[j] + in);
+            for (int i = 0; i < NT; i++) p.w[i][c] = *(const v4i*)(wr[i] + in);
+            p.a[c] = *(const v4i*)(ar + in);
         }
-#pragma unroll
-        for (int j = 0; j < MT; j++) p.s[j] = sa[j][b] * swb;
+        p.s = sa[b] * sw[b];
     };
     auto multiply = [&](uint32_t b, Pieces& p) {
-        acc_t x[MT];
+        v4f x[NT];
 #pragma unroll
-        for (int j = 0; j < MT; j++)
-#pragma unroll
-            for (int e = 0; e < E; e++) x[j][e] = 0;
+        for (int i = 0; i < NT; i++) x[i] = v4f{0, 0, 0, 0};
         const bool cut = (b + 1) * 128 > a.k;
 #pragma unroll
-        for (int c = 0; c < C; c++) {
+        for (int c = 0; c < 2; c++) {
             if (cut) {
-                const int left = max(0, (int)a.k - (int)(b * 128 + (c * G + g) * 16));
-                p.w[c] = keep(p.w[c], left);
+                const int left = max(0, (int)a.k - (int)(b * 128 + (c * 4 + g) * 16));
+                p.a[c] = keep(p.a[c], left);
 #pragma unroll
-                for (int j = 0; j < MT; j++) p.a[j][c] = keep(p.a[j][c], left);
+                for (int i = 0; i < NT; i++) p.w[i][c] = keep(p.w[i][c], left);
             }
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const v8h w = halves(p.w[c][2 * h], p.w[c][2 * h + 1]);
+                const v8h y = halves(p.a[c][2 * h], p.a[c][2 * h + 1]);
 #pragma unroll
-                for (int j = 0; j < MT; j++) x[j] = Acc<R>::product(w, halves(p.a[j][c][2 * h], p.a[j][c][2 * h + 1]), x[j]);
+                for (int i = 0; i < NT; i++) x[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(p.w[i][c][2 * h], p.w[i][c][2 * h + 1]), y, x[i], 0, 0, 0);
             }
         }
 #pragma unroll
-        for (int j = 0; j < MT; j++)
-#pragma unroll
-            for (int e = 0; e < E; e++) acc[j][e] += x[j][e] * p.s[j];
+        for (int i = 0; i < NT; i++) acc[i] += x[i] * p.s;
     };
     if (wave < blocks) {
         Pieces one, two;
@@ -127,30 +107,29 @@ template <class T, int R, int MT, int KS> __global__ __launch_bounds__(64 * KS) 
             }
         }
     }
-    // element e: row 8 (e / 4) + 4 g + e % 4 of W (R = 16: 4 g + e), row l of A
+    // element e: row 4 g + e of W, row l of A
 #pragma unroll
-    for (int j = 0; j < MT; j++)
+    for (int i = 0; i < NT; i++)
 #pragma unroll
-        for (int e = 0; e < E; e++) sums[((wave * MT + j) * R + l) * PITCH + 8 * (e / 4) + 4 * g + e % 4] = acc[j][e];
+        for (int e = 0; e < 4; e++) sums[((wave * NT + i) * 16 + l) * PITCH + 4 * g + e] = acc[i][e];
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < R * MT * R; i += blockDim.x) {
-        const uint32_t m = i / R, n = i % R;
-        if (m >= a.m || n0 + n >= a.n) continue;
+    for (uint32_t i = threadIdx.x; i < 256 * NT; i += blockDim.x) {
+        const uint32_t r = i / (16 * NT), n = i % (16 * NT);
+        if (r >= a.m || n0 + n >= a.n) continue;
         float x = 0;
-        for (uint32_t k = 0; k < ks; k++) x += sums[(k * MT * R + m) * PITCH + n];
-        ((raw*)a.out)[m * a.ld_out + n0 + n] = from_float<T>(x);
+        for (uint32_t k = 0; k < ks; k++) x += sums[((k * NT + n / 16) * 16 + r) * PITCH + n % 16];
+        ((raw*)a.out)[r * a.ld_out + n0 + n] = from_float<T>(x);
     }
 }
 
-template <class T, int R, int MT, int KS> static hipError_t launch_few(const GemmArgs& a, hipStream_t stream) {
-    const auto kernel = matmul_q8_few_kernel<T, R, MT, KS>;
-    constexpr int LDS = R * MT * (R + 4) * 4;            // a wavefront
-    static const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, KS * LDS);
-    if (ready != hipSuccess) return ready;
-    const uint32_t tiles = (a.n + R - 1) / R, blocks = (a.k + 127) / 128;
+template <class T> static hipError_t launch_few(const GemmArgs& a, hipStream_t stream) {
+    const uint32_t blocks = (a.k + 127) / 128, wide = (a.n + 31) / 32;
+    const bool pairs = wide >= 512;                      // enough of them to fill the card
+    const uint32_t tiles = pairs ? wide : (a.n + 15) / 16;
     uint32_t ks = 1;
-    while (ks < KS && ks < blocks && tiles * ks < 8192) ks *= 2;
-    kernel<<<tiles, 64 * ks, ks * LDS, stream>>>(a);
+    while (ks < 16 && ks < blocks && tiles * ks < 8192) ks *= 2;
+    if (pairs) matmul_q8_few_kernel<T, 2><<<tiles, 64 * ks, ks * 2 * 16 * 20 * 4, stream>>>(a);
+    else matmul_q8_few_kernel<T, 1><<<tiles, 64 * ks, ks * 16 * 20 * 4, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -208,11 +187,11 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
     if (!tile_of((a.n + G::BN - 1) / G::BN, (a.m + G::BM - 1) / G::BM, n0, m0)) return;
     n0 *= G::BN;
     m0 *= G::BM;
-    const uint32_t blocks = (a.k + 127) / 128;
+    const uint32_t first = blockIdx.y * a.per, blocks = min((a.k + 127) / 128 - first, a.per), k = a.k - first * 128;     // this part's
 
     // a wavefront fills eight rows at a time: lane i the piece i % 8 of row i / 8
     constexpr int WAVES = WN * WM, FW = G::BN / 8 / WAVES, FA = G::BM / 8 / WAVES, FILLS = FW + FA;
-    const uint8_t *w0 = a.w + n0 * a.ld_w, *a0 = a.a + m0 * a.ld_a;
+    const uint8_t *w0 = a.w + n0 * a.ld_w + first * 128, *a0 = a.a + m0 * a.ld_a + first * 128;
     const uint32_t piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
     uint32_t off[FILLS];                               // ld <= 2^23: 256 rows stay below 2^31
 #pragma unroll
@@ -221,14 +200,14 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
         off[f] = f < FW ? min(r, a.n - 1 - n0) * (uint32_t)a.ld_w : min(r, a.m - 1 - m0) * (uint32_t)a.ld_a;
     }
     auto fill = [&](uint32_t b, int from, int end) {
-        const uint32_t at = b * 128 + piece * 16, in = at < a.k ? at : 0;          // past the end: anything that is there, cleared below
+        const uint32_t at = b * 128 + piece * 16, in = at < k ? at : 0;          // past the end: anything that is there, cleared below
         uint8_t* to = lds + (b & 1) * G::BYTES + wave * 1024;
 #pragma unroll
         for (int f = from; f < end; f++)
             __builtin_amdgcn_global_load_lds((gptr)((f < FW ? w0 : a0) + (off[f] + in)), (lptr)(to + f * WAVES * 1024), 16, 0, 0);
     };
     float* scales = (float*)(lds + 2 * G::BYTES);
-    const float* sw = a.sw + min(n0 + wn * TN * 32, a.n - 1) / 128 * a.ld_sw;
+    const float* sw = a.sw + min(n0 + wn * TN * 32, a.n - 1) / 128 * a.ld_sw + first;
     v16f acc[TN][TM];
 #pragma unroll
     for (int i = 0; i < TN; i++)
@@ -243,7 +222,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
             float* to = scales + (b >> 3 & 1) * 8 * G::BM;
             for (uint32_t i = tid; i < 8 * G::BM; i += G::THREADS) {
                 const uint32_t r = i / 8, c = b + i % 8;
-                to[i % 8 * G::BM + r] = c < blocks ? a.sa[min(m0 + r, a.m - 1) * a.ld_sa + c] : 0.0f;
+                to[i % 8 * G::BM + r] = c < blocks ? a.sa[min(m0 + r, a.m - 1) * a.ld_sa + first + c] : 0.0f;
             }
         }
         const float swb = sw[b];
@@ -251,8 +230,8 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
         __syncthreads();
         if (!FAST && b + 1 < blocks) fill(b + 1, 0, FILLS);
         uint8_t* buf = lds + (b & 1) * G::BYTES;
-        if (b + 1 == blocks && (a.k & 127)) {            // columns past the end become zeros, in both operands
-            const uint32_t left = a.k & 127;
+        if (b + 1 == blocks && b * 128 + 128 > k) {            // columns past the end become zeros, in both operands
+            const uint32_t left = k & 127;
             for (uint32_t i = tid; i < (G::BN + G::BM) * 8; i += G::THREADS) {
                 const uint32_t r = i >> 3, c = (i & 7) ^ (r >> 1 & 7);
                 v4i* p = (v4i*)(buf + i * 16);
@@ -277,7 +256,8 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
                 for (int h = 0; h < 2; h++) wf[h] = fragment(wb + i * 4096, 4 * h + 2 * g, l);
 #pragma unroll
                 for (int j = 0; j < TM; j++) {
-                    if (i < 2 && b + 1 < blocks) fill(b + 1, (i * TM + j) * FILLS / 4, (i * TM + j + 1) * FILLS / 4);
+                    constexpr int HALF = (TN * TM + 1) / 2;
+                    if (i * TM + j < HALF && b + 1 < blocks) fill(b + 1, (i * TM + j) * FILLS / HALF, (i * TM + j + 1) * FILLS / HALF);
                     v16f p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[0], af[j][0], zero16(), 0, 0, 0, 0, 0, 0);
                     p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[1], af[j][1], p, 0, 0, 0, 0, 0, 0);
 #pragma unroll
@@ -319,9 +299,10 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
     // so that a row's are written in a piece: TN * 32 in a row, 16 bytes a lane.
     constexpr int ES = sizeof(raw), PITCH = TN * 32 * ES + 16, LANES = TN * 32 * ES / 16;    // lanes a row
     static_assert(WAVES * 32 * PITCH <= G::LDS, "the staged results fit");
+    raw* const results = (raw*)a.out + blockIdx.y * a.part;
     uint8_t* mine = lds + wave * 32 * PITCH;
     const uint32_t nw = n0 + wn * TN * 32;
-    const bool whole = !(((uintptr_t)a.out | a.ld_out * ES) & 15) && nw + TN * 32 <= a.n;
+    const bool whole = !(((uintptr_t)results | a.ld_out * ES) & 15) && nw + TN * 32 <= a.n;
 #pragma unroll
     for (int j = 0; j < TM; j++) {
         __syncthreads();
@@ -340,34 +321,92 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
 #pragma unroll
             for (int r = 0; r < 32; r += 64 / LANES) {
                 const uint32_t row = r + lane / LANES, at = lane % LANES * 16;
-                if (mw + row < a.m) *(v4i*)((uint8_t*)a.out + ((mw + row) * a.ld_out + nw) * ES + at) = *(const v4i*)(mine + row * PITCH + at);
+                if (mw + row < a.m) *(v4i*)((uint8_t*)results + ((mw + row) * a.ld_out + nw) * ES + at) = *(const v4i*)(mine + row * PITCH + at);
             }
         } else {
             for (uint32_t r = 0; r < 32 && mw + r < a.m; r++)
                 for (uint32_t n = lane; n < TN * 32 && nw + n < a.n; n += 64)
-                    ((raw*)a.out)[(mw + r) * a.ld_out + nw + n] = ((const raw*)(mine + r * PITCH))[n];
+                    results[(mw + r) * a.ld_out + nw + n] = ((const raw*)(mine + r * PITCH))[n];
         }
     }
 }
 
-template <class T, bool FAST, int WN, int WM, int TN, int TM> static hipError_t launch_tiles(const GemmArgs& a, hipStream_t stream) {
+// Sums the parts' results, in order
+template <class T> __global__ __launch_bounds__(256) void matmul_q8_join_kernel(const float* parts, uint32_t n_parts, u64 part, u64 ld_part, typename T::raw* out, u64 ld_out, uint32_t n) {
+    const uint32_t i = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const float* p = parts + blockIdx.y * ld_part + i;
+    v4f x = *(const v4f*)p;
+    for (uint32_t k = 1; k < n_parts; k++) x += *(const v4f*)(p + k * part);
+#pragma unroll
+    for (uint32_t e = 0; e < 4; e++)
+        if (i + e < n) out[blockIdx.y * ld_out + i + e] = from_float<T>(x[e]);
+}
+
+template <class T, bool FAST, int WN, int WM, int TN, int TM> static hipError_t launch_tiles(const GemmArgs& a, uint32_t parts, hipStream_t stream) {
     using G = Tile<WN, WM, TN, TM>;
     const auto kernel = matmul_q8_tiles_kernel<T, FAST, WN, WM, TN, TM>;
     static const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
     if (ready != hipSuccess) return ready;
     const uint32_t tiles = ((a.n + G::BN - 1) / G::BN) * ((a.m + G::BM - 1) / G::BM);
-    kernel<<<(tiles + 7) / 8 * 8, G::THREADS, G::LDS, stream>>>(a);
+    kernel<<<dim3((tiles + 7) / 8 * 8, parts), G::THREADS, G::LDS, stream>>>(a);
     return hipGetLastError();
+}
+
+// How a product of more than 16 rows of A is cut: rows of W and of A to a tile, parts of the sum's axis.  Tiles of 256 x 256 read least
+// and run fastest once there are enough of them for the 256 compute units; below, smaller ones, of which two or three share a unit, and
+// where these do not fill the card either, the sum's axis in parts of at least 4 blocks, joined by a second kernel.
+struct Cut {
+    uint32_t bn, bm, parts, per;
+};
+static Cut cut_of(uint32_t m, uint32_t n, uint32_t k) {
+    const uint32_t blocks = (k + 127) / 128;
+    auto tiles = [&](uint32_t bn, uint32_t bm) { return ((n + bn - 1) / bn) * ((m + bm - 1) / bm); };
+    Cut c = {128, m <= 32 ? 32u : m <= 64 ? 64u : 128u, 1, blocks};
+    if (m > 128 && tiles(256, 256) >= 224) c.bn = c.bm = 256;
+    const uint32_t want = c.bm == 256 ? 0 : 512, have = tiles(c.bn, c.bm);
+    if (have < want) {
+        const uint32_t parts = min(min((want + have - 1) / have, blocks / 4), 16u);
+        if (parts > 1) {
+            c.per = (blocks + parts - 1) / parts;
+            c.parts = (blocks + c.per - 1) / c.per;
+        }
+    }
+    return c;
+}
+static uint64_t cut_bytes(const Cut& c, uint32_t m, uint32_t n) { return c.parts > 1 ? (uint64_t)c.parts * m * ((n + 3) & ~3u) * 4 : 0; }
+
+template <class T> static hipError_t run_tiles(const GemmArgs& a, const Cut& c, bool fast, hipStream_t stream) {
+    if (c.bm == 256) return fast ? launch_tiles<T, true, 2, 4, 4, 2>(a, c.parts, stream) : launch_tiles<T, false, 2, 4, 2, 2>(a, c.parts, stream);
+    if (c.bm == 128) return fast ? launch_tiles<T, true, 2, 2, 2, 2>(a, c.parts, stream) : launch_tiles<T, false, 2, 2, 2, 2>(a, c.parts, stream);
+    if (c.bm == 64) return launch_tiles<T, false, 2, 2, 2, 1>(a, c.parts, stream);
+    return launch_tiles<T, false, 4, 1, 1, 1>(a, c.parts, stream);
+}
+
+static int32_t check_matmul(he_ctx* ctx, const he_matmul_plan* p, const char* who) {
+    if (!p) return he_fail(ctx, HE_ERR_BADARG, "%s: null plan", who);
+    if (!dtype_known(p->out_dtype)) return he_fail(ctx, HE_ERR_BADARG, "%s: unknown type %d", who, p->out_dtype);
+    if (p->k == 0 || p->k > (1u << 20)) return he_fail(ctx, HE_ERR_BADARG, "%s: %u columns to sum over, outside 1..2^20", who, p->k);
+    if (p->m > (1u << 20) || p->n > (1u << 20)) return he_fail(ctx, HE_ERR_BADARG, "%s: more than 2^20 rows", who);
+    if ((uint64_t)p->m * p->n > 1ull << 33) return he_fail(ctx, HE_ERR_BADARG, "%s: more than 2^33 results", who);
+    return HE_OK;
+}
+
+extern "C" int32_t he_ws_query_matmul_q8(const he_ctx* ctx, const he_matmul_plan* p, uint64_t* h_bytes) {
+    return he_guard(ctx, "he_ws_query_matmul_q8: host allocation failed", [&]() -> int32_t {
+    if (!ctx || !h_bytes) return HE_ERR_BADARG;
+    const int32_t rc = check_matmul(const_cast<he_ctx*>(ctx), p, "he_ws_query_matmul_q8");
+    if (rc != HE_OK) return rc;
+    *h_bytes = p->m > 16 && p->n ? cut_bytes(cut_of(p->m, p->n, p->k), p->m, p->n) : 0;
+    return HE_OK;
+    });
 }
 
 extern "C" int32_t he_matmul_q8(he_ctx* ctx, const he_matmul_plan* p) {
     return he_guard(ctx, "he_matmul_q8: host allocation failed", [&]() -> int32_t {
     if (!ctx) return HE_ERR_BADARG;
-    if (!p) return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: null plan");
-    if (!dtype_known(p->out_dtype)) return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: unknown type %d", p->out_dtype);
-    if (p->k == 0 || p->k > (1u << 20)) return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: %u columns to sum over, outside 1..2^20", p->k);
-    if (p->m > (1u << 20) || p->n > (1u << 20)) return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: more than 2^20 rows");
-    if ((uint64_t)p->m * p->n > 1ull << 33) return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: more than 2^33 results");
+    int32_t rc = check_matmul(ctx, p, "he_matmul_q8");
+    if (rc != HE_OK) return rc;
     if (p->m == 0 || p->n == 0) return HE_OK;
     if (!p->d_a || !p->d_w || !p->d_a_scales || !p->d_w_scales || !p->d_out) return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: null argument");
     const uint32_t kb = (p->k + 127) / 128, nb = (p->n + 127) / 128, es = dtype_bytes(p->out_dtype);
@@ -382,16 +421,29 @@ extern "C" int32_t he_matmul_q8(he_ctx* ctx, const he_matmul_plan* p) {
     if (overlap(p->d_out, no, p->d_a, span(p->m, k16, p->ld_a, 1)) || overlap(p->d_out, no, p->d_w, span(p->n, k16, p->ld_w, 1)) ||
         overlap(p->d_out, no, p->d_a_scales, span(p->m, kb, p->ld_a_scales, 4)) || overlap(p->d_out, no, p->d_w_scales, span(nb, kb, p->ld_w_scales, 4)))
         return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: the output overlaps an operand");
-    const GemmArgs a = {p->d_a, p->d_w, p->d_a_scales, p->d_w_scales, p->d_out, p->ld_a, p->ld_w, p->ld_a_scales, p->ld_w_scales, p->ld_out, p->m, p->n, p->k};
-    hipError_t rc = hipSuccess;
+    GemmArgs a = {p->d_a, p->d_w, p->d_a_scales, p->d_w_scales, p->d_out, p->ld_a, p->ld_w, p->ld_a_scales, p->ld_w_scales, p->ld_out, p->m, p->n, p->k, kb, 0};
+    const Cut c = cut_of(p->m, p->n, p->k);
+    const bool parts = p->m > 16 && c.parts > 1;
+    if (parts) {
+        if ((rc = he_ensure_ws(ctx, cut_bytes(c, p->m, p->n))) != HE_OK) return rc;
+        a.ld_out = (p->n + 3) & ~3u;
+        a.part = p->m * a.ld_out;
+        a.out = ctx->d_ws;
+        a.per = c.per;
+    }
+    hipError_t err = hipSuccess;
     with_dtype(p->out_dtype, [&](auto t) {
         using T = decltype(t);
-        if (p->m <= 16) rc = launch_few<T, 16, 1, 16>(a, ctx->stream);
-        else if (p->m <= 32) rc = launch_few<T, 32, 1, 16>(a, ctx->stream);
-        else if (p->m <= 64) rc = launch_few<T, 32, 2, 8>(a, ctx->stream);
-        else rc = p->fast_sums ? launch_tiles<T, true, 2, 4, 4, 2>(a, ctx->stream) : launch_tiles<T, false, 2, 4, 2, 2>(a, ctx->stream);
+        if (p->m <= 16) err = launch_few<T>(a, ctx->stream);
+        else if (!parts) err = run_tiles<T>(a, c, p->fast_sums != 0, ctx->stream);
+        else if ((err = run_tiles<f32_t>(a, c, p->fast_sums != 0, ctx->stream)) == hipSuccess) {
+            for (uint32_t r = 0; r < p->m; r += 65535)   // a grid's second side
+                matmul_q8_join_kernel<T><<<dim3((p->n + 1023) / 1024, min(p->m - r, 65535u)), 256, 0, ctx->stream>>>(
+                    (const float*)ctx->d_ws + r * a.ld_out, c.parts, a.part, a.ld_out, (typename T::raw*)p->d_out + r * p->ld_out, p->ld_out, p->n);
+            err = hipGetLastError();
+        }
     });
-    if (rc != hipSuccess) return he_fail(ctx, HE_ERR_HIP, "he_matmul_q8: %s", hipGetErrorString(rc));
+    if (err != hipSuccess) return he_fail(ctx, HE_ERR_HIP, "he_matmul_q8: %s", hipGetErrorString(err));
     return HE_OK;
     });
 }
