@@ -6,6 +6,7 @@ is no CPU fallback: if the library is missing or a call fails, an exception is r
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -66,30 +67,14 @@ class BlockPlan(C.Structure):
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # he_dtype
 _CODES = (torch.uint8, torch.float8_e4m3fn)
+_F32 = (torch.float32,)
 
 
-class RmsNormPlan(C.Structure):
-    _fields_ = [("rows", C.c_uint32), ("dim", C.c_uint32), ("dtype", C.c_int32), ("eps", C.c_float), ("d_x", C.c_void_p), ("ld_x", C.c_uint64),
-                ("d_residual", C.c_void_p), ("ld_residual", C.c_uint64), ("d_weight", C.c_void_p), ("d_sum", C.c_void_p), ("ld_sum", C.c_uint64),
-                ("d_codes", C.c_void_p), ("ld_codes", C.c_uint64), ("d_scales", C.c_void_p), ("ld_scales", C.c_uint64)]
-
-
-class MatmulPlan(C.Structure):
-    _fields_ = [("m", C.c_uint32), ("n", C.c_uint32), ("k", C.c_uint32), ("out_dtype", C.c_int32), ("fast_sums", C.c_uint32), ("d_a", C.c_void_p), ("ld_a", C.c_uint64),
-                ("d_a_scales", C.c_void_p), ("ld_a_scales", C.c_uint64), ("d_w", C.c_void_p), ("ld_w", C.c_uint64),
-                ("d_w_scales", C.c_void_p), ("ld_w_scales", C.c_uint64), ("d_out", C.c_void_p), ("ld_out", C.c_uint64)]
-
-
-class TopPlan(C.Structure):
-    _fields_ = [("rows", C.c_uint32), ("vocab", C.c_uint32), ("k", C.c_uint32), ("dtype", C.c_int32), ("tau", C.c_float), ("d_z", C.c_void_p),
-                ("ld_z", C.c_uint64), ("d_values", C.c_void_p), ("d_index", C.c_void_p), ("d_rest", C.c_void_p)]
-
-
-class DistillPlan(C.Structure):
-    _fields_ = [("rows", C.c_uint32), ("vocab", C.c_uint32), ("k", C.c_uint32), ("dtype", C.c_int32), ("tau", C.c_float), ("alpha", C.c_float),
-                ("d_z", C.c_void_p), ("ld_z", C.c_uint64), ("d_values", C.c_void_p), ("d_index", C.c_void_p), ("d_rest", C.c_void_p),
-                ("d_labels", C.c_void_p), ("d_loss", C.c_void_p), ("d_stats", C.c_void_p), ("d_row_weights", C.c_void_p),
-                ("d_grad", C.c_void_p), ("ld_grad", C.c_uint64)]
+# The plans of the plaintext side as they lie in memory (the fields of the C structures in their order, native alignment)
+_RMSNORM = struct.Struct("@IIifPQPQPPQPQPQ")
+_MATMUL = struct.Struct("@IIIiIPQPQPQPQPQ")
+_TOP = struct.Struct("@IIIifPQPPP")
+_DISTILL = struct.Struct("@IIIiffPQPPPPPPPPQ")
 
 
 _lib = None
@@ -143,12 +128,12 @@ def load():
         "he_ws_query_conv2d": [vp, C.POINTER(ConvPlan), u64p],
         "he_rescale_noalloc": [vp, vp, u32, vp],
         "he_ptct_mac_rot": [vp, vp, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(u32), u32, u32, i32],
-        "he_rmsnorm_q8": [vp, C.POINTER(RmsNormPlan)],
-        "he_matmul_q8": [vp, C.POINTER(MatmulPlan)],
-        "he_ws_query_matmul_q8": [vp, C.POINTER(MatmulPlan), u64p],
-        "he_top_logits": [vp, C.POINTER(TopPlan)],
-        "he_distill_loss": [vp, C.POINTER(DistillPlan)],
-        "he_distill_grad": [vp, C.POINTER(DistillPlan)],
+        "he_rmsnorm_q8": [vp, C.c_char_p],
+        "he_matmul_q8": [vp, C.c_char_p],
+        "he_ws_query_matmul_q8": [vp, C.c_char_p, u64p],
+        "he_top_logits": [vp, C.c_char_p],
+        "he_distill_loss": [vp, C.c_char_p],
+        "he_distill_grad": [vp, C.c_char_p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -189,23 +174,24 @@ def _rows(t, what, rows, cols, dtypes):
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("%s: the elements of a row must be contiguous" % what)
-    return t.data_ptr(), max(ld, cols) if rows <= 1 else ld
+    return t.data_ptr(), ld if rows > 1 or ld > cols else cols
 
 
 def _codes(t, what, rows, cols):
     """The same for rows of codes, whose last row has to be there up to the next multiple of 16 bytes."""
     ptr, ld = _rows(t, what, rows, cols, _CODES)
-    if rows <= 1:
-        ld = -(-max(ld, cols) // 16) * 16
-    if rows and t.untyped_storage().nbytes() - t.storage_offset() < (rows - 1) * ld + -(-cols // 16) * 16:
-        raise ValueError("%s: the last row ends before the next multiple of 16 bytes" % what)
+    if cols % 16:
+        if rows <= 1:
+            ld = -(-ld // 16) * 16
+        if rows and t.untyped_storage().nbytes() - t.storage_offset() < (rows - 1) * ld + -(-cols // 16) * 16:
+            raise ValueError("%s: the last row ends before the next multiple of 16 bytes" % what)
     return ptr, ld
 
 
 def _dense(t, what, shape, dtype):
-    """Pointer of a dense tensor of that shape and type; None stays None."""
+    """Pointer of a dense tensor of that shape and type; None is a null pointer."""
     if t is None:
-        return None
+        return 0
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
         raise TypeError("%s must be a CUDA tensor of %s" % (what, dtype))
     if t.shape != shape or not t.is_contiguous():
@@ -217,6 +203,14 @@ def _matrix(t, what):
     if not (isinstance(t, torch.Tensor) and t.dim() == 2):
         raise TypeError("%s must be a matrix on the GPU" % what)
     return t.shape
+
+
+def _plain(t, what):
+    """The he_dtype of a tensor's elements."""
+    d = _DTYPE.get(t.dtype)
+    if d is None:
+        raise TypeError("%s must be %s, not %s" % (what, " or ".join(str(d) for d in _DTYPE), t.dtype))
+    return d
 
 
 def _u32arr(xs):
@@ -559,60 +553,58 @@ class HEContext:
     def he_rmsnorm_q8(self, x, codes, scales, eps, residual=None, weight=None, sum_out=None):
         """Residual addition, root-mean-square norm and 8-bit output; x, residual, sum_out [rows][dim], codes uint8 or float8_e4m3fn."""
         rows, dim = _matrix(x, "x")
-        t = (x.dtype,) if x.dtype in _DTYPE else tuple(_DTYPE)
+        d, t = _plain(x, "x"), (x.dtype,)
         dx, ldx = _rows(x, "x", rows, dim, t)
-        dr, ldr = _rows(residual, "residual", rows, dim, t) if residual is not None else (None, 0)
-        ds, lds = _rows(sum_out, "sum_out", rows, dim, t) if sum_out is not None else (None, 0)
+        dr, ldr = _rows(residual, "residual", rows, dim, t) if residual is not None else (0, 0)
+        ds, lds = _rows(sum_out, "sum_out", rows, dim, t) if sum_out is not None else (0, 0)
         dc, ldc = _codes(codes, "codes", rows, dim)
-        dk, ldk = _rows(scales, "scales", rows, -(-dim // 128), (torch.float32,))
-        plan = RmsNormPlan(rows, dim, _DTYPE[x.dtype], eps, dx, ldx, dr, ldr, _dense(weight, "weight", (dim,), x.dtype), ds, lds, dc, ldc, dk, ldk)
-        self._ck(self._lib.he_rmsnorm_q8(self._h, C.byref(plan)))
+        dk, ldk = _rows(scales, "scales", rows, -(-dim // 128), _F32)
+        self._ck(self._lib.he_rmsnorm_q8(self._h, _RMSNORM.pack(rows, dim, d, eps, dx, ldx, dr, ldr, _dense(weight, "weight", (dim,), x.dtype), ds, lds,
+                                                                dc, ldc, dk, ldk)))
         return codes
 
     def he_matmul_q8(self, a, a_scales, w, w_scales, out, fast_sums=False):
         """out [M][N] = A [M][K] times W [N][K] transposed, both codes with scales; fast_sums: sums of a block need not be exact in 32 bits."""
         (m, k), (n, _) = _matrix(a, "a"), _matrix(w, "w")
+        kb = -(-k // 128)
         da, lda = _codes(a, "a", m, k)
         dw, ldw = _codes(w, "w", n, k)
-        kb = -(-k // 128)
-        dsa, ldsa = _rows(a_scales, "a_scales", m, kb, (torch.float32,))
-        dsw, ldsw = _rows(w_scales, "w_scales", -(-n // 128), kb, (torch.float32,))
-        do, ldo = _rows(out, "out", m, n, tuple(_DTYPE))
-        plan = MatmulPlan(m, n, k, _DTYPE[out.dtype], 1 if fast_sums else 0, da, lda, dsa, ldsa, dw, ldw, dsw, ldsw, do, ldo)
-        self._ck(self._lib.he_matmul_q8(self._h, C.byref(plan)))
+        dsa, ldsa = _rows(a_scales, "a_scales", m, kb, _F32)
+        dsw, ldsw = _rows(w_scales, "w_scales", -(-n // 128), kb, _F32)
+        do, ldo = _rows(out, "out", m, n, _DTYPE)
+        self._ck(self._lib.he_matmul_q8(self._h, _MATMUL.pack(m, n, k, _DTYPE[out.dtype], 1 if fast_sums else 0, da, lda, dsa, ldsa, dw, ldw, dsw, ldsw, do, ldo)))
         return out
 
     def he_ws_query_matmul_q8(self, m, n, k):
         v = C.c_uint64()
-        self._ck(self._lib.he_ws_query_matmul_q8(self._h, C.byref(MatmulPlan(m, n, k)), C.byref(v)))
+        self._ck(self._lib.he_ws_query_matmul_q8(self._h, _MATMUL.pack(m, n, k, *[0] * 12), C.byref(v)))
         return v.value
 
     def he_top_logits(self, z, tau, values, index, rest=None):
         """values, index [rows][k]: the k largest of every row of z in order; rest [rows]: log-sum-exp of the others / tau."""
         (rows, vocab), (_, k) = _matrix(z, "z"), _matrix(values, "values")
-        dz, ldz = _rows(z, "z", rows, vocab, tuple(_DTYPE))
-        plan = TopPlan(rows, vocab, k, _DTYPE[z.dtype], tau, dz, ldz, _dense(values, "values", (rows, k), torch.float32),
-                       _dense(index, "index", (rows, k), torch.int32), _dense(rest, "rest", (rows,), torch.float32))
-        self._ck(self._lib.he_top_logits(self._h, C.byref(plan)))
+        d = _plain(z, "z")
+        dz, ldz = _rows(z, "z", rows, vocab, _DTYPE)
+        self._ck(self._lib.he_top_logits(self._h, _TOP.pack(rows, vocab, k, d, tau, dz, ldz, _dense(values, "values", (rows, k), torch.float32),
+                                                            _dense(index, "index", (rows, k), torch.int32), _dense(rest, "rest", (rows,), torch.float32))))
         return values, index, rest
 
     def _distill_plan(self, z, values, index, rest, tau, labels, alpha, loss, stats, row_weights, grad):
         (rows, vocab), (_, k) = _matrix(z, "z"), _matrix(values, "values")
-        dz, ldz = _rows(z, "z", rows, vocab, tuple(_DTYPE))
-        dg, ldg = _rows(grad, "grad", rows, vocab, (z.dtype,)) if grad is not None else (None, 0)
-        return DistillPlan(rows, vocab, k, _DTYPE[z.dtype], tau, alpha, dz, ldz, _dense(values, "values", (rows, k), torch.float32),
-                           _dense(index, "index", (rows, k), torch.int32), _dense(rest, "rest", (rows,), torch.float32),
-                           _dense(labels, "labels", (rows,), torch.int32), _dense(loss, "loss", (rows,), torch.float32),
-                           _dense(stats, "stats", (rows, 4), torch.float32), _dense(row_weights, "row_weights", (rows,), torch.float32), dg, ldg)
+        d = _plain(z, "z")
+        dz, ldz = _rows(z, "z", rows, vocab, _DTYPE)
+        dg, ldg = _rows(grad, "grad", rows, vocab, (z.dtype,)) if grad is not None else (0, 0)
+        f32, one = torch.float32, (rows,)
+        return _DISTILL.pack(rows, vocab, k, d, tau, alpha, dz, ldz, _dense(values, "values", (rows, k), f32), _dense(index, "index", (rows, k), torch.int32),
+                             _dense(rest, "rest", one, f32), _dense(labels, "labels", one, torch.int32), _dense(loss, "loss", one, f32),
+                             _dense(stats, "stats", (rows, 4), f32), _dense(row_weights, "row_weights", one, f32), dg, ldg)
 
     def he_distill_loss(self, z, values, index, rest, tau, loss, labels=None, alpha=0.0, stats=None, grad=None, row_weights=None):
         """loss [rows] of the student's logits z against the teacher's top logits; with grad also row_weights times its gradient."""
-        plan = self._distill_plan(z, values, index, rest, tau, labels, alpha, loss, stats, row_weights, grad)
-        self._ck(self._lib.he_distill_loss(self._h, C.byref(plan)))
+        self._ck(self._lib.he_distill_loss(self._h, self._distill_plan(z, values, index, rest, tau, labels, alpha, loss, stats, row_weights, grad)))
         return loss
 
     def he_distill_grad(self, z, values, index, rest, tau, stats, row_weights, grad, labels=None, alpha=0.0):
         """row_weights times the gradient of the loss by z, from the statistics that he_distill_loss left."""
-        plan = self._distill_plan(z, values, index, rest, tau, labels, alpha, None, stats, row_weights, grad)
-        self._ck(self._lib.he_distill_grad(self._h, C.byref(plan)))
+        self._ck(self._lib.he_distill_grad(self._h, self._distill_plan(z, values, index, rest, tau, labels, alpha, None, stats, row_weights, grad)))
         return grad

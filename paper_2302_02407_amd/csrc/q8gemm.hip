@@ -35,32 +35,38 @@ __device__ __forceinline__ v4i keep(v4i v, int left) {
     return v;
 }
 
-// ---- up to 16 rows of A: W is read once, straight from memory
+// ---- few rows of A and W straight from memory
 //
-// A wavefront owns NT times 16 rows of W and every KS-th block of 128 columns; the KS wavefronts of a work group join their sums in LDS, in
-// order.  KS is chosen so that about 8192 wavefronts are there: what bounds it is W's bytes, and the pieces on the way of 32
-// wavefronts to a compute unit keep memory busy.  A and the scales come from the caches, A's pieces once for the NT tiles.  Pieces of 16
-// bytes go to lanes so that four lanes side by side read 64 bytes of a row; any assignment of columns to lanes gives the same products as
-// long as both operands have it.  Codes go through the matrix instruction of f16, which adds in 32 bits: exact, and not what bounds it.
-//
-// 1 x 32768 x 4096: 28.7 us (4.7 TB/s).
-template <class T, int NT> __global__ __launch_bounds__(1024) void matmul_q8_few_kernel(GemmArgs a) {
+// A wavefront owns NT times 16 rows of W by MT times 16 rows of A and every KS-th block of 128 columns; the KS wavefronts of a work group
+// join their sums in LDS, in order.  KS is chosen so that about 8192 wavefronts are there: what bounds it is W's bytes (or, where
+// there are few of them, one launch's latency), and the pieces on the way of 32 wavefronts to a compute unit keep memory busy.  A and
+// the scales come from the caches, A's pieces once for the NT tiles.  Pieces of 16 bytes go to lanes so that four lanes side by side read
+// 64 bytes of a row; any assignment of columns to lanes gives the same products as long as both operands have it.  Codes go through
+// the matrix instruction of f16, which adds in 32 bits: exact, and not what bounds it.
+template <class T, int NT, int MT> __global__ __launch_bounds__(1024) void matmul_q8_few_kernel(GemmArgs a) {
     using raw = typename T::raw;
     constexpr int PITCH = 20;
-    extern __shared__ float sums[];                                                   // [KS][NT][16 rows of A][PITCH]
+    extern __shared__ float sums[];                                                   // [KS][NT][MT][16 rows of A][PITCH]
     const uint32_t lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, ks = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t n0 = blockIdx.x * (16 * NT), blocks = (a.k + 127) / 128, m = min(l, a.m - 1);
-    const uint8_t *wr[NT], *ar = a.a + m * a.ld_a;
-    const float *sw = a.sw + (n0 >> 7) * a.ld_sw, *sa = a.sa + m * a.ld_sa;
-    v4f acc[NT];
+    const uint32_t n0 = blockIdx.x * (16 * NT), blocks = (a.k + 127) / 128;
+    const uint8_t *wr[NT], *ar[MT];
+    const float *sw = a.sw + (n0 >> 7) * a.ld_sw, *sa[MT];
+    v4f acc[NT][MT];
+#pragma unroll
+    for (int j = 0; j < MT; j++) {
+        const uint64_t m = min(16 * j + l, a.m - 1);
+        ar[j] = a.a + m * a.ld_a;
+        sa[j] = a.sa + m * a.ld_sa;
+    }
 #pragma unroll
     for (int i = 0; i < NT; i++) {
         wr[i] = a.w + min(n0 + 16 * i + l, a.n - 1) * a.ld_w;
-        acc[i] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < MT; j++) acc[i][j] = v4f{0, 0, 0, 0};
     }
     struct Pieces {
-        v4i w[NT][2], a[2];
-        float s;
+        v4i w[NT][2], a[MT][2];
+        float s[MT];
     };
     auto load = [&](uint32_t b, Pieces& p) {
 #pragma unroll
@@ -68,32 +74,46 @@ template <class T, int NT> __global__ __launch_bounds__(1024) void matmul_q8_few
             const uint32_t at = b * 128 + (c * 4 + g) * 16, in = at < a.k ? at : 0;       // past the end: cleared when it is used
 #pragma unroll
             for (int i = 0; i < NT; i++) p.w[i][c] = *(const v4i*)(wr[i] + in);
-            p.a[c] = *(const v4i*)(ar + in);
+#pragma unroll
+            for (int j = 0; j < MT; j++) p.a[j][c] = *(const v4i*)(ar[j] + in);
         }
-        p.s = sa[b] * sw[b];
+        const float swb = sw[b];
+#pragma unroll
+        for (int j = 0; j < MT; j++) p.s[j] = sa[j][b] * swb;
     };
     auto multiply = [&](uint32_t b, Pieces& p) {
-        v4f x[NT];
+        v4f x[NT][MT];
 #pragma unroll
-        for (int i = 0; i < NT; i++) x[i] = v4f{0, 0, 0, 0};
+        for (int i = 0; i < NT; i++)
+#pragma unroll
+            for (int j = 0; j < MT; j++) x[i][j] = v4f{0, 0, 0, 0};
         const bool cut = (b + 1) * 128 > a.k;
 #pragma unroll
         for (int c = 0; c < 2; c++) {
             if (cut) {
                 const int left = max(0, (int)a.k - (int)(b * 128 + (c * 4 + g) * 16));
-                p.a[c] = keep(p.a[c], left);
+#pragma unroll
+                for (int j = 0; j < MT; j++) p.a[j][c] = keep(p.a[j][c], left);
 #pragma unroll
                 for (int i = 0; i < NT; i++) p.w[i][c] = keep(p.w[i][c], left);
             }
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const v8h y = halves(p.a[c][2 * h], p.a[c][2 * h + 1]);
+                v8h y[MT];
 #pragma unroll
-                for (int i = 0; i < NT; i++) x[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(p.w[i][c][2 * h], p.w[i][c][2 * h + 1]), y, x[i], 0, 0, 0);
+                for (int j = 0; j < MT; j++) y[j] = halves(p.a[j][c][2 * h], p.a[j][c][2 * h + 1]);
+#pragma unroll
+                for (int i = 0; i < NT; i++) {
+                    const v8h w = halves(p.w[i][c][2 * h], p.w[i][c][2 * h + 1]);
+#pragma unroll
+                    for (int j = 0; j < MT; j++) x[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, y[j], x[i][j], 0, 0, 0);
+                }
             }
         }
 #pragma unroll
-        for (int i = 0; i < NT; i++) acc[i] += x[i] * p.s;
+        for (int i = 0; i < NT; i++)
+#pragma unroll
+            for (int j = 0; j < MT; j++) acc[i][j] += x[i][j] * p.s[j];
     };
     if (wave < blocks) {
         Pieces one, two;
@@ -111,26 +131,38 @@ template <class T, int NT> __global__ __launch_bounds__(1024) void matmul_q8_few
 #pragma unroll
     for (int i = 0; i < NT; i++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) sums[((wave * NT + i) * 16 + l) * PITCH + 4 * g + e] = acc[i][e];
+        for (int j = 0; j < MT; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sums[(((wave * NT + i) * MT + j) * 16 + l) * PITCH + 4 * g + e] = acc[i][j][e];
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < 256 * NT; i += blockDim.x) {
+    for (uint32_t i = threadIdx.x; i < 256 * NT * MT; i += blockDim.x) {
         const uint32_t r = i / (16 * NT), n = i % (16 * NT);
         if (r >= a.m || n0 + n >= a.n) continue;
         float x = 0;
-        for (uint32_t k = 0; k < ks; k++) x += sums[((k * NT + n / 16) * 16 + r) * PITCH + n % 16];
+        for (uint32_t k = 0; k < ks; k++) x += sums[(((k * NT + n / 16) * MT + r / 16) * 16 + r % 16) * PITCH + n % 16];
         ((raw*)a.out)[r * a.ld_out + n0 + n] = from_float<T>(x);
     }
 }
 
-template <class T> static hipError_t launch_few(const GemmArgs& a, hipStream_t stream) {
-    const uint32_t blocks = (a.k + 127) / 128, wide = (a.n + 31) / 32;
-    const bool pairs = wide >= 512;                      // enough of them to fill the card
-    const uint32_t tiles = pairs ? wide : (a.n + 15) / 16;
+// With up to 32 rows of A: products whose W has less than 32 MiB, where the tiles below would need a second launch for the parts of the
+// sum's axis (16 x 1000 x 2048: 6.8 us, there 9.7; 16 x 10007 x 4096: 22.6, there 13.4), and those of up to 4 rows with so many of W that
+// the tiles come in one round and a third (1 x 131072 x 4096: 107 us, there 131; with 16 rows 148, there 134).
+static bool few_rows(uint32_t m, uint32_t n, uint32_t k) { return m <= 32 && ((uint64_t)n * k < 1u << 25 || (m <= 4 && n > 98304)); }
+
+template <class T, int NT, int MT> static hipError_t launch_few(const GemmArgs& a, hipStream_t stream) {
+    const auto kernel = matmul_q8_few_kernel<T, NT, MT>;
+    constexpr int LDS = NT * MT * 16 * 20 * 4;           // a wavefront
+    static const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 16 * LDS);
+    if (ready != hipSuccess) return ready;
+    const uint32_t blocks = (a.k + 127) / 128, tiles = (a.n + 16 * NT - 1) / (16 * NT);
     uint32_t ks = 1;
     while (ks < 16 && ks < blocks && tiles * ks < 8192) ks *= 2;
-    if (pairs) matmul_q8_few_kernel<T, 2><<<tiles, 64 * ks, ks * 2 * 16 * 20 * 4, stream>>>(a);
-    else matmul_q8_few_kernel<T, 1><<<tiles, 64 * ks, ks * 16 * 20 * 4, stream>>>(a);
+    kernel<<<tiles, 64 * ks, ks * LDS, stream>>>(a);
     return hipGetLastError();
+}
+template <class T> static hipError_t run_few(const GemmArgs& a, hipStream_t stream) {
+    if (a.m <= 16) return a.n >= 16384 ? launch_few<T, 2, 1>(a, stream) : launch_few<T, 1, 1>(a, stream);     // two tiles a wavefront where that fills the card
+    return launch_few<T, 1, 2>(a, stream);
 }
 
 // ---- tiles staged in LDS
@@ -353,7 +385,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> static hipError_t 
     return hipGetLastError();
 }
 
-// How a product of more than 16 rows of A is cut: rows of W and of A to a tile, parts of the sum's axis.  Tiles of 256 x 256 read least
+// How the other products are cut: rows of W and of A to a tile, parts of the sum's axis.  Tiles of 256 x 256 read least
 // and run fastest once there are enough of them for the 256 compute units; below, smaller ones, of which two or three share a unit, and
 // where these do not fill the card either, the sum's axis in parts of at least 4 blocks, joined by a second kernel.
 struct Cut {
@@ -397,7 +429,7 @@ extern "C" int32_t he_ws_query_matmul_q8(const he_ctx* ctx, const he_matmul_plan
     if (!ctx || !h_bytes) return HE_ERR_BADARG;
     const int32_t rc = check_matmul(const_cast<he_ctx*>(ctx), p, "he_ws_query_matmul_q8");
     if (rc != HE_OK) return rc;
-    *h_bytes = p->m > 16 && p->n ? cut_bytes(cut_of(p->m, p->n, p->k), p->m, p->n) : 0;
+    *h_bytes = p->m && p->n && !few_rows(p->m, p->n, p->k) ? cut_bytes(cut_of(p->m, p->n, p->k), p->m, p->n) : 0;
     return HE_OK;
     });
 }
@@ -423,7 +455,7 @@ extern "C" int32_t he_matmul_q8(he_ctx* ctx, const he_matmul_plan* p) {
         return he_fail(ctx, HE_ERR_BADARG, "he_matmul_q8: the output overlaps an operand");
     GemmArgs a = {p->d_a, p->d_w, p->d_a_scales, p->d_w_scales, p->d_out, p->ld_a, p->ld_w, p->ld_a_scales, p->ld_w_scales, p->ld_out, p->m, p->n, p->k, kb, 0};
     const Cut c = cut_of(p->m, p->n, p->k);
-    const bool parts = p->m > 16 && c.parts > 1;
+    const bool few = few_rows(p->m, p->n, p->k), parts = !few && c.parts > 1;
     if (parts) {
         if ((rc = he_ensure_ws(ctx, cut_bytes(c, p->m, p->n))) != HE_OK) return rc;
         a.ld_out = (p->n + 3) & ~3u;
@@ -434,7 +466,7 @@ extern "C" int32_t he_matmul_q8(he_ctx* ctx, const he_matmul_plan* p) {
     hipError_t err = hipSuccess;
     with_dtype(p->out_dtype, [&](auto t) {
         using T = decltype(t);
-        if (p->m <= 16) err = launch_few<T>(a, ctx->stream);
+        if (few) err = run_few<T>(a, ctx->stream);
         else if (!parts) err = run_tiles<T>(a, c, p->fast_sums != 0, ctx->stream);
         else if ((err = run_tiles<f32_t>(a, c, p->fast_sums != 0, ctx->stream)) == hipSuccess) {
             for (uint32_t r = 0; r < p->m; r += 65535)   // a grid's second side
