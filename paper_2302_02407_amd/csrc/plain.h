@@ -150,20 +150,23 @@ __device__ __forceinline__ float unordered(int32_t k) { return __builtin_bit_cas
 
 // Maximum or minimum of integers over a wavefront, the same in all lanes: rotations within rows of 16 lanes, then the four rows in scalars.
 // (Of floats every step would cost two more instructions, which make a signalling NaN a quiet one.)
-template <int CTRL> __device__ __forceinline__ int32_t rotated(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
-__device__ __forceinline__ int32_t wave_max(int32_t v) {
-    v = max(v, rotated<0x128>(v));        // row_ror:8, 4, 2, 1
+template <int CTRL> __device__ __forceinline__ int32_t rotated(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }   // 0x120 + n: row_ror:n
+// Maximum, minimum over each row of 16 lanes
+__device__ __forceinline__ int32_t row_max(int32_t v) {
+    v = max(v, rotated<0x128>(v));
     v = max(v, rotated<0x124>(v));
     v = max(v, rotated<0x122>(v));
-    v = max(v, rotated<0x121>(v));
-    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+    return max(v, rotated<0x121>(v));
 }
-// Minimum over each row of 16 lanes
 __device__ __forceinline__ int32_t row_min(int32_t v) {
     v = min(v, rotated<0x128>(v));
     v = min(v, rotated<0x124>(v));
     v = min(v, rotated<0x122>(v));
     return min(v, rotated<0x121>(v));
+}
+__device__ __forceinline__ int32_t wave_max(int32_t v) {
+    v = row_max(v);
+    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
 // Calls f with the type of `dtype` (an he_dtype that has been checked)
