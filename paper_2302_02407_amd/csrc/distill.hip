@@ -107,10 +107,16 @@ template <class T, int WAVES> __device__ __forceinline__ void named_entries(cons
 }
 
 // One row a work group.  LOSS: writes the loss (and the statistics); GRAD: writes the gradient; REST: the rest counts as one outcome.
-// GRAD alone takes the sums from the statistics.  The row is read twice, 16 bytes a lane: once for the sums (against each lane's running
-// reference) and once for the gradient, the second time from the caches: what the rows of all work groups at work hold (at most 512 of
-// 256 KiB) stays in the last level's 256 MiB.
-template <class T, class R_, int THREADS, bool LOSS, bool GRAD, bool REST> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void distill_kernel(DistillArgs a) {
+// GRAD alone takes the sums from the statistics.  16 bytes a lane at a time, sums against each lane's running reference.  Loss and gradient
+// together need the row twice: V pieces a lane stay in registers between (16 of them: 64 of 128 registers; with 512 threads a work group 128
+// KiB, two work groups to a compute unit, one of which reads or writes while the other adds up), what is beyond is read again, backwards,
+// so that the caches still have some of it, and the gradient of long rows is written past them.
+//
+// 4096 x 131072 bf16, both: 467 us (4.6 TB/s of one read and one write).  With nothing kept 529 us, without its second pass going
+// backwards past the caches 483; all of the row kept, one work group of 1024 threads to a compute unit, 680: nothing runs beside its sums.
+// 4096 x 50021: 236 us, with nothing kept 283; 8192 x 10000, too short for it to matter: 92 us, with 16 pieces kept, fewer work
+// groups at a time, 138.
+template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST> __global__ __launch_bounds__(THREADS, THREADS == 1024 && V == 0 ? 8 : 4) void distill_kernel(DistillArgs a) {
     using raw = typename T::raw;
     constexpr int N = Vec<T>::N, WAVES = THREADS / 64;
     __shared__ RowShared<WAVES> s;
@@ -126,13 +132,48 @@ template <class T, class R_, int THREADS, bool LOSS, bool GRAD, bool REST> __glo
         if (LOSS && t == 0) a.loss[row] = 0;
         if (LOSS && a.stats && t < 4) a.stats[row * 4 + t] = 0;
         if (GRAD)
-            for (uint32_t p = 0; p < turns; p++) in.store(grad, p * THREADS + t, Vec<T>{{0, 0, 0, 0}});
+            for (uint32_t p = 0; p < turns; p++) in.store(grad, p * THREADS + t, Vec<T>{{0, 0, 0, 0}}, false);
         return;
     }
     const uint32_t words = (a.vocab + 31) / 32;
     const float c = HE_LOG2E / a.tau;
     const bool ce_on = a.alpha > 0.0f && a.labels && (uint32_t)label < a.vocab, two = ce_on && a.tau != 1.0f;
-    Vec<T> one = in.load(t), two_ = in.load(THREADS + t);
+    const uint32_t kept = min(turns, (uint32_t)V), read = turns - kept;
+    Vec<T> one, other, row_[V ? V : 1];
+    auto at = [&](uint32_t p, bool back) { return (kept + (back ? (p < read ? read - 1 - p : 0) : p)) * THREADS + t; };
+    auto begin = [&](bool back) {
+        one = in.load(at(0, back));
+        other = in.load(at(1, back));
+    };
+    // f(number, piece) for all of the row: what is kept and what is read, two buffers in turn, each refilled as soon as it is taken; or
+    // backwards
+    auto keep = [&](auto&& f, int p) {
+        if ((uint32_t)p >= turns) return;
+        f(p * THREADS + t, row_[p]);
+        // what comes of it now is not kept for the next time: two numbers of 16 bits take one register here, two there
+        asm volatile("" : "+v"(row_[p].w[0]), "+v"(row_[p].w[1]), "+v"(row_[p].w[2]), "+v"(row_[p].w[3]));
+    };
+    auto each = [&](auto&& f, bool back) {
+        if (!back)
+#pragma unroll
+            for (int p = 0; p < V; p++) keep(f, p);
+        for (uint32_t p = 0; p < read; p += 2) {
+            const Vec<T> x = one;
+            one = in.load(at(p + 2, back));
+            f(at(p, back), x);
+            if (p + 1 >= read) break;
+            const Vec<T> y = other;
+            other = in.load(at(p + 3, back));
+            f(at(p + 1, back), y);
+        }
+        if (back)
+#pragma unroll
+            for (int p = V - 1; p >= 0; p--) keep(f, p);
+    };
+#pragma unroll
+    for (int p = 0; p < V; p++)
+        if ((uint32_t)p < turns) row_[p] = in.load(p * THREADS + t);
+    begin(false);
     if (REST && LOSS) {
         for (uint32_t i = t; i < words; i += THREADS) named[i] = 0;
         __syncthreads();
@@ -148,12 +189,11 @@ template <class T, class R_, int THREADS, bool LOSS, bool GRAD, bool REST> __glo
     Sum S = {NOTHING, 0}, S1 = {NOTHING, 0};
     if (LOSS) {
         if (REST) __syncthreads();
-        auto turn = [&](uint32_t p, Vec<T>& buf) {
-            const uint32_t v = p * THREADS + t, base = in.base(v), past = v * N - base;
+        each([&](uint32_t v, const Vec<T>& piece) {
+            const uint32_t base = in.base(v), past = v * N - base;
             float x[N];
 #pragma unroll
-            for (int i = 0; i < N; i++) x[i] = buf[i];
-            buf = in.load(v + 2 * THREADS);
+            for (int i = 0; i < N; i++) x[i] = piece[i];
             uint32_t out = 0;
             if (REST) {
                 out = named[base >> 5] >> (base & 31);
@@ -179,15 +219,8 @@ template <class T, class R_, int THREADS, bool LOSS, bool GRAD, bool REST> __glo
 #pragma unroll
                 for (int i = 0; i < N; i++) S1.value += exp2_fast(fmaf(x[i], HE_LOG2E, -R1));
             }
-        };
-        for (uint32_t p = 0; p < turns; p += 2) {
-            turn(p, one);
-            if (p + 1 < turns) turn(p + 1, two_);
-        }
-        if (GRAD) {                                       // on their way while the sums are joined
-            one = in.load(t);
-            two_ = in.load(THREADS + t);
-        }
+        }, false);
+        if (GRAD) begin(true);                            // on their way while the sums are joined
         S = wave_total(S);
         if (two) S1 = wave_total(S1);
         if (lane == 0) {
@@ -288,10 +321,7 @@ template <class T, class R_, int THREADS, bool LOSS, bool GRAD, bool REST> __glo
     if (!GRAD) return;
     __syncthreads();
     const float R = s.factor[0], R1 = s.factor[1], fk = s.factor[2], fc = s.factor[3];
-    auto turn = [&](uint32_t p, Vec<T>& buf) {
-        const uint32_t v = p * THREADS + t;
-        const Vec<T> x = buf;
-        buf = in.load(v + 2 * THREADS);
+    each([&](uint32_t v, const Vec<T>& x) {
         float y[N];
 #pragma unroll
         for (int i = 0; i < N; i++) y[i] = fk * exp2_fast(fmaf(x[i], c, -R));
@@ -300,12 +330,8 @@ template <class T, class R_, int THREADS, bool LOSS, bool GRAD, bool REST> __glo
             for (int i = 0; i < N; i++) y[i] = fmaf(fc, exp2_fast(fmaf(x[i], HE_LOG2E, -R1)), y[i]);
         Vec<T> g;
         g.set(y);
-        in.store(grad, v, g);
-    };
-    for (uint32_t p = 0; p < turns; p += 2) {
-        turn(p, one);
-        if (p + 1 < turns) turn(p + 1, two_);
-    }
+        in.store(grad, v, g, THREADS > 256);
+    }, LOSS);
     __syncthreads();
     for (uint32_t i = t; i <= HE_TOP_MAX; i += THREADS)
         if (s.put_at[i] >= 0) grad[s.put_at[i]] = from_float<T>(s.put[i]);
@@ -356,15 +382,23 @@ template <bool LOSS, bool GRAD> static void launch(he_ctx* ctx, const he_distill
     const uint32_t lds = p->d_rest && LOSS ? (p->vocab + 31) / 32 * 4 : 0;
     with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        auto go = [&](auto threads, auto row) {
-            constexpr int THREADS = decltype(threads)::value;
+        auto go = [&](auto threads, auto pieces, auto row) {
+            constexpr int THREADS = decltype(threads)::value, V = decltype(pieces)::value;
             using R = typename decltype(row)::type;
-            if (p->d_rest) distill_kernel<T, R, THREADS, LOSS, GRAD, true><<<p->rows, THREADS, lds, ctx->stream>>>(a);
-            else distill_kernel<T, R, THREADS, LOSS, GRAD, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
+            if (p->d_rest) distill_kernel<T, R, THREADS, V, LOSS, GRAD, true><<<p->rows, THREADS, lds, ctx->stream>>>(a);
+            else distill_kernel<T, R, THREADS, V, LOSS, GRAD, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
         };
-        if (p->vocab < (uint32_t)Vec<T>::N) go(std::integral_constant<int, 64>{}, Of<ShortRow<T>>{});
-        else if ((uint64_t)p->vocab * dtype_bytes(p->dtype) > 32768) go(std::integral_constant<int, 1024>{}, Of<Row<T>>{});
-        else go(std::integral_constant<int, 256>{}, Of<Row<T>>{});
+        using std::integral_constant;
+        const uint64_t bytes = (uint64_t)p->vocab * dtype_bytes(p->dtype);
+        if (p->vocab < (uint32_t)Vec<T>::N) go(integral_constant<int, 64>{}, integral_constant<int, 0>{}, Of<ShortRow<T>>{});
+        else if constexpr (LOSS && GRAD) {
+            if (bytes <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 1>{}, Of<Row<T>>{});
+            else if (bytes <= 16384) go(integral_constant<int, 256>{}, integral_constant<int, 4>{}, Of<Row<T>>{});
+            else if (bytes <= 32768) go(integral_constant<int, 256>{}, integral_constant<int, 0>{}, Of<Row<T>>{});
+            else if (bytes <= 65536) go(integral_constant<int, 256>{}, integral_constant<int, 16>{}, Of<Row<T>>{});
+            else go(integral_constant<int, 512>{}, integral_constant<int, 16>{}, Of<Row<T>>{});
+        } else if (bytes > 32768) go(integral_constant<int, 1024>{}, integral_constant<int, 0>{}, Of<Row<T>>{});
+        else go(integral_constant<int, 256>{}, integral_constant<int, 0>{}, Of<Row<T>>{});
     });
 }
 

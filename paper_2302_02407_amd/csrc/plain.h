@@ -32,10 +32,35 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
+// Reductions over a wavefront, the same in all lanes: rotations within rows of 16 lanes, then the four rows' results as scalars.  (The
+// maximum of integers takes an instruction a step; of floats two more make a signalling NaN a quiet one.)
+template <int CTRL> __device__ __forceinline__ int32_t rotated(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }   // 0x120 + n: row_ror:n
+// Maximum, minimum over each row of 16 lanes
+__device__ __forceinline__ int32_t row_max(int32_t v) {
+    v = max(v, rotated<0x128>(v));
+    v = max(v, rotated<0x124>(v));
+    v = max(v, rotated<0x122>(v));
+    return max(v, rotated<0x121>(v));
+}
+__device__ __forceinline__ int32_t row_min(int32_t v) {
+    v = min(v, rotated<0x128>(v));
+    v = min(v, rotated<0x124>(v));
+    v = min(v, rotated<0x122>(v));
+    return min(v, rotated<0x121>(v));
+}
+__device__ __forceinline__ int32_t wave_max(int32_t v) {
+    v = row_max(v);
+    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
 template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = f(v, __shfl_xor(v, o));
-    return v;
+    const auto bits = [](float x) { return __builtin_bit_cast(int32_t, x); };
+    const auto number = [](int32_t x) { return __builtin_bit_cast(float, x); };
+    v = f(v, number(rotated<0x128>(bits(v))));
+    v = f(v, number(rotated<0x124>(bits(v))));
+    v = f(v, number(rotated<0x122>(bits(v))));
+    v = f(v, number(rotated<0x121>(bits(v))));
+    const auto row = [&](int lane) { return number(__builtin_amdgcn_readlane(bits(v), lane)); };
+    return f(f(row(0), row(16)), f(row(32), row(48)));
 }
 __device__ __forceinline__ float wave_sum(float v) { return wave_reduce(v, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float wave_max(float v) { return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
@@ -63,6 +88,11 @@ template <class T> struct Vec {
     uint32_t w[4];
     __device__ __forceinline__ void load(const raw* p) { __builtin_memcpy(w, p, 16); }
     __device__ __forceinline__ void store(raw* p) const { __builtin_memcpy(p, w, 16); }
+    // What is not read again soon: it leaves the cache to what is
+    __device__ __forceinline__ void store_past(raw* p) const {
+        typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+        __builtin_nontemporal_store(u4{w[0], w[1], w[2], w[3]}, (u4*)p);
+    }
     __device__ __forceinline__ float operator[](int i) const {
         if constexpr (N == 4) return __builtin_bit_cast(float, w[i]);
         else if constexpr (__is_same(T, bf16_t)) return __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
@@ -109,10 +139,12 @@ template <class T> struct Row {
         return x;
     }
     // Piece v of a row that is written: all of it, or of a last one what is its own
-    __device__ __forceinline__ void store(raw* to, uint32_t v, const Vec<T>& x) const {
+    __device__ __forceinline__ void store(raw* to, uint32_t v, const Vec<T>& x, bool past_cache) const {
         const uint32_t at = base(v), past = v * N - at;
-        if (past == 0) x.store(to + at);
-        else
+        if (past == 0) {
+            if (past_cache) x.store_past(to + at);
+            else x.store(to + at);
+        } else
 #pragma unroll
             for (uint32_t i = 0; i < N; i++)
                 if (i >= past) to[at + i] = from_float<T>(x[i]);
@@ -134,7 +166,7 @@ template <class T> struct ShortRow {
         v.set(x);
         return v;
     }
-    __device__ __forceinline__ void store(raw* to, uint32_t v, const Vec<T>& x) const {
+    __device__ __forceinline__ void store(raw* to, uint32_t v, const Vec<T>& x, bool) const {
 #pragma unroll
         for (uint32_t i = 0; i < N; i++)
             if (v == 0 && i < n) to[i] = from_float<T>(x[i]);
@@ -147,27 +179,6 @@ __device__ __forceinline__ int32_t ordered(float v) {
     return b ^ (b >> 31 & 0x7fffffff);
 }
 __device__ __forceinline__ float unordered(int32_t k) { return __builtin_bit_cast(float, k ^ (k >> 31 & 0x7fffffff)); }
-
-// Maximum or minimum of integers over a wavefront, the same in all lanes: rotations within rows of 16 lanes, then the four rows in scalars.
-// (Of floats every step would cost two more instructions, which make a signalling NaN a quiet one.)
-template <int CTRL> __device__ __forceinline__ int32_t rotated(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }   // 0x120 + n: row_ror:n
-// Maximum, minimum over each row of 16 lanes
-__device__ __forceinline__ int32_t row_max(int32_t v) {
-    v = max(v, rotated<0x128>(v));
-    v = max(v, rotated<0x124>(v));
-    v = max(v, rotated<0x122>(v));
-    return max(v, rotated<0x121>(v));
-}
-__device__ __forceinline__ int32_t row_min(int32_t v) {
-    v = min(v, rotated<0x128>(v));
-    v = min(v, rotated<0x124>(v));
-    v = min(v, rotated<0x122>(v));
-    return min(v, rotated<0x121>(v));
-}
-__device__ __forceinline__ int32_t wave_max(int32_t v) {
-    v = row_max(v);
-    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
-}
 
 // Calls f with the type of `dtype` (an he_dtype that has been checked)
 template <class F> static inline void with_dtype(int32_t dtype, F&& f) {
