@@ -3,6 +3,7 @@
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v4i_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
@@ -334,7 +335,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
     raw* const results = (raw*)a.out + blockIdx.y * a.part;
     uint8_t* mine = lds + wave * 32 * PITCH;
     const uint32_t nw = n0 + wn * TN * 32;
-    const bool whole = !(((uintptr_t)results | a.ld_out * ES) & 15) && nw + TN * 32 <= a.n;
+    const bool whole = nw + TN * 32 <= a.n;              // rows start anywhere: 16 bytes at a time all the same
 #pragma unroll
     for (int j = 0; j < TM; j++) {
         __syncthreads();
@@ -353,7 +354,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
 #pragma unroll
             for (int r = 0; r < 32; r += 64 / LANES) {
                 const uint32_t row = r + lane / LANES, at = lane % LANES * 16;
-                if (mw + row < a.m) *(v4i*)((uint8_t*)results + ((mw + row) * a.ld_out + nw) * ES + at) = *(const v4i*)(mine + row * PITCH + at);
+                if (mw + row < a.m) *(v4i_any*)((uint8_t*)results + ((mw + row) * a.ld_out + nw) * ES + at) = *(const v4i*)(mine + row * PITCH + at);
             }
         } else {
             for (uint32_t r = 0; r < 32 && mw + r < a.m; r++)
