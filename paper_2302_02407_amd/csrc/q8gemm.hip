@@ -183,6 +183,7 @@ template <class T> static hipError_t run_few(const GemmArgs& a, hipStream_t stre
 // run at a time (a pair of the first and 16 of the second take 172 cycles, not 130, with two wavefronts to a unit).
 typedef const __attribute__((address_space(1))) void* gptr;
 typedef __attribute__((address_space(3))) void* lptr;
+typedef const __attribute__((address_space(4))) float* cptr;    // read by scalar loads
 
 template <int WN, int WM, int TN, int TM> struct Tile {
     static constexpr int BN = WN * TN * 32, BM = WM * TM * 32, THREADS = WN * WM * 64;
@@ -240,7 +241,8 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
             __builtin_amdgcn_global_load_lds((gptr)((f < FW ? w0 : a0) + (off[f] + in)), (lptr)(to + f * WAVES * 1024), 16, 0, 0);
     };
     float* scales = (float*)(lds + 2 * G::BYTES);
-    const float* sw = a.sw + min(n0 + wn * TN * 32, a.n - 1) / 128 * a.ld_sw + first;
+    const cptr sw = (cptr)(uintptr_t)(a.sw + min(n0 + wn * TN * 32, a.n - 1) / 128 * a.ld_sw + first);
+    float swb = sw[0];
     v16f acc[TN][TM];
 #pragma unroll
     for (int i = 0; i < TN; i++)
@@ -258,7 +260,6 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
                 to[i % 8 * G::BM + r] = c < blocks ? a.sa[min(m0 + r, a.m - 1) * a.ld_sa + first + c] : 0.0f;
             }
         }
-        const float swb = sw[b];
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (!FAST && b + 1 < blocks) fill(b + 1, 0, FILLS);
@@ -275,6 +276,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
         float s[TM];
 #pragma unroll
         for (int j = 0; j < TM; j++) s[j] = scales[((b >> 3 & 1) * 8 + (b & 7)) * G::BM + (wm * TM + j) * 32 + l] * swb;
+        if (b + 1 < blocks) swb = sw[b + 1];
         const uint8_t *wb = buf + (wn * TN * 32 + l) * 128, *ab = buf + (G::BN + wm * TM * 32 + l) * 128;
         if (FAST) {
             v8i af[TM][2];
