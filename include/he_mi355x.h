@@ -418,7 +418,9 @@ int32_t he_ws_query_matmul_q8(const he_ctx* ctx, const he_matmul_plan* plan, uin
 
 /* The k largest logits of every row in descending order, the lowest index first among equals (a NaN counts as larger than any
  * number, -0 equals +0), and d_rest[row] = log of the sum over the row's OTHER logits z of exp(z / tau): -infinity where nothing
- * but -infinity is left.  d_values, d_index: [rows][k], dense; d_rest may be NULL. */
+ * but -infinity is left.  In that sum, and in those of the distillation below, a logit z with z <= -2^126 min(1, tau), such as the
+ * lowest number of f32 or bf16 in a masked place, counts as -infinity; the order takes it as it is.  From 2^126 min(1, tau) up a
+ * logit counts as +infinity in d_rest.  d_values, d_index: [rows][k], dense; d_rest may be NULL. */
 #define HE_TOP_MAX 128
 typedef struct {
     uint32_t rows, vocab, k;       /* 1 <= k <= min(vocab, HE_TOP_MAX), vocab <= 2^20 */

@@ -136,7 +136,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
         return;
     }
     const uint32_t words = (a.vocab + 31) / 32;
-    const float c = HE_LOG2E / a.tau;
+    const float c = HE_LOG2E / a.tau, low = masked_from(a.tau);
     const bool ce_on = a.alpha > 0.0f && a.labels && (uint32_t)label < a.vocab, two = ce_on && a.tau != 1.0f;
     const uint32_t kept = min(turns, (uint32_t)V), read = turns - kept;
     Vec<T> one, other, row_[V ? V : 1];
@@ -208,7 +208,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
             float most = x[0];
 #pragma unroll
             for (int i = 1; i < N; i++) most = fmaxf(most, x[i]);
-            if (!(most > HE_MASKED)) most = -INFINITY;
+            if (!(most > low)) most = -INFINITY;
             raise(S, most * c);
             const float R = ref_or_0(S.ref);
 #pragma unroll
@@ -254,7 +254,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
         const float rest = s.teacher[0], all_log = s.teacher[1], rest_log = s.teacher[2], teacher_most = s.teacher[3], zl = ce_on ? s.label_z : 0.0f;
         // all: against the larger of the reference and the named logits' largest
         const float c1 = two ? HE_LOG2E : c, zt = fmaxf(REST && e.first[0] ? e.z[0] : -INFINITY, REST && e.first[1] ? e.z[1] : -INFINITY), zm = wave_max(zt);
-        const float M = !(zm > HE_MASKED) ? S.ref : fmaxf(S.ref, zm * c), M1 = !(zm > HE_MASKED) ? S1.ref : fmaxf(S1.ref, zm * c1);
+        const float M = !(zm > low) ? S.ref : fmaxf(S.ref, zm * c), M1 = !(zm > low) ? S1.ref : fmaxf(S1.ref, zm * c1);
         const float R = ref_or_0(M), R1 = ref_or_0(M1);
         float x[2], x1[2];
 #pragma unroll

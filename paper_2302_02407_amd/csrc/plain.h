@@ -9,7 +9,10 @@
 
 #define HE_LOG2E 1.44269504088896340736f
 #define HE_LN2 0.69314718055994530942f
-#define HE_MASKED -0x1p126f      // a logit from here down counts as -infinity in a sum (the lowest number of a type, times log2(e), is none)
+// A logit z with z or z / tau at -2^126 or below, such as the lowest number of its type in a masked place, counts as -infinity in a sum of
+// exponentials: from there on log2(e) / tau times z need not be a number any more.
+#define HE_MASKED -0x1p126f
+__device__ __forceinline__ float masked_from(float tau) { return HE_MASKED * fminf(1.0f, tau); }
 
 struct f32_t { using raw = uint32_t; };
 struct bf16_t { using raw = uint16_t; };

@@ -66,12 +66,13 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
     }
     if (t == 0) s.got = 0;
     __syncthreads();
+    const float low = masked_from(a.tau);
     float most = -INFINITY;
     for (uint32_t i = t; i < a.vocab; i += THREADS) {
         const float v = to_float<T>(z[i]);
         const u64 c = place_of(v, i);
         if (c >= prefix) s.keep[atomicAdd(&s.got, 1u)] = c;     // exactly k
-        else most = fmaxf(most, v);
+        else if (!(v <= low)) most = fmaxf(most, v);
     }
     most = group_max<THREADS / 64>(most, s.room);
     __syncthreads();
@@ -88,10 +89,10 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
     float sum = 0;
     for (uint32_t i = t; i < a.vocab; i += THREADS) {
         const float v = to_float<T>(z[i]);
-        if (place_of(v, i) < prefix) sum += v == INFINITY ? INFINITY : exp2_fast((v - at) * scale);
+        if (place_of(v, i) < prefix && !(v <= low)) sum += v >= -low ? INFINITY : exp2_fast((v - at) * scale);
     }
     sum = group_sum<THREADS / 64>(sum, s.room);
-    if (t == 0) a.rest[row] = at == INFINITY ? sum : logf(sum) + at / a.tau;
+    if (t == 0) a.rest[row] = at >= -low ? sum : logf(sum) + at / a.tau;
 }
 
 // One row a work group, read once, 16 bytes a lane at a time.  Pieces of 16 bytes with an element that reaches a threshold are set aside in
@@ -113,9 +114,9 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     const Row<T> in{z, a.vocab};
     const uint32_t vecs = in.pieces(), turns = (vecs + THREADS - 1) / THREADS;
     const uint32_t full = min((uint32_t)WAVES, vecs / 64), r = full ? (a.k + full - 1) / full : 65;
-    const float c = HE_LOG2E / a.tau;
+    const float c = HE_LOG2E / a.tau, low = masked_from(a.tau);
     if (t == 0) s.got = s.kept = 0, s.more = 0;
-    float m = -3e38f, sum = 0, high = -INFINITY, least = -INFINITY;
+    float m = low, sum = 0, high = -INFINITY, least = -INFINITY;
     auto raise = [&](int32_t* tw) {
         int32_t w = ordered(high), best = INT32_MIN;
         if (r <= 64)
@@ -156,7 +157,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
                 sum *= exp2_fast((m - mx) * c);
                 m = mx;
             }
-            const float mc = m == -3e38f ? 0.0f : m * c;     // nothing but -infinity so far
+            const float mc = m == low ? 0.0f : m * c;      // nothing that counts so far
 #pragma unroll
             for (int i = 0; i < N; i++) sum += exp2_fast(fmaf(e[i], c, -mc));
         }
@@ -207,7 +208,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     u64 more = 0;
     auto add = [&](float v) {
         lost = lost || v != v;
-        if (v != -INFINITY && most != INFINITY) more += (u64)(exp2_fast((v - most) * c) * 0x1p44f);
+        if (!(v <= low) && most < -low) more += (u64)(exp2_fast((v - most) * c) * 0x1p44f);
     };
     for (uint32_t i = t; i < got * N; i += THREADS) {
         const float v = to_float<T>(((const raw*)s.aside)[i]);
@@ -217,9 +218,9 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     for (int q = 0; q < Q; q++)
         if (over[q]) add(value_of((uint32_t)(over[q] >> 32)));
     if (more) atomicAdd((unsigned long long*)&s.more, (unsigned long long)more);
-    sum = group_sum<WAVES>(most == INFINITY ? 0.0f : sum * exp2_fast((m - most) * c), s.room);
+    sum = group_sum<WAVES>(!(most < -low) ? 0.0f : sum * exp2_fast((m - most) * c), s.room);
     lost = __syncthreads_or(lost);
-    if (t == 0) a.rest[row] = lost ? NAN : most == INFINITY ? INFINITY : logf(sum + (float)s.more * 0x1p-44f) + most / a.tau;
+    if (t == 0) a.rest[row] = lost ? NAN : most >= -low ? INFINITY : logf(sum + (float)s.more * 0x1p-44f) + most / a.tau;
 }
 
 extern "C" int32_t he_top_logits(he_ctx* ctx, const he_top_plan* p) {

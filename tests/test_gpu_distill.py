@@ -262,3 +262,60 @@ def test_refusals(ctx):
     top(z[:0], 1.0, f(0, 5), i32(0, 5))                                   # no rows: fine
     loss(z[:0], v[:0], i[:0], None, 1.0, f(0))
     torch.cuda.synchronize()
+
+
+def with_masks(rows, vocab, low, seed):
+    """Rows with some logits, all but two, all, and none at the lowest value."""
+    z = 3 * torch.randn((rows, vocab), generator=rng(seed))
+    z[0::4][torch.rand((len(z[0::4]), vocab), generator=rng(seed + 1)) < 0.7] = low
+    z[1::4] = torch.where((torch.arange(vocab) == 1) | (torch.arange(vocab) == vocab - 1), z[1::4], low)
+    z[2::4] = low
+    return z
+
+
+LOWS = [(torch.float32, torch.finfo(torch.float32).min), (torch.float32, -1e38), (torch.bfloat16, torch.finfo(torch.bfloat16).min), (torch.bfloat16, -3.0e38)]
+
+
+@pytest.mark.parametrize("vocab", [3, 10, 700, 9001, 40000])
+@pytest.mark.parametrize("tau", [0.25, 1.0, 3.0])
+@pytest.mark.parametrize("dtype,low", LOWS)
+def test_top_of_rows_masked_by_the_lowest_value(ctx, vocab, tau, dtype, low):
+    z = with_masks(8, vocab, low, vocab).to(dtype)
+    k = min(5, vocab)
+    got, (values, index, _) = run_top(ctx, z, k, tau), R.top(z, k, tau)
+    check_top(got, (values, index, R.top(torch.where(z.double() <= -1e37, -math.inf, z.double()), k, tau)[2]))
+    assert (got[2][2::4] == -math.inf).all()
+
+
+@pytest.mark.parametrize("tau", [0.5, 1.0])
+def test_top_of_numbers_that_overflow_a_sum(ctx, tau):
+    z = torch.randn((3, 5000), generator=rng(0))
+    z[0, 17], z[0, 4000] = 3.3e38, 3.2e38
+    z[1, 9], z[1, 11] = 3.3e38, -3.3e38
+    got, want = run_top(ctx, z, 1, tau), R.top(z, 1, tau)
+    assert torch.equal(got[1], want[1]) and got[2][0] == math.inf
+    check_top([g[1:] for g in got], [w[1:] for w in want])
+
+
+@pytest.mark.parametrize("vocab", [3, 10, 700, 9001, 40000])
+@pytest.mark.parametrize("tau", [0.25, 1.0, 3.0])
+@pytest.mark.parametrize("with_rest", [False, True])
+@pytest.mark.parametrize("dtype,low", LOWS)
+@pytest.mark.parametrize("mode", ["step", "later"])
+def test_distillation_of_rows_masked_by_the_lowest_value(ctx, vocab, tau, with_rest, dtype, low, mode):
+    """As if the masked logits were -infinity.  The teacher's indices and the label are among those that are not masked; what it names of a row that is
+    masked throughout does not matter."""
+    rows, k = 8, min(4, vocab)
+    z = with_masks(rows, vocab, low, vocab + 1).to(dtype)
+    as_meant = torch.where(z.double() <= -1e37, -math.inf, z.double())
+    order = as_meant.argsort(dim=1, descending=True, stable=True)
+    index = torch.where(as_meant.gather(1, order[:, :k]) > -math.inf, order[:, :k], -1).to(torch.int32)
+    values = 2 * torch.randn((rows, k), generator=rng(1))
+    rest = torch.randn(rows, generator=rng(2)) if with_rest else None
+    if with_rest:                                             # where nothing else is left, the teacher has nothing else either
+        rest = torch.where((as_meant > -math.inf).sum(dim=1) > (index >= 0).sum(dim=1), rest, -math.inf)
+    labels, weights = order[:, 0].to(torch.int32), torch.rand(rows, generator=rng(3)) + 0.5
+    want = R.distill(as_meant, values, index, rest, tau, labels, 0.25)
+    got = run_loss(ctx, z, (values, index, rest), tau, labels, 0.25, weights, mode, vocab + 1, 1)
+    check_loss(got, want, dtype, tau, 0.25, weights)
+    assert (got[0][2::4] == 0).all() and (got[1][2::4] == 0).all()
