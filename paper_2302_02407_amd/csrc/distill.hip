@@ -332,6 +332,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
         g.set(y);
         in.store(grad, v, g, THREADS > 256);
     }, LOSS);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // every wavefront's pieces are in memory before single elements of them are written anew
     __syncthreads();
     for (uint32_t i = t; i <= HE_TOP_MAX; i += THREADS)
         if (s.put_at[i] >= 0) grad[s.put_at[i]] = from_float<T>(s.put[i]);
