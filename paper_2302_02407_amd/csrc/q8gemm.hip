@@ -178,10 +178,12 @@ template <class T> static hipError_t run_few(const GemmArgs& a, hipStream_t stre
 // sixteen of them, two rows of 128 bytes to a line of all 64 banks, cover every bank once.  The fills are spread over the first half of a
 // block's squares: all at once they wait for the cache's 64 bytes a cycle and hold the wavefront's matrix instructions back.
 //
-// 8192 x 32768 x 4096 to bf16 1.08 ms (2030 TFLOP/s), exact sums to f32 2.15 ms (1020).  With no fills at all (on what lies there)
+// 8192 x 32768 x 4096 to bf16 1.07 ms (2060 TFLOP/s), exact sums to f32 2.12 ms (1040).  With no fills at all (on what lies there)
 // the first takes 0.91 ms; the matrix instructions alone are 45% of its cycles, the multiply-adds 30%, and of the two kinds about half can
-// run at a time (a pair of the first and 16 of the second take 172 cycles, not 130, with two wavefronts to a unit).
-typedef const __attribute__((address_space(1))) void* gptr;
+// run at a time (a pair of the first and 16 of the second take 172 cycles, not 130, with two wavefronts to a unit).  So a square's
+// multiply-adds stand between the next one's two instructions: with them behind its own, 1.09 ms, and 777 x 10007 x 2040 38.5 us, not
+// 35.9.  A third buffer does not fit beside the tile; asking for lines two or three blocks early, so that fills find them in the
+// die's cache, takes 1.11 ms.
 typedef __attribute__((address_space(3))) void* lptr;
 typedef const __attribute__((address_space(4))) float* cptr;    // read by scalar loads
 
@@ -211,6 +213,13 @@ __device__ __forceinline__ bool tile_of(uint32_t tiles_n, uint32_t tiles_m, uint
     return true;
 }
 
+// A tile's rows from one column on, for loads that check their bounds: what lies past the last row, or past the last row's k columns (to a
+// multiple of 16), comes as zeros.  So no lane holds an offset for every row it loads, and there is room for the results of two squares.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const uint8_t* p, uint32_t rows, uint32_t ld, uint32_t k) {
+    constexpr int RAW_DWORDS = 0x00027000;               // word 3 of a descriptor without a stride: offsets are compared with the size in bytes
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (min(rows, 256u) - 1) * ld + (k + 15) / 16 * 16, RAW_DWORDS);    // ld <= 2^23: below 2^32
+}
+
 template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launch_bounds__(WN* WM * 64, 2) void matmul_q8_tiles_kernel(GemmArgs a) {
     using raw = typename T::raw;
     using G = Tile<WN, WM, TN, TM>;
@@ -225,20 +234,17 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
 
     // a wavefront fills eight rows at a time: lane i the piece i % 8 of row i / 8
     constexpr int WAVES = WN * WM, FW = G::BN / 8 / WAVES, FA = G::BM / 8 / WAVES, FILLS = FW + FA;
-    const uint8_t *w0 = a.w + n0 * a.ld_w + first * 128, *a0 = a.a + m0 * a.ld_a + first * 128;
-    const uint32_t piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
-    uint32_t off[FILLS];                               // ld <= 2^23: 256 rows stay below 2^31
-#pragma unroll
-    for (int f = 0; f < FILLS; f++) {
-        const uint32_t r = ((f < FW ? f : f - FW) * WAVES + wave) * 8 + (lane >> 3);
-        off[f] = f < FW ? min(r, a.n - 1 - n0) * (uint32_t)a.ld_w : min(r, a.m - 1 - m0) * (uint32_t)a.ld_a;
-    }
-    auto fill = [&](uint32_t b, int from, int end) {
-        const uint32_t at = b * 128 + piece * 16, in = at < k ? at : 0;          // past the end: anything that is there, cleared below
+    const auto w_rows = rows_from(a.w + n0 * a.ld_w + first * 128, a.n - n0, (uint32_t)a.ld_w, k);
+    const auto a_rows = rows_from(a.a + m0 * a.ld_a + first * 128, a.m - m0, (uint32_t)a.ld_a, k);
+    const uint32_t r0 = wave * 8 + (lane >> 3), piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+    const uint32_t w_at = r0 * (uint32_t)a.ld_w + piece * 16, w_step = WAVES * 8 * (uint32_t)a.ld_w;
+    const uint32_t a_at = r0 * (uint32_t)a.ld_a + piece * 16, a_step = WAVES * 8 * (uint32_t)a.ld_a;
+    auto fill = [&](uint32_t b, int from, int end) {     // pieces past the k columns: anything that is there, cleared below
         uint8_t* to = lds + (b & 1) * G::BYTES + wave * 1024;
 #pragma unroll
         for (int f = from; f < end; f++)
-            __builtin_amdgcn_global_load_lds((gptr)((f < FW ? w0 : a0) + (off[f] + in)), (lptr)(to + f * WAVES * 1024), 16, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(f < FW ? w_rows : a_rows, (lptr)(to + f * WAVES * 1024), 16,
+                                                     f < FW ? w_at + (f * w_step + b * 128) : a_at + ((f - FW) * a_step + b * 128), 0, 0, 0);
     };
     float* scales = (float*)(lds + 2 * G::BYTES);
     const cptr sw = (cptr)(uintptr_t)(a.sw + min(n0 + wn * TN * 32, a.n - 1) / 128 * a.ld_sw + first);
@@ -284,21 +290,25 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
             for (int j = 0; j < TM; j++)
 #pragma unroll
                 for (int h = 0; h < 2; h++) af[j][h] = fragment(ab + j * 4096, 4 * h + 2 * g, l);
+            v16f p[2];                                   // of square q, and of the one before, which joins the sums meanwhile
+            v8i wf[2];
 #pragma unroll
-            for (int i = 0; i < TN; i++) {
-                v8i wf[2];
+            for (int q = 0; q <= TN * TM; q++) {
+                const int i = q / TM, j = q % TM;
+                if (q < TN * TM && j == 0)
 #pragma unroll
-                for (int h = 0; h < 2; h++) wf[h] = fragment(wb + i * 4096, 4 * h + 2 * g, l);
+                    for (int h = 0; h < 2; h++) wf[h] = fragment(wb + i * 4096, 4 * h + 2 * g, l);
+                constexpr int HALF = (TN * TM + 1) / 2;
+                if (q < HALF && b + 1 < blocks) fill(b + 1, q * FILLS / HALF, (q + 1) * FILLS / HALF);
+                if (q < TN * TM) p[q & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[0], af[j][0], zero16(), 0, 0, 0, 0, 0, 0);
+                if (q)
 #pragma unroll
-                for (int j = 0; j < TM; j++) {
-                    constexpr int HALF = (TN * TM + 1) / 2;
-                    if (i * TM + j < HALF && b + 1 < blocks) fill(b + 1, (i * TM + j) * FILLS / HALF, (i * TM + j + 1) * FILLS / HALF);
-                    v16f p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[0], af[j][0], zero16(), 0, 0, 0, 0, 0, 0);
-                    p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[1], af[j][1], p, 0, 0, 0, 0, 0, 0);
+                    for (int e = 0; e < 8; e++) acc[(q - 1) / TM][(q - 1) % TM][e] += p[~q & 1][e] * s[(q - 1) % TM];
+                if (q < TN * TM) p[q & 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[1], af[j][1], p[q & 1], 0, 0, 0, 0, 0, 0);
+                if (q)
 #pragma unroll
-                    for (int e = 0; e < 16; e++) acc[i][j][e] += p[e] * s[j];
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                    for (int e = 8; e < 16; e++) acc[(q - 1) / TM][(q - 1) % TM][e] += p[~q & 1][e] * s[(q - 1) % TM];
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
             v8h af[TM][8];                               // piece 2c + g of a row: 32 columns at a time

@@ -226,3 +226,42 @@ def test_head_on_a_stream_of_its_own(ctx):
         c.he_sync()
         outs.append(out)
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("m,n,k", [(3590, 4090, 130), (300, 30000, 64), (20000, 700, 16)])
+@pytest.mark.parametrize("dtype,fast", [(torch.bfloat16, True), (torch.float16, True), (torch.float32, False)])
+def test_product_of_many_tiles(ctx, dtype, fast, m, n, k):
+    """Enough rows on both sides for the largest tiles.  Codes that are whole numbers up to 8: a block's sum is exact either way (a fast sum
+    drops of a product what is 2^-13 of its group's largest, at most 64)."""
+    g = rng(n)
+    a, w = [torch.randint(-8, 9, (r, k), generator=g).float().to(R.F8) for r in (m, n)]
+    kb = -(-k // 128)
+    sa, sw = torch.rand((m, kb), generator=g) + 0.01, torch.rand((-(-n // 128), kb), generator=g) + 0.01
+    out = R.matrix(m, n, dtype, n + 3, 1)
+    ctx.he_matmul_q8(R.code_rows(a), sa.cuda(), R.code_rows(w), sw.cuda(), out, fast_sums=fast)
+    x, y = a.float(), w.float()
+    want, size = torch.zeros((m, n), dtype=torch.float32), torch.zeros((m, n), dtype=torch.float32)
+    for b in range(kb):                                      # a block's sum is a whole number: exact in 32 bits
+        at = slice(128 * b, 128 * b + 128)
+        part = (x[:, at] @ y[:, at].T) * sa[:, b:b + 1] * sw.repeat_interleave(128, dim=0)[:n, b]
+        want += part
+        size += part.abs()
+    off = (out.cpu().float() - want).abs()
+    assert (off <= size * ((kb + 4) * 2.0 ** -23) + want.abs() * R.ULP[dtype] * 1.01 + (2.0 ** -25 if dtype == torch.float16 else 0)).all()
+    assert int(torch.empty(0, dtype=dtype, device="cuda").set_(out.untyped_storage()).isnan().sum()) == out.untyped_storage().nbytes() // out.element_size() - m * n
+
+
+def test_product_in_parts_and_its_workspace(ctx):
+    """Few tiles and a long sum: parts of it in the workspace, no more of which is needed than was asked for."""
+    from he_inputs.params import config_params
+    from paper_2302_02407_amd.binding import HEContext
+    m, n, k = 200, 130, 8192
+    need = ctx.he_ws_query_matmul_q8(m, n, k)
+    assert need > 0 and ctx.he_ws_query_matmul_q8(1, n, k) == 0 and ctx.he_ws_query_matmul_q8(4096, 4096, 4096) == 0
+    a, sa, w, sw = operands(m, n, k, 1)
+    fresh = HEContext.from_params(config_params(0))
+    fresh.he_ws_reserve(need)
+    before = fresh.he_ws_bytes()
+    for dtype in TYPES:
+        check_product(fresh, a, sa, w, sw, dtype, 1, 1)
+    assert fresh.he_ws_bytes() == before
