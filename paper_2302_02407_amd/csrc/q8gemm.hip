@@ -182,8 +182,10 @@ template <class T> static hipError_t run_few(const GemmArgs& a, hipStream_t stre
 // the first takes 0.91 ms; the matrix instructions alone are 45% of its cycles, the multiply-adds 30%, and of the two kinds about half can
 // run at a time (a pair of the first and 16 of the second take 172 cycles, not 130, with two wavefronts to a unit).  So a square's
 // multiply-adds stand between the next one's two instructions: with them behind its own, 1.09 ms, and 777 x 10007 x 2040 38.5 us, not
-// 35.9.  A third buffer does not fit beside the tile; asking for lines two or three blocks early, so that fills find them in the
+// 35.9.  A third buffer does not fit beside the largest tile, and beside the smaller ones it takes the room of a second work group, which
+// covers more (777 x 10007 x 2040 44 us); asking for lines two or three blocks early, so that fills find them in the
 // die's cache, takes 1.11 ms.
+typedef const __attribute__((address_space(1))) void* gptr;
 typedef __attribute__((address_space(3))) void* lptr;
 typedef const __attribute__((address_space(4))) float* cptr;    // read by scalar loads
 
@@ -246,7 +248,16 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
             __builtin_amdgcn_raw_ptr_buffer_load_lds(f < FW ? w_rows : a_rows, (lptr)(to + f * WAVES * 1024), 16,
                                                      f < FW ? w_at + (f * w_step + b * 128) : a_at + ((f - FW) * a_step + b * 128), 0, 0, 0);
     };
-    float* scales = (float*)(lds + 2 * G::BYTES);
+    float* scales = (float*)(lds + 2 * G::BYTES);        // [2][BM rows][8 blocks]
+    // Of blocks b .. b + 7, b a multiple of 8; asked for 4 blocks early, as loads to registers they would be waited for (1024 x 4096 x 4096
+    // to bf16 31.4 us, 32.5 then; exact sums of large tiles 2.07 ms, 2.04 then).
+    auto fill_scales = [&](uint32_t b) {
+#pragma unroll
+        for (int i = 0; i < G::BM / 8 / WAVES; i++) {
+            const uint32_t at = i * WAVES + wave, r = at * 8 + (lane >> 3), c = min(b + (lane & 7), blocks - 1);
+            __builtin_amdgcn_global_load_lds((gptr)(a.sa + min(m0 + r, a.m - 1) * a.ld_sa + first + c), (lptr)(scales + (b >> 3 & 1) * 8 * G::BM + at * 64), 4, 0, 0);
+        }
+    };
     const cptr sw = (cptr)(uintptr_t)(a.sw + min(n0 + wn * TN * 32, a.n - 1) / 128 * a.ld_sw + first);
     float swb = sw[0];
     v16f acc[TN][TM];
@@ -257,17 +268,12 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0;
 
+    fill_scales(0);
     fill(0, 0, FILLS);
     for (uint32_t b = 0; b < blocks; b++) {
-        if ((b & 7) == 0) {                              // scales of the next eight blocks
-            float* to = scales + (b >> 3 & 1) * 8 * G::BM;
-            for (uint32_t i = tid; i < 8 * G::BM; i += G::THREADS) {
-                const uint32_t r = i / 8, c = b + i % 8;
-                to[i % 8 * G::BM + r] = c < blocks ? a.sa[min(m0 + r, a.m - 1) * a.ld_sa + first + c] : 0.0f;
-            }
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
+        if ((b & 7) == 4 && b + 4 < blocks) fill_scales(b + 4);
         if (!FAST && b + 1 < blocks) fill(b + 1, 0, FILLS);
         uint8_t* buf = lds + (b & 1) * G::BYTES;
         if (b + 1 == blocks && b * 128 + 128 > k) {            // columns past the end become zeros, in both operands
@@ -281,7 +287,7 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> __global__ __launc
         }
         float s[TM];
 #pragma unroll
-        for (int j = 0; j < TM; j++) s[j] = scales[((b >> 3 & 1) * 8 + (b & 7)) * G::BM + (wm * TM + j) * 32 + l] * swb;
+        for (int j = 0; j < TM; j++) s[j] = scales[(b >> 3 & 1) * 8 * G::BM + ((wm * TM + j) * 32 + l) * 8 + (b & 7)] * swb;
         if (b + 1 < blocks) swb = sw[b + 1];
         const uint8_t *wb = buf + (wn * TN * 32 + l) * 128, *ab = buf + (G::BN + wm * TM * 32 + l) * 128;
         if (FAST) {
