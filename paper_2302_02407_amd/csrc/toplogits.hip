@@ -25,7 +25,7 @@ __device__ __forceinline__ u64 place_of(float z, uint32_t i) { return (u64)order
 // An element's place in the order is one number of 64 bits, its key above the complement of its index, all different.
 
 template <int THREADS> struct TopShared {
-    static constexpr int ROOM = THREADS == 1024 ? 1024 : 512, KEEP = 512;
+    static constexpr int ROOM = THREADS == 1024 ? 1024 : THREADS == 64 ? 64 : 512, KEEP = 512;
     uint4 aside[ROOM];                         // 16 bytes of the row each, and which
     uint32_t which[ROOM];                      // index of the first of its elements, and above 24 bits how many are another's
     u64 keep[KEEP], more;
@@ -47,7 +47,7 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
     uint32_t want = a.k;                       // how many of the elements that agree with `prefix` are still wanted
     for (int shift = 56; shift >= 0; shift -= 8) {
         __syncthreads();
-        if (t < 256) s.bins[t] = 0;
+        for (uint32_t i = t; i < 256; i += THREADS) s.bins[i] = 0;
         __syncthreads();
         for (uint32_t i = t; i < a.vocab; i += THREADS) {
             const u64 c = place_of(to_float<T>(z[i]), i);
@@ -76,8 +76,8 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
     }
     most = group_max<THREADS / 64>(most, s.room);
     __syncthreads();
-    if (t < a.k) {
-        const u64 c = s.keep[t];
+    for (uint32_t i0 = t; i0 < a.k; i0 += THREADS) {
+        const u64 c = s.keep[i0];
         uint32_t place = 0;
         for (uint32_t j = 0; j < a.k; j++) place += s.keep[j] > c;
         const uint32_t i = ~(uint32_t)c;
@@ -103,6 +103,9 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
 // many come before it: the first k are the result, in order.  The others join the sum as whole multiples of 2^-44 of the rest's largest
 // term, in any order the same number.  An element of -infinity can only be among the first k if its index is below k: of the first k
 // elements at most as many are larger as there are larger ones at all.
+//
+// 2048 x 131072 bf16, k = 64: 144 us (3.7 TB/s), 90% of its cycles vector instructions: about 16 for an element, of which 8 are the sum's (one
+// exponential among them) and the rest maxima, thresholds and what is set aside.  As ten passes of a digit it took 3.1 ms.
 template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void top_logits_kernel(TopArgs a) {
     using raw = typename T::raw;
     constexpr int N = Vec<T>::N, WAVES = THREADS / 64, ROOM = TopShared<THREADS>::ROOM, KEEP = TopShared<THREADS>::KEEP;
@@ -113,7 +116,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     if (a.vocab < (uint32_t)N) return exact_row<T, THREADS>(a, s, row);
     const Row<T> in{z, a.vocab};
     const uint32_t vecs = in.pieces(), turns = (vecs + THREADS - 1) / THREADS;
-    const uint32_t full = min((uint32_t)WAVES, vecs / 64), r = full ? (a.k + full - 1) / full : 65;
+    const uint32_t full = max(1u, min((uint32_t)WAVES, vecs / 64)), r = (a.k + full - 1) / full;      // a lane without a piece counts as -infinity
     const float c = HE_LOG2E / a.tau, low = masked_from(a.tau);
     if (t == 0) s.got = s.kept = 0, s.more = 0;
     float m = low, sum = 0, high = -INFINITY, least = -INFINITY;
@@ -183,8 +186,8 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     __syncthreads();
     const uint32_t kept = s.kept;
     if (kept > KEEP) return exact_row<T, THREADS>(a, s, row);
-    u64 over[KEEP / 256];                                // what this thread looks after and is not among the first k, 0: nothing
     constexpr int Q = KEEP > THREADS ? KEEP / THREADS : 1;
+    u64 over[Q];                                         // what this thread looks after and is not among the first k, 0: nothing
 #pragma unroll
     for (int q = 0; q < Q; q++) {
         const uint32_t i = q * THREADS + t;
@@ -245,7 +248,11 @@ extern "C" int32_t he_top_logits(he_ctx* ctx, const he_top_plan* p) {
     const TopArgs a = {p->d_z, p->d_values, p->d_index, p->d_rest, p->ld_z, p->vocab, p->k, p->tau};
     with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        if ((uint64_t)p->vocab * es > 32768) top_logits_kernel<T, 1024><<<p->rows, 1024, 0, ctx->stream>>>(a);
+        // Rows of at most a piece a lane go to one wavefront (4000 x 500 bf16, k = 20: 15 us, by four 83; 3090 x 48: 6.7 and 14), unless most of a
+        // row's elements are candidates, which four put in order sooner (256 x 500, k = 100: 21 us, by one 62).
+        const uint64_t bytes = (uint64_t)p->vocab * es;
+        if (bytes > 32768) top_logits_kernel<T, 1024><<<p->rows, 1024, 0, ctx->stream>>>(a);
+        else if (bytes <= 1024 && (p->k <= 32 || p->vocab <= 128)) top_logits_kernel<T, 64><<<p->rows, 64, 0, ctx->stream>>>(a);
         else top_logits_kernel<T, 256><<<p->rows, 256, 0, ctx->stream>>>(a);
     });
     HE_LAUNCHED(ctx);
