@@ -319,3 +319,34 @@ def test_distillation_of_rows_masked_by_the_lowest_value(ctx, vocab, tau, with_r
     got = run_loss(ctx, z, (values, index, rest), tau, labels, 0.25, weights, mode, vocab + 1, 1)
     check_loss(got, want, dtype, tau, 0.25, weights)
     assert (got[0][2::4] == 0).all() and (got[1][2::4] == 0).all()
+
+
+@pytest.mark.parametrize("vocab,k", [(300, 7), (1000, 20), (1024, 100), (513, 1)])
+@pytest.mark.parametrize("mode", ["step", "later", "onto"])
+def test_loss_of_many_short_rows(ctx, vocab, k, mode):
+    """From 1024 rows on one wavefront takes a row of up to 4 KB."""
+    rows, tau, g = 1030, 2.0, rng(vocab)
+    dtype = torch.float32 if vocab != 513 else torch.bfloat16
+    z, t = (2 * torch.randn((rows, vocab), generator=g)).to(dtype), 2 * torch.randn((rows, vocab), generator=g)
+    values, index, rest = R.top(t, k, tau)
+    values, index, rest = values.float(), index.to(torch.int32), rest.float()
+    labels = torch.randint(-1, vocab + 1, (rows,), generator=g, dtype=torch.int32)
+    weights = torch.rand(rows, generator=g) + 0.5
+    want = R.distill(z, values, index, rest, tau, labels, 0.25)
+    check_loss(run_loss(ctx, z, (values, index, rest), tau, labels, 0.25, weights, mode, vocab + 3, 1), want, dtype, tau, 0.25, weights)
+
+
+@pytest.mark.parametrize("vocab,k", [(40, 40), (120, 120), (200, 32), (256, 33), (511, 1), (512, 32)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_top_of_short_rows(ctx, vocab, k, dtype):
+    """In order, all equal, with NaN, masked and in no order: rows that one wavefront takes, and such as it leaves to four."""
+    g = rng(vocab + k)
+    z = torch.randn((8, vocab), generator=g).to(dtype)
+    z[1] = z[1].sort().values
+    z[2] = z[2].sort(descending=True).values
+    z[3] = 0.5
+    z[4, ::3] = -math.inf
+    z[5] = -math.inf
+    z[6, vocab // 2], z[6, 1] = math.nan, math.inf
+    z[7, : vocab // 2] = z[7, 0]
+    check_top(run_top(ctx, z, k, 1.5, vocab + 1, 1), R.top(z, k, 1.5))
