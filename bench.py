@@ -16,6 +16,7 @@ real ones look like limb by limb), generated on the device, so the timed region 
 everything resident in HBM.
 """
 import argparse
+import gc
 import json
 import os
 import sys
@@ -204,11 +205,13 @@ def main():
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         fn()
         torch.cuda.synchronize()
+        gc.disable()                               # a full collection takes 37 ms, the calls below one or less
         e0.record()
         for _ in range(reps):
             fn()
         e1.record()
         torch.cuda.synchronize()
+        gc.enable()
         return e0.elapsed_time(e1) / reps
 
 
