@@ -185,6 +185,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
             for (int u = 0; u < 2; u++)
                 if (const int32_t at = s.at[lane + 64 * u]; at >= 0) atomicOr(&named[at >> 5], 1u << (at & 31));
         if (lane == 0 && ce_on) s.label_z = to_float<T>(z[label]);
+        wave_sync();                                      // where no sums are taken, no barrier lies between this and its other lanes' reading
     }
     Sum S = {NOTHING, 0}, S1 = {NOTHING, 0};
     if (LOSS) {
