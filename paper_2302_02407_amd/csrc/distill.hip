@@ -2,10 +2,11 @@
 //
 // Of a row's logits z the indices that the teacher names are few: they and the label are handled apart, and the pass over the row
 // sums the others.  The rest's probability then keeps its relative accuracy however small it is.  With c = log2(e) / tau all sums are of
-// 2^(c z - R) for a reference R that is a number of its own, near c times the largest z: the difference is one multiply-add with one
-// rounding, so nothing is lost where logits are large.  With S the sum over the indices that are not named, Z over all, and S1, Z1 the
-// same at temperature 1 (reference R1), the gradient at an index that is not named is
-//   2^(c z - R) * (1 - alpha) tau (1/Z - P_rest/S) + 2^(log2(e) z - R1) * alpha/Z1,
+// 2^(c (z - R)) for a reference R that is one of the row's logits, the largest: the difference comes first, so that its rounding is one of
+// the difference, and the largest term is 1, whatever size the logits are.  (c z - R with R near c times the largest, one multiply-add, leaves
+// the rounding of R in the exponent: past 2^7 from logits of 2^32 on, where the sum is 0 or infinite.)  With S the sum over the indices that
+// are not named, Z over all, and S1, Z1 the same at temperature 1, the gradient at an index that is not named is
+//   2^(c (z - R)) * (1 - alpha) tau (1/Z - P_rest/S) + 2^(log2(e) (z - R)) * alpha/Z1,
 // two factors a row.  Where no rest is given (P_rest = 0) nothing has to be told apart and the pass sums over all.
 #include "plain.h"
 
@@ -20,31 +21,32 @@ struct DistillArgs {
     float tau, alpha;
 };
 
-// A sum of powers of two against its reference: value * 2^ref
-struct Sum {
-    float ref, value;
+// Sums of a row's exponentials against a logit: value * 2^(c ref), and at temperature 1.  Without a term: ref = masked_from(tau), below
+// any logit that counts.
+struct Sums {
+    float ref, value, value1;
 };
-#define NOTHING -3e38f     // the reference of a sum without a term
-__device__ __forceinline__ float ref_or_0(float r) { return r == NOTHING ? 0.0f : r; }
-__device__ __forceinline__ void raise(Sum& s, float ref) {
+struct Scale {
+    float c, low;
+    bool two;                       // there is a sum at temperature 1, and it is another
+    __device__ __forceinline__ float number(float ref) const { return ref == low ? 0.0f : ref; }    // masked logits have no power against 0
+    __device__ __forceinline__ float power(float d) const { return exp2_fast(d * c); }
+    __device__ __forceinline__ float power1(float d) const { return exp2_fast(d * HE_LOG2E); }
+};
+__device__ __forceinline__ void raise(Sums& s, float ref, const Scale& scale) {
     if (ref > s.ref) {
-        s.value *= exp2_fast(s.ref - ref);
+        s.value *= scale.power(s.ref - ref);
+        if (scale.two) s.value1 *= scale.power1(s.ref - ref);
         s.ref = ref;
     }
 }
-// Over a wavefront, then over the work group (room: 2 floats a wavefront; a barrier before it is used again is the caller's)
-__device__ __forceinline__ Sum wave_total(Sum s) {
+// Over a wavefront, then over the work group (a barrier before `w` is used again is the caller's)
+__device__ __forceinline__ Sums wave_total(Sums s, const Scale& scale) {
     const float r = wave_max(s.ref);
-    return {r, wave_sum(s.value == 0.0f ? 0.0f : s.value * exp2_fast(s.ref - r))};
+    return {r, wave_sum(s.value * scale.power(s.ref - r)), scale.two ? wave_sum(s.value1 * scale.power1(s.ref - r)) : 0.0f};
 }
-template <int WAVES> __device__ __forceinline__ Sum total_of(const Sum* w) {
-    Sum s = w[0];
-#pragma unroll
-    for (int i = 1; i < WAVES; i++) s.ref = fmaxf(s.ref, w[i].ref);
-    s.value = 0;
-#pragma unroll
-    for (int i = 0; i < WAVES; i++) s.value += w[i].value == 0.0f ? 0.0f : w[i].value * exp2_fast(w[i].ref - s.ref);
-    return s;
+template <int WAVES> __device__ __forceinline__ Sums total_of(const Sums* w, const Scale& scale, uint32_t lane) {
+    return wave_total(lane < WAVES ? w[lane] : Sums{scale.low, 0, 0}, scale);
 }
 
 // What a row's threads share
@@ -58,8 +60,8 @@ template <int WAVES> struct RowShared {
     float teacher[5];               // P_rest, log of the sum over all (against the largest), log P_rest, the largest, whether anything is there
     int32_t put_at[HE_TOP_MAX + 1]; // where the gradient is written last, -1: nowhere; the label at the end
     float put[HE_TOP_MAX + 1];
-    Sum part[2][WAVES];
-    float factor[4];                // R, R1, and the factors of the two powers
+    Sums part[WAVES];
+    float factor[3];                // R and the factors of the two powers
 };
 
 // The teacher's entries of a row and what goes with them, by one wavefront, entry lane + 64 u; in LDS until the sums are there
@@ -136,8 +138,8 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
         return;
     }
     const uint32_t words = (a.vocab + 31) / 32;
-    const float c = HE_LOG2E / a.tau, low = masked_from(a.tau);
-    const bool ce_on = a.alpha > 0.0f && a.labels && (uint32_t)label < a.vocab, two = ce_on && a.tau != 1.0f;
+    const bool ce_on = a.alpha > 0.0f && a.labels && (uint32_t)label < a.vocab;
+    const Scale scale = {HE_LOG2E / a.tau, masked_from(a.tau), ce_on && a.tau != 1.0f};
     const uint32_t kept = min(turns, (uint32_t)V), read = turns - kept;
     Vec<T> one, other, row_[V ? V : 1];
     auto at = [&](uint32_t p, bool back) { return (kept + (back ? (p < read ? read - 1 - p : 0) : p)) * THREADS + t; };
@@ -187,7 +189,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
         if (lane == 0 && ce_on) s.label_z = to_float<T>(z[label]);
         wave_sync();                                      // where no sums are taken, no barrier lies between this and its other lanes' reading
     }
-    Sum S = {NOTHING, 0}, S1 = {NOTHING, 0};
+    Sums S = {scale.low, 0, 0};
     if (LOSS) {
         if (REST) __syncthreads();
         each([&](uint32_t v, const Vec<T>& piece) {
@@ -209,35 +211,23 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
             float most = x[0];
 #pragma unroll
             for (int i = 1; i < N; i++) most = fmaxf(most, x[i]);
-            if (!(most > low)) most = -INFINITY;
-            raise(S, most * c);
-            const float R = ref_or_0(S.ref);
+            raise(S, most, scale);
+            const float R = scale.number(S.ref);
 #pragma unroll
-            for (int i = 0; i < N; i++) S.value += exp2_fast(fmaf(x[i], c, -R));
-            if (two) {
-                raise(S1, most * HE_LOG2E);
-                const float R1 = ref_or_0(S1.ref);
+            for (int i = 0; i < N; i++) S.value += scale.power(x[i] - R);
+            if (scale.two)
 #pragma unroll
-                for (int i = 0; i < N; i++) S1.value += exp2_fast(fmaf(x[i], HE_LOG2E, -R1));
-            }
+                for (int i = 0; i < N; i++) S.value1 += scale.power1(x[i] - R);
         }, false);
         if (GRAD) begin(true);                            // on their way while the sums are joined
-        S = wave_total(S);
-        if (two) S1 = wave_total(S1);
-        if (lane == 0) {
-            s.part[0][wave] = S;
-            s.part[1][wave] = S1;
-        }
+        S = wave_total(S, scale);
+        if (lane == 0) s.part[wave] = S;
         __syncthreads();
     }
     if (wave == 0) {
-        if (LOSS) {
-            S = total_of<WAVES>(s.part[0]);
-            S1 = two ? total_of<WAVES>(s.part[1]) : S;
-        } else {
-            S = {a.stats[row * 4], a.stats[row * 4 + 1]};
-            S1 = {a.stats[row * 4 + 2], a.stats[row * 4 + 3]};
-        }
+        if (LOSS) S = total_of<WAVES>(s.part, scale, lane);
+        else S = {a.stats[row * 4], a.stats[row * 4 + 1], a.stats[row * 4 + 2]};
+        if (!scale.two) S.value1 = S.value;
         struct {
             int32_t at[2];
             float t[2], z[2], p[2];
@@ -254,54 +244,53 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
         }
         const float rest = s.teacher[0], all_log = s.teacher[1], rest_log = s.teacher[2], teacher_most = s.teacher[3], zl = ce_on ? s.label_z : 0.0f;
         // all: against the larger of the reference and the named logits' largest
-        const float c1 = two ? HE_LOG2E : c, zt = fmaxf(REST && e.first[0] ? e.z[0] : -INFINITY, REST && e.first[1] ? e.z[1] : -INFINITY), zm = wave_max(zt);
-        const float M = !(zm > low) ? S.ref : fmaxf(S.ref, zm * c), M1 = !(zm > low) ? S1.ref : fmaxf(S1.ref, zm * c1);
-        const float R = ref_or_0(M), R1 = ref_or_0(M1);
+        const auto power1 = [&](float d) { return scale.two ? scale.power1(d) : scale.power(d); };
+        const float zt = fmaxf(REST && e.first[0] ? e.z[0] : -INFINITY, REST && e.first[1] ? e.z[1] : -INFINITY), M = fmaxf(S.ref, wave_max(zt)), R = scale.number(M);
         float x[2], x1[2];
 #pragma unroll
         for (int u = 0; u < 2; u++) {
-            x[u] = e.at[u] >= 0 ? exp2_fast(fmaf(e.z[u], c, -R)) : 0.0f;
-            x1[u] = e.at[u] >= 0 ? exp2_fast(fmaf(e.z[u], c1, -R1)) : 0.0f;
+            x[u] = e.at[u] >= 0 ? scale.power(e.z[u] - R) : 0.0f;
+            x1[u] = e.at[u] >= 0 ? power1(e.z[u] - R) : 0.0f;
         }
         const float top = wave_sum(REST ? (e.first[0] ? x[0] : 0.0f) + (e.first[1] ? x[1] : 0.0f) : 0.0f);
         const float top1 = wave_sum(REST ? (e.first[0] ? x1[0] : 0.0f) + (e.first[1] ? x1[1] : 0.0f) : 0.0f);
-        const float down = exp2_fast(S.ref - M), down1 = exp2_fast(S1.ref - M1), others = S.value * down;
-        const float Z = top + others, Z1 = top1 + S1.value * down1;
+        const float down = scale.power(S.ref - M), down1 = power1(S.ref - M), others = S.value * down;
+        const float Z = top + others, Z1 = top1 + S.value1 * down1;
         const bool dead = Z == 0.0f;                      // nothing but -infinity
         const bool kl_on = s.teacher[4] != 0.0f && a.alpha < 1.0f && !dead, ce = ce_on && !dead;
         if (LOSS) {
+            // tau times the divergence, so that a logit's distance from the largest stands as it is
             const float log_z = logf(Z);
             float term = 0;
 #pragma unroll
             for (int u = 0; u < 2; u++)
-                if (e.p[u] > 0.0f) term += e.p[u] * ((e.t[u] - teacher_most - all_log) - (fmaf(e.z[u], c, -R) * HE_LN2 - log_z));
+                if (e.p[u] > 0.0f) term += e.p[u] * (a.tau * (e.t[u] - teacher_most - all_log + log_z) - (e.z[u] - R));
             float kl = wave_sum(term);
             if (REST && rest > 0.0f) {
-                const float lq = others >= top ? -log1pf(top / others) : (S.ref - M) * HE_LN2 + logf(S.value) - log_z;
-                kl += rest * (rest_log - lq);
+                const float lq = others >= top ? -a.tau * log1pf(top / others) : scale.number(S.ref) - R + a.tau * (logf(S.value) - log_z);
+                kl += rest * (a.tau * rest_log - lq);
             }
             if (lane == 0) {
-                float loss = kl_on ? (1.0f - a.alpha) * a.tau * a.tau * kl : 0.0f;
-                if (ce) loss += a.alpha * (logf(Z1) - fmaf(zl, c1, -R1) * HE_LN2);
+                float loss = kl_on ? (1.0f - a.alpha) * a.tau * kl : 0.0f;
+                if (ce) loss += a.alpha * (logf(Z1) - (zl - R));
                 a.loss[row] = loss;
                 if (a.stats) {
                     a.stats[row * 4] = S.ref;
                     a.stats[row * 4 + 1] = S.value;
-                    a.stats[row * 4 + 2] = S1.ref;
-                    a.stats[row * 4 + 3] = S1.value;
+                    a.stats[row * 4 + 2] = S.value1;
+                    a.stats[row * 4 + 3] = 0;
                 }
             }
         }
         if (GRAD) {
             const float weight = a.weights[row], wk = kl_on ? weight * (1.0f - a.alpha) * a.tau : 0.0f, wc = ce ? weight * a.alpha : 0.0f;
             float fk = dead ? 0.0f : wk * (down / Z - (S.value > 0.0f ? rest / S.value : 0.0f)), fc = dead ? 0.0f : wc * (down1 / Z1);
-            const float label_power = ce ? exp2_fast(fmaf(zl, c1, -ref_or_0(S1.ref))) : 0.0f, label_power_k = ce ? exp2_fast(fmaf(zl, c, -ref_or_0(S.ref))) : 0.0f;
+            const float own = scale.number(S.ref), label_power = ce ? power1(zl - own) : 0.0f, label_power_k = ce ? scale.power(zl - own) : 0.0f;
             const bool alone = __all(e.at[0] != label && e.at[1] != label);
             if (lane == 0) {
-                s.factor[0] = ref_or_0(S.ref);
-                s.factor[1] = ref_or_0(S1.ref);
-                s.factor[2] = two ? fk : fk + fc;         // one temperature: one power
-                s.factor[3] = fc;
+                s.factor[0] = own;
+                s.factor[1] = scale.two ? fk : fk + fc;   // one temperature: one power
+                s.factor[2] = fc;
                 s.put_at[HE_TOP_MAX] = ce && alone ? label : -1;
                 s.put[HE_TOP_MAX] = (fk != 0.0f ? fk * label_power_k : 0.0f) + fc * label_power - wc;
             }
@@ -321,14 +310,14 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
     }
     if (!GRAD) return;
     __syncthreads();
-    const float R = s.factor[0], R1 = s.factor[1], fk = s.factor[2], fc = s.factor[3];
+    const float R = s.factor[0], fk = s.factor[1], fc = s.factor[2];
     each([&](uint32_t v, const Vec<T>& x) {
         float y[N];
 #pragma unroll
-        for (int i = 0; i < N; i++) y[i] = fk * exp2_fast(fmaf(x[i], c, -R));
-        if (two)
+        for (int i = 0; i < N; i++) y[i] = fk * scale.power(x[i] - R);
+        if (scale.two)
 #pragma unroll
-            for (int i = 0; i < N; i++) y[i] = fmaf(fc, exp2_fast(fmaf(x[i], HE_LOG2E, -R1)), y[i]);
+            for (int i = 0; i < N; i++) y[i] = fmaf(fc, scale.power1(x[i] - R), y[i]);
         Vec<T> g;
         g.set(y);
         in.store(grad, v, g, THREADS > 256);

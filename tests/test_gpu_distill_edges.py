@@ -1,13 +1,14 @@
 """GPU: the distillation loss and its gradient, and the top logits, at the edges of what their definitions say.
 
 Tolerances are those of the ordinary rows (test_gpu_distill.py): an edge changes what a row's result is, not how it is rounded."""
+import itertools
 import math
 
 import pytest
 import torch
 
 import plain_ref as R
-from test_gpu_distill import check_loss, check_top, rng, run_loss, run_top, teacher
+from test_gpu_distill import check_loss, check_top, rng, run_loss, run_top, teacher, with_masks
 
 pytestmark = pytest.mark.gpu
 MODES = ["step", "later", "onto"]
@@ -36,3 +37,56 @@ def test_label_of_a_gradient_taken_later(ctx, vocab, tau):
     weights = torch.rand(rows, generator=g) + 0.5
     want = R.distill(z, *t, tau, labels, alpha)
     check_loss(run_loss(ctx, z, t, tau, labels, alpha, weights, "later"), want, torch.float32, tau, alpha, weights)
+
+
+def by_definition(z, values, index, rest, tau, labels, alpha):
+    """(loss, gradient, the sum of what its terms amount to) for distinct entries that are all there.  The rest's share of each logit is a softmax of its
+    own: from logarithms of probabilities, as far below 0 as logits can be, it would be lost to rounding in 64 bits."""
+    x, at = z.double(), index.long()
+    t = torch.cat([values.double() / tau, torch.full((len(z), 1), -math.inf).double() if rest is None else rest.double()[:, None]], dim=1)
+    p, logp = torch.softmax(t, dim=1), torch.log_softmax(t, dim=1)
+    named = torch.zeros(z.shape, dtype=torch.bool).scatter_(1, at, True)
+    logq, others = torch.log_softmax(x / tau, dim=1), torch.where(named, -math.inf, x / tau)
+    kl, parts = (p[:, :-1] * (logp[:, :-1] - logq.gather(1, at))).sum(dim=1), [torch.softmax(x / tau, dim=1), -torch.zeros_like(x).scatter_(1, at, p[:, :-1])]
+    if rest is not None:
+        kl += p[:, -1] * (logp[:, -1] - torch.logsumexp(torch.where(named, -math.inf, logq), dim=1))
+        parts.append(-p[:, -1:] * torch.softmax(others, dim=1))
+    loss, parts = (1 - alpha) * tau ** 2 * kl, [(1 - alpha) * tau * q for q in parts]
+    if labels is not None:
+        y = labels.long()[:, None]
+        loss -= alpha * torch.log_softmax(x, dim=1).gather(1, y)[:, 0]
+        parts += [alpha * torch.softmax(x, dim=1), -alpha * torch.zeros_like(x).scatter_(1, y, 1.0)]
+    return loss, sum(parts), sum(q.abs() for q in parts)
+
+
+FAR = [-1e9, -1e10, -3e12, -1e20, -1e30, -1e36]
+
+
+@pytest.mark.parametrize("vocab", [3, 10, 700, 9001, 40000])
+@pytest.mark.parametrize("mode", ["step", "later"])
+def test_distillation_with_masks_that_are_numbers(ctx, mode, vocab):
+    """Masks of -1e9 to -1e36 are logits like others: beside real ones they are nothing, and a row of nothing else is uniform."""
+    g, alpha = rng(vocab), 0.25
+    for low, dtype, (tau, with_rest) in itertools.product(FAR, (torch.float32, torch.bfloat16), ((0.25, True), (1.0, False), (1.0, True), (3.0, False), (3.0, True))):
+        z = with_masks(8, vocab, low, vocab + 1).to(dtype)
+        t = teacher(torch.randn((8, vocab), generator=g), min(vocab - 1, 4), tau, g, with_rest)
+        labels, weights = z.double().argmax(dim=1).to(torch.int32), torch.rand(8, generator=g) + 0.5
+        want = by_definition(z, *t, tau, labels, alpha)
+        check_loss(run_loss(ctx, z, t, tau, labels, alpha, weights, mode, vocab + 1, 1), want, dtype, tau, alpha, weights)
+
+
+@pytest.mark.parametrize("vocab", [3, 40, 700, 9001, 40000])
+@pytest.mark.parametrize("tau,alpha,with_rest", [(0.25, 0.0, True), (1.0, 0.0, False), (1.0, 0.5, True), (4.0, 0.5, True), (4.0, 0.5, False)])
+def test_distillation_of_large_logits(ctx, tau, alpha, with_rest, vocab):
+    """Logits around a number of any size: what counts is how they differ.  Losses that 32 bits do not hold are infinite."""
+    g, rows = rng(vocab), 8
+    z = 3 * torch.randn((rows, vocab), generator=g)
+    t = teacher(z, 2, tau, g, with_rest)
+    z += torch.tensor([1e4, -1e6, 1e8, -1e8, 1e10, 1e20, 1e30, -1e30])[:, None]
+    z[5, int(t[1][5, 0])] = 3e20
+    z[6, vocab // 2] = 3.2e38
+    labels, weights = t[1][:, 0].clone() if alpha else None, torch.rand(rows, generator=g) + 0.5
+    loss, grad, size = by_definition(z, *t, tau, labels, alpha)
+    loss = torch.where(loss > 3.4e38, math.inf, loss)
+    for mode in ("step", "later"):
+        check_loss(run_loss(ctx, z, t, tau, labels, alpha, weights, mode), (loss, grad, size), torch.float32, tau, alpha, weights)
