@@ -28,12 +28,31 @@ template <int THREADS> struct TopShared {
     static constexpr int ROOM = THREADS == 1024 ? 1024 : THREADS == 64 ? 64 : 512, KEEP = 512;
     uint4 aside[ROOM];                         // 16 bytes of the row each, and which
     uint32_t which[ROOM];                      // index of the first of its elements, and above 24 bits how many are another's
-    u64 keep[KEEP], more;
+    u64 keep[KEEP], more, last;                // last: the k-th place
     uint32_t bins[256];
     int32_t tw[2][THREADS / 64];
     float room[THREADS / 64];
     uint32_t digit, left, got, kept;
 };
+
+// A sum times a power of two: what is beside nothing is nothing, also where it had become infinite
+__device__ __forceinline__ float times_power(float sum, float exponent) {
+    const float f = exp2_fast(exponent);
+    return f > 0.0f || sum != sum ? sum * f : 0.0f;
+}
+
+// d_rest of a row, whose k-th place is `last` and whose largest other logit that counts is `most`, by reading it once more
+template <class T, int THREADS> __device__ __forceinline__ void rest_of(const TopArgs& a, TopShared<THREADS>& s, u64 row, u64 last, float most) {
+    const typename T::raw* z = (const typename T::raw*)a.z + row * a.ld_z;
+    const float c = HE_LOG2E / a.tau, low = masked_from(a.tau), at = most == -INFINITY ? 0.0f : most;
+    float sum = 0;
+    for (uint32_t i = threadIdx.x; i < a.vocab; i += THREADS) {
+        const float v = to_float<T>(z[i]);
+        if (place_of(v, i) < last && !(v <= low)) sum += v >= -low ? INFINITY : exp2_fast((v - at) * c);
+    }
+    sum = group_sum<THREADS / 64>(sum, s.room);
+    if (threadIdx.x == 0) a.rest[row] = at >= -low ? sum : logf(sum) + at / a.tau;
+}
 
 // A row by reading it as often as it takes: the k-th largest place is found a digit of 8 bits at a time, from the row's counts of that digit
 // among the elements that agree with the digits before; then the elements from it on are gathered and the rest is summed against its own
@@ -84,15 +103,7 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
         a.values[row * a.k + place] = to_float<T>(z[i]);
         a.index[row * a.k + place] = (int32_t)i;
     }
-    if (!a.rest) return;
-    const float scale = HE_LOG2E / a.tau, at = most == -INFINITY ? 0.0f : most;
-    float sum = 0;
-    for (uint32_t i = t; i < a.vocab; i += THREADS) {
-        const float v = to_float<T>(z[i]);
-        if (place_of(v, i) < prefix && !(v <= low)) sum += v >= -low ? INFINITY : exp2_fast((v - at) * scale);
-    }
-    sum = group_sum<THREADS / 64>(sum, s.room);
-    if (t == 0) a.rest[row] = at >= -low ? sum : logf(sum) + at / a.tau;
+    if (a.rest) rest_of<T, THREADS>(a, s, row, prefix, most);
 }
 
 // One row a work group, read once, 16 bytes a lane at a time.  Pieces of 16 bytes with an element that reaches a threshold are set aside in
@@ -101,7 +112,10 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
 // smallest of those over the wavefronts is it.  It is taken anew after 0, 2, 6, 14 ... turns, so that of a row in no particular order a
 // few times k (1 + ln(turns)) pieces are set aside, and once more at the end.  Of the elements that reach the last one each counts how
 // many come before it: the first k are the result, in order.  The others join the sum as whole multiples of 2^-44 of the rest's largest
-// term, in any order the same number.  An element of -infinity can only be among the first k if its index is below k: of the first k
+// term, in any order the same number.  A term's exponent is one multiply-add, c z - R with R = c times the running maximum; the rounding of R
+// stays in it, 2^-25 of R, which is that of the result (its size is R ln 2) as long as it is a factor of at most 2^(1/2): up to R = 2^24.  Beyond, a lane's
+// sum may be off by any factor; it counts for nothing beside a rest below that, and a rest beyond it (of nothing but masks at -1e9, say) is
+// summed anew from differences.  An element of -infinity can only be among the first k if its index is below k: of the first k
 // elements at most as many are larger as there are larger ones at all.
 //
 // 2048 x 131072 bf16, k = 64: 144 us (3.7 TB/s), 90% of its cycles vector instructions: about 16 for an element, of which 8 are the sum's (one
@@ -157,7 +171,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
             }
         } else {
             if (mx > m) {
-                sum *= exp2_fast((m - mx) * c);
+                sum = times_power(sum, (m - mx) * c);
                 m = mx;
             }
             const float mc = m == low ? 0.0f : m * c;      // nothing that counts so far
@@ -200,6 +214,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
             const uint32_t at = ~(uint32_t)mine;
             a.values[row * a.k + place] = to_float<T>(z[at]);          // as it stands there: -0, the NaN's bits
             a.index[row * a.k + place] = (int32_t)at;
+            if (place == a.k - 1) s.last = mine;
         } else {
             over[q] = mine;
             most = fmaxf(most, value_of((uint32_t)(mine >> 32)));
@@ -208,6 +223,10 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     if (!a.rest) return;
     bool lost = false;                                   // a NaN among the rest
     most = group_max<WAVES>(most, s.room);
+    if (most > low && fabsf(most) * c >= 0x1p24f) {
+        __syncthreads();                                 // `last` is there
+        return rest_of<T, THREADS>(a, s, row, s.last, most);
+    }
     u64 more = 0;
     auto add = [&](float v) {
         lost = lost || v != v;
@@ -221,7 +240,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     for (int q = 0; q < Q; q++)
         if (over[q]) add(value_of((uint32_t)(over[q] >> 32)));
     if (more) atomicAdd((unsigned long long*)&s.more, (unsigned long long)more);
-    sum = group_sum<WAVES>(!(most < -low) ? 0.0f : sum * exp2_fast((m - most) * c), s.room);
+    sum = group_sum<WAVES>(!(most < -low) ? 0.0f : times_power(sum, (m - most) * c), s.room);
     lost = __syncthreads_or(lost);
     if (t == 0) a.rest[row] = lost ? NAN : most >= -low ? INFINITY : logf(sum + (float)s.more * 0x1p-44f) + most / a.tau;
 }

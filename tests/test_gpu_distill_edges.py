@@ -90,3 +90,20 @@ def test_distillation_of_large_logits(ctx, tau, alpha, with_rest, vocab):
     loss = torch.where(loss > 3.4e38, math.inf, loss)
     for mode in ("step", "later"):
         check_loss(run_loss(ctx, z, t, tau, labels, alpha, weights, mode), (loss, grad, size), torch.float32, tau, alpha, weights)
+
+
+@pytest.mark.parametrize("vocab", [3, 10, 200, 700, 1000, 9001, 40000])
+def test_top_with_masks_that_are_numbers(ctx, vocab):
+    for low, dtype, tau in itertools.product(FAR, (torch.float32, torch.bfloat16), (0.25, 1.0, 3.0)):
+        z = with_masks(8, vocab, low, vocab).to(dtype)
+        for k in (1, min(5, vocab)):
+            check_top(run_top(ctx, z, k, tau, vocab + 1, 1), R.top(z, k, tau))
+
+
+@pytest.mark.parametrize("vocab", [3, 40, 700, 9001, 40000])
+def test_top_of_large_logits(ctx, vocab):
+    z = 3 * torch.randn((8, vocab), generator=rng(vocab))
+    z += torch.tensor([1e4, -1e6, 1e8, -1e8, 1e10, 1e20, 1e30, -1e30])[:, None]
+    z[5, vocab // 2], z[6, vocab // 3] = 3e20, 1e36
+    for k, tau in itertools.product((1, min(20, vocab)), (0.25, 1.0, 30.0)):
+        check_top(run_top(ctx, z, k, tau), R.top(z, k, tau))
