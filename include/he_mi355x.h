@@ -440,7 +440,8 @@ int32_t he_top_logits(he_ctx* ctx, const he_top_plan* plan);
  * two and y the row's label
  *   loss = (1 - alpha) tau^2 sum P log(P / Q) + alpha (log-sum-exp(z) - z[y]).
  * Entries whose index is outside 0..vocab-1 are not there; an index that stands twice adds its probabilities.  Where nothing of
- * the teacher is there, or it is -infinity throughout, the first term is 0.  A row whose label is negative is padding: loss and
+ * the teacher is there, or it is -infinity throughout, the first term is 0.  Where what is there holds a NaN or +infinity (a value counts
+ * divided by tau, in 32 bits), its distribution is none: the loss is NaN, and so is the gradient where it has a part in it.  A row whose label is negative is padding: loss and
  * gradient 0.  So are those of a row whose student logits are all -infinity.  A label >= vocab is not there: the second term is 0.
  * Without d_labels alpha has to be 0.
  * he_distill_loss writes d_loss [rows], and d_stats if that is given; with d_grad it also writes, in the same pass over the

@@ -259,14 +259,15 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
         const bool dead = Z == 0.0f;                      // nothing but -infinity
         const bool kl_on = s.teacher[4] != 0.0f && a.alpha < 1.0f && !dead, ce = ce_on && !dead;
         if (LOSS) {
-            // tau times the divergence, so that a logit's distance from the largest stands as it is
+            // tau times the divergence, so that a logit's distance from the largest stands as it is.  What has no probability is left out; a
+            // probability that is not a number, a teacher's that is not finite, makes the loss one that is none.
             const float log_z = logf(Z);
             float term = 0;
 #pragma unroll
             for (int u = 0; u < 2; u++)
-                if (e.p[u] > 0.0f) term += e.p[u] * (a.tau * (e.t[u] - teacher_most - all_log + log_z) - (e.z[u] - R));
+                if (e.p[u] != 0.0f) term += e.p[u] * (a.tau * (e.t[u] - teacher_most - all_log + log_z) - (e.z[u] - R));
             float kl = wave_sum(term);
-            if (REST && rest > 0.0f) {
+            if (REST && rest != 0.0f) {
                 const float lq = others >= top ? -a.tau * log1pf(top / others) : scale.number(S.ref) - R + a.tau * (logf(S.value) - log_z);
                 kl += rest * (a.tau * rest_log - lq);
             }

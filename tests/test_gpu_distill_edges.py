@@ -107,3 +107,30 @@ def test_top_of_large_logits(ctx, vocab):
     z[5, vocab // 2], z[6, vocab // 3] = 3e20, 1e36
     for k, tau in itertools.product((1, min(20, vocab)), (0.25, 1.0, 30.0)):
         check_top(run_top(ctx, z, k, tau), R.top(z, k, tau))
+
+
+def spoilt_teacher(z, tau, g, with_rest):
+    """A teacher that is not finite in rows 1, 3, 5 and 6 (the last two in what it gives the rest), and in an entry of row 7 that is not there."""
+    v, i, r = teacher(z, 3, tau, g, with_rest)
+    v[1, 2], v[3, 0], v[7, 1], i[7, 1] = math.nan, math.inf, math.nan, -1
+    if with_rest:
+        r[5], r[6] = math.nan, math.inf
+    return (v, i, r), [1, 3, 5, 6] if with_rest else [1, 3]
+
+
+@pytest.mark.parametrize("vocab", [3, 40, 700, 9001, 40000])
+@pytest.mark.parametrize("with_rest", [False, True])
+@pytest.mark.parametrize("mode", MODES)
+def test_a_teacher_that_is_not_finite(ctx, mode, with_rest, vocab):
+    """Its distribution is not one of numbers, and neither is the loss: never a finite one without a sign of it."""
+    g, rows, tau, alpha = rng(vocab), 9, 2.0, 0.25
+    z = 2 * torch.randn((rows, vocab), generator=g)
+    t, spoilt = spoilt_teacher(z, tau, g, with_rest and vocab > 3)
+    labels = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+    weights = torch.rand(rows, generator=g) + 0.5
+    got = run_loss(ctx, z, t, tau, labels, alpha, weights, mode, vocab + 1, 1)
+    loss, grad = got[:2]
+    assert loss[spoilt].isnan().all() and grad[spoilt].isnan().any(dim=1).all()
+    sound = [r for r in range(rows) if r not in spoilt]
+    want = R.distill(z, t[0].nan_to_num(nan=0.0), *t[1:], tau, labels, alpha)          # row 7's entry is not there
+    check_loss(rows_of(got[:2], sound) + (0,), rows_of(want[:2], sound) + (want[2][sound],), torch.float32, tau, alpha, weights[sound])
