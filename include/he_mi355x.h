@@ -443,7 +443,8 @@ int32_t he_top_logits(he_ctx* ctx, const he_top_plan* plan);
  * the teacher is there, or it is -infinity throughout, the first term is 0.  Where what is there holds a NaN or +infinity (a value counts
  * divided by tau, in 32 bits), its distribution is none: the loss is NaN, and so is the gradient where it has a part in it.  A row whose label is negative is padding: loss and
  * gradient 0.  So are those of a row whose student logits are all -infinity.  A label >= vocab is not there: the second term is 0.
- * Without d_labels alpha has to be 0.
+ * Without d_labels alpha has to be 0; with alpha = 1 the first term is 0, whatever the teacher is.  A term that is 0 by these rules has
+ * no gradient, whatever the logits are.
  * he_distill_loss writes d_loss [rows], and d_stats if that is given; with d_grad it also writes, in the same pass over the
  * logits, d_row_weights[row] times the gradient of the row's loss by z (in z's type; d_grad may be d_z with the same ld).
  * he_distill_grad writes that gradient from the d_stats that he_distill_loss left for the same operands. */

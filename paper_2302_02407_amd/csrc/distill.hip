@@ -62,6 +62,7 @@ template <int WAVES> struct RowShared {
     float put[HE_TOP_MAX + 1];
     Sums part[WAVES];
     float factor[3];                // R and the factors of the two powers
+    int32_t none;                   // neither term is there
 };
 
 // The teacher's entries of a row and what goes with them, by one wavefront, entry lane + 64 u; in LDS until the sums are there
@@ -130,11 +131,13 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
     const R_ in{z, a.vocab};
     const uint32_t turns = (in.pieces() + THREADS - 1) / THREADS;
     const int32_t label = a.labels ? a.labels[row] : 0;
+    auto no_gradient = [&]() {
+        for (uint32_t p = 0; p < turns; p++) in.store(grad, p * THREADS + t, Vec<T>{{0, 0, 0, 0}}, false);
+    };
     if (a.labels && label < 0) {
         if (LOSS && t == 0) a.loss[row] = 0;
         if (LOSS && a.stats && t < 4) a.stats[row * 4 + t] = 0;
-        if (GRAD)
-            for (uint32_t p = 0; p < turns; p++) in.store(grad, p * THREADS + t, Vec<T>{{0, 0, 0, 0}}, false);
+        if (GRAD) no_gradient();
         return;
     }
     const uint32_t words = (a.vocab + 31) / 32;
@@ -284,11 +287,13 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
             }
         }
         if (GRAD) {
-            const float weight = a.weights[row], wk = kl_on ? weight * (1.0f - a.alpha) * a.tau : 0.0f, wc = ce ? weight * a.alpha : 0.0f;
-            float fk = dead ? 0.0f : wk * (down / Z - (S.value > 0.0f ? rest / S.value : 0.0f)), fc = dead ? 0.0f : wc * (down1 / Z1);
+            // a term that is not there adds nothing, though what it would be made of need not be a number
+            const float weight = a.weights[row], wk = weight * (1.0f - a.alpha) * a.tau, wc = ce ? weight * a.alpha : 0.0f;
+            const float fk = kl_on ? wk * (down / Z - (S.value > 0.0f ? rest / S.value : 0.0f)) : 0.0f, fc = ce ? wc * (down1 / Z1) : 0.0f;
             const float own = scale.number(S.ref), label_power = ce ? power1(zl - own) : 0.0f, label_power_k = ce ? scale.power(zl - own) : 0.0f;
             const bool alone = __all(e.at[0] != label && e.at[1] != label);
             if (lane == 0) {
+                s.none = !kl_on && !ce;
                 s.factor[0] = own;
                 s.factor[1] = scale.two ? fk : fk + fc;   // one temperature: one power
                 s.factor[2] = fc;
@@ -302,7 +307,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
                 float q = 0;
                 if (e.first[u])
                     for (uint32_t i = 0; i < a.k; i++) q += s.at[i] == e.at[u] ? s.entry[i].p : 0.0f;
-                float g = dead ? 0.0f : wk * (x[u] / Z - q) + wc * (x1[u] / Z1);
+                float g = (kl_on ? wk * (x[u] / Z - q) : 0.0f) + (ce ? wc * (x1[u] / Z1) : 0.0f);
                 if (ce && e.at[u] == label) g -= wc;
                 s.put_at[j] = e.first[u] ? e.at[u] : -1;
                 s.put[j] = g;
@@ -311,6 +316,7 @@ template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST
     }
     if (!GRAD) return;
     __syncthreads();
+    if (s.none) return no_gradient();
     const float R = s.factor[0], fk = s.factor[1], fc = s.factor[2];
     each([&](uint32_t v, const Vec<T>& x) {
         float y[N];

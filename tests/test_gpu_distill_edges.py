@@ -134,3 +134,27 @@ def test_a_teacher_that_is_not_finite(ctx, mode, with_rest, vocab):
     sound = [r for r in range(rows) if r not in spoilt]
     want = R.distill(z, t[0].nan_to_num(nan=0.0), *t[1:], tau, labels, alpha)          # row 7's entry is not there
     check_loss(rows_of(got[:2], sound) + (0,), rows_of(want[:2], sound) + (want[2][sound],), torch.float32, tau, alpha, weights[sound])
+
+
+@pytest.mark.parametrize("vocab", [3, 40, 700, 9001, 40000])
+@pytest.mark.parametrize("mode", MODES)
+def test_a_term_that_is_not_there_adds_nothing(ctx, mode, vocab):
+    """With alpha = 1 the teacher does not count, whatever it is; a row that has neither term has no gradient, whatever the student is."""
+    g, rows, tau = rng(vocab), 9, 2.0
+    z = 2 * torch.randn((rows, vocab), generator=g)
+    t, _ = spoilt_teacher(z, tau, g, vocab > 3)
+    labels = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+    weights = torch.rand(rows, generator=g) + 0.5
+    any_finite = [None if x is None else x.nan_to_num(nan=0.0, posinf=0.0) for x in t]
+    check_loss(run_loss(ctx, z, t, tau, labels, 1.0, weights, mode), R.distill(z, *any_finite, tau, labels, 1.0), torch.float32, tau, 1.0, weights)
+    none = [torch.zeros((rows, 3)), torch.full((rows, 3), -1, dtype=torch.int32), None]
+    z[1, vocab // 2], z[3, 0], z[4], z[5] = math.nan, math.inf, math.nan, -math.inf
+    labels[:] = vocab
+    loss, grad, _ = run_loss(ctx, z, none, tau, None, 0.0, weights, mode)
+    assert (loss == 0).all() and (grad == 0).all()
+    for alpha in (0.25, 1.0):
+        loss, grad, _ = run_loss(ctx, z, none, tau, labels, alpha, weights, mode)
+        assert (loss == 0).all() and (grad == 0).all()
+    labels[:] = 0
+    loss, grad, _ = run_loss(ctx, z, none, tau, labels, 0.25, weights, mode)       # one of the two is there
+    assert loss[[1, 3, 4]].isnan().all() and grad[[1, 3, 4]].isnan().any(dim=1).all() and grad[[0, 2, 5, 6, 7, 8]].isfinite().all()
