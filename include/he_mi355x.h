@@ -425,7 +425,7 @@ int32_t he_ws_query_matmul_q8(const he_ctx* ctx, const he_matmul_plan* plan, uin
 typedef struct {
     uint32_t rows, vocab, k;       /* 1 <= k <= min(vocab, HE_TOP_MAX), vocab <= 2^20 */
     int32_t dtype;
-    float tau;                     /* > 0 */
+    float tau;                     /* from 2^-60 to 2^60 */
     const void* d_z;
     uint64_t ld_z;
     float* d_values;
@@ -451,7 +451,7 @@ int32_t he_top_logits(he_ctx* ctx, const he_top_plan* plan);
 typedef struct {
     uint32_t rows, vocab, k;       /* k from 1 to HE_TOP_MAX, vocab from 1 to 2^20 */
     int32_t dtype;                 /* of z and of the gradient */
-    float tau, alpha;              /* tau > 0, 0 <= alpha <= 1 */
+    float tau, alpha;              /* tau from 2^-60 to 2^60, 0 <= alpha <= 1 */
     const void* d_z;
     uint64_t ld_z;
     const float* d_values;         /* [rows][k] */

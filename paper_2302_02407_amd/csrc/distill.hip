@@ -340,7 +340,7 @@ static int32_t check(he_ctx* ctx, const he_distill_plan* p, const char* who) {
     if (!dtype_known(p->dtype)) return he_fail(ctx, HE_ERR_BADARG, "%s: unknown type %d", who, p->dtype);
     if (p->vocab == 0 || p->vocab > HE_VOCAB_MAX) return he_fail(ctx, HE_ERR_BADARG, "%s: %u logits outside 1..2^20", who, p->vocab);
     if (p->k == 0 || p->k > HE_TOP_MAX) return he_fail(ctx, HE_ERR_BADARG, "%s: k = %u outside 1..%d", who, p->k, HE_TOP_MAX);
-    if (!(p->tau > 0.0f) || p->tau == INFINITY) return he_fail(ctx, HE_ERR_BADARG, "%s: the temperature is not a positive number", who);
+    if (!tau_fits(p->tau)) return he_fail(ctx, HE_ERR_BADARG, "%s: the temperature is not a number from 2^-60 to 2^60", who);
     if (!(p->alpha >= 0.0f && p->alpha <= 1.0f)) return he_fail(ctx, HE_ERR_BADARG, "%s: alpha outside 0..1", who);
     if (p->rows > HE_ROWS_MAX) return he_fail(ctx, HE_ERR_BADARG, "%s: more than 2^21 rows", who);
     if (p->alpha > 0.0f && !p->d_labels && p->rows) return he_fail(ctx, HE_ERR_BADARG, "%s: alpha without labels", who);

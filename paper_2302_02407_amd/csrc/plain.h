@@ -199,6 +199,8 @@ static inline bool overlap(const void* a, uint64_t na, const void* b, uint64_t n
 static inline uint64_t span(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t size) { return rows && cols ? ((rows - 1) * ld + cols) * size : 0; }
 // Rows of `cols` elements, ld apart: they do not overlap, and no offset of HE_ROWS_MAX of them leaves 64 bits
 static inline bool ld_fits(uint64_t ld, uint64_t cols) { return ld >= cols && ld <= (1u << 28); }
+// Temperatures of which log2(e) / tau and tau^2 are numbers, and at which a masked logit, from 2^126 on, is far from any other
+static inline bool tau_fits(float tau) { return tau >= 0x1p-60f && tau <= 0x1p60f; }
 #define HE_ROWS_MAX (1u << 21)     // a work group of at most 1024 threads a row: a launch's threads stay below 2^32
 #define HE_VOCAB_MAX (1u << 20)
 // Kernel arguments have been checked; what can still fail is the launch

@@ -252,7 +252,7 @@ extern "C" int32_t he_top_logits(he_ctx* ctx, const he_top_plan* p) {
     if (!dtype_known(p->dtype)) return he_fail(ctx, HE_ERR_BADARG, "he_top_logits: unknown type %d", p->dtype);
     if (p->vocab == 0 || p->vocab > HE_VOCAB_MAX) return he_fail(ctx, HE_ERR_BADARG, "he_top_logits: %u logits outside 1..2^20", p->vocab);
     if (p->k == 0 || p->k > HE_TOP_MAX || p->k > p->vocab) return he_fail(ctx, HE_ERR_BADARG, "he_top_logits: k = %u outside 1..min(vocab, %d)", p->k, HE_TOP_MAX);
-    if (!(p->tau > 0.0f) || p->tau == INFINITY) return he_fail(ctx, HE_ERR_BADARG, "he_top_logits: the temperature is not a positive number");
+    if (!tau_fits(p->tau)) return he_fail(ctx, HE_ERR_BADARG, "he_top_logits: the temperature is not a number from 2^-60 to 2^60");
     if (p->rows > HE_ROWS_MAX) return he_fail(ctx, HE_ERR_BADARG, "he_top_logits: more than 2^21 rows");
     if (p->rows == 0) return HE_OK;
     if (!p->d_z || !p->d_values || !p->d_index) return he_fail(ctx, HE_ERR_BADARG, "he_top_logits: null argument");

@@ -158,3 +158,25 @@ def test_a_term_that_is_not_there_adds_nothing(ctx, mode, vocab):
     labels[:] = 0
     loss, grad, _ = run_loss(ctx, z, none, tau, labels, 0.25, weights, mode)       # one of the two is there
     assert loss[[1, 3, 4]].isnan().all() and grad[[1, 3, 4]].isnan().any(dim=1).all() and grad[[0, 2, 5, 6, 7, 8]].isfinite().all()
+
+
+def test_temperatures_that_32_bits_do_not_carry(ctx):
+    """From 2^-60 to 2^60 a row's factors (log2(e) / tau, tau^2) and a masked logit's power are what they should be; others are refused."""
+    from paper_2302_02407_amd.binding import HEError
+    g = rng(1)
+    z = torch.randn((5, 700), generator=g)
+    z[1:3, 100:600] = torch.finfo(torch.float32).min
+    z[3] = torch.finfo(torch.float32).min
+    for tau in (2.0 ** -60, 2.0 ** 60):
+        got, (values, index, _) = run_top(ctx, z, 5, tau), R.top(z, 5, tau)
+        check_top(got, (values, index, R.top(torch.where(z < -1e30, -math.inf, z.double()), 5, tau)[2]))
+    d, v, i, r = z.cuda(), torch.zeros((5, 4), device="cuda"), torch.zeros((5, 4), dtype=torch.int32, device="cuda"), torch.zeros(5, device="cuda")
+    for tau in (2.0 ** -61, 2.0 ** 61, 1e-40, 1e38):
+        for call in (lambda: ctx.he_top_logits(d, tau, v, i, r), lambda: ctx.he_distill_loss(d, v, i, r, tau, torch.zeros(5, device="cuda")),
+                     lambda: ctx.he_distill_grad(d, v, i, r, tau, torch.zeros((5, 4), device="cuda"), r, torch.zeros_like(d))):
+            with pytest.raises(HEError) as e:
+                call()
+            assert e.value.code == -1
+    for tau in (2.0 ** -60, 2.0 ** 60):
+        ctx.he_distill_loss(d, v, i, None, tau, r)
+    torch.cuda.synchronize()
