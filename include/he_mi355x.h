@@ -371,7 +371,7 @@ int32_t he_ws_query_ca_ra_block(const he_ctx* ctx, const he_block_plan* plan, ui
 typedef enum { HE_F32 = 0, HE_BF16 = 1, HE_F16 = 2 } he_dtype;
 
 /* h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight; per 128 columns scale = max|y| / 448 and code = e4m3(y / scale); a
- * block of zeros has scale 0 and codes 0, one that holds an infinity or a NaN has a scale that is not finite.  d_sum receives h in
+ * block of zeros has scale 0 and codes 0, one that holds an infinity or a NaN (h times its weight in 32 bits too) has a scale that is not finite.  d_sum receives h in
  * the inputs' type (the norm takes it before that rounding).  d_residual and d_sum: both or neither; d_weight may be NULL (ones).
  * d_sum may be d_x or d_residual (with the same ld); no output may overlap an input otherwise, or another output. */
 typedef struct {

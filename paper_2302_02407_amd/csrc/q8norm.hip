@@ -89,7 +89,31 @@ template <class T, bool RES, int ROW, int V> __global__ __launch_bounds__(ROW < 
         for (int i = 0; i < 8; i++) sq += h[p][i] * h[p][i];
     }
     sq = group_sum<ROW / 64>(sq, room);
-    const float r = 1.0f / sqrtf(sq / (float)a.dim + a.eps);
+    float mean = sq / (float)a.dim, r = 1.0f / sqrtf(mean + a.eps);
+    int e = 0;                                            // of a power of two that the row is taken by
+    if (mean < 0x1p-100f || mean == INFINITY) {           // squares that are no numbers, or rounded to the smallest ones: anew, by the largest element
+        float most = 0;
+#pragma unroll
+        for (int p = 0; p < V; p++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(h[p][i]));
+        most = group_max<ROW / 64>(most, room);
+        if (most == 0.0f) r = 0;                          // zeros stay zeros, without eps too
+        else if (most < INFINITY) {
+            e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
+            sq = 0;
+#pragma unroll
+            for (int p = 0; p < V; p++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float x = ldexpf(h[p][i], -e);
+                    sq += x * x;
+                }
+            mean = group_sum<ROW / 64>(sq, room) / (float)a.dim;
+            const float root = ldexpf(sqrtf(a.eps), -e);  // where it is far above the row's size, what the row adds is below its rounding
+            r = root > 0x1p30f ? ldexpf(1.0f / sqrtf(a.eps), e) : 1.0f / sqrtf(mean + root * root);
+        }
+    }
 #pragma unroll
     for (int p = 0; p < V; p++) {
         const uint32_t at = (p * ROW + t) * 8;
@@ -104,6 +128,9 @@ template <class T, bool RES, int ROW, int V> __global__ __launch_bounds__(ROW < 
                 for (int i = 0; i < 8; i++)
                     if (at + i < a.dim) sum[at + i] = from_float<T>(h[p][i]);
         }
+        if (e)
+#pragma unroll
+            for (int i = 0; i < 8; i++) h[p][i] = ldexpf(h[p][i], -e);
         if (!ALL) {
             __builtin_amdgcn_sched_barrier(0);
             if (weighted) scale[p].load(w + min(at, a.dim - 8));
