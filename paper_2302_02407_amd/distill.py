@@ -48,10 +48,13 @@ def quantize_table(w):
 
 
 class TeacherHead:
-    """The last steps of a teacher and its answers, for up to `rows` rows at a time; what lies between stays in buffers made here."""
+    """The last steps of a teacher and its answers, for up to `rows` rows at a time; what lies between stays in buffers made here.
 
-    def __init__(self, ctx, table, norm_weight, rows, k, tau, eps=1e-6, dtype=torch.bfloat16, fast_sums=True):
-        self.ctx, self.k, self.tau, self.eps, self.norm_weight, self.fast_sums = ctx, k, tau, eps, norm_weight, fast_sums
+    fast_sums: whether the product's sums may lose what he_matmul_q8 says; None: where the logits have 16 bits."""
+
+    def __init__(self, ctx, table, norm_weight, rows, k, tau, eps=1e-6, dtype=torch.bfloat16, fast_sums=None):
+        self.ctx, self.k, self.tau, self.eps, self.norm_weight = ctx, k, tau, eps, norm_weight
+        self.fast_sums = dtype != torch.float32 if fast_sums is None else fast_sums
         self.table, self.table_scales = quantize_table(table)
         vocab, dim = table.shape
         self.codes = _code_rows(rows, dim, table.device)
