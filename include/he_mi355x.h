@@ -398,9 +398,11 @@ int32_t he_rmsnorm_q8(he_ctx* ctx, const he_rmsnorm_plan* plan);
 typedef struct {
     uint32_t m, n, k;              /* k from 1 to 2^20; m, n <= 2^20, m * n <= 2^33; ld_a, ld_w <= 2^23 */
     int32_t out_dtype;
-    uint32_t fast_sums;            /* != 0: within a block of 128 columns the sums may be taken by the matrix instruction of 8-bit numbers, which
-                                      drops of a product what lies 13 binary orders below the largest product of its group of
-                                      columns: about 2e-5 of a typical result, well below what a result rounded to 16 bits loses */
+    uint32_t fast_sums;            /* != 0: within a block of 128 columns the sums may be taken by the matrix instruction of 8-bit numbers (whether they
+                                      are goes by the sizes), which drops of a product what lies 13 binary orders below the largest
+                                      product of its group of columns: about 2e-5 of a typical result, up to 1e-4 of the sum of its
+                                      terms' magnitudes (measured), never more than 2^-6 of the largest product of each block.  A result that is small by
+                                      cancellation can be off by more than its rounding to 16 bits */
     const uint8_t* d_a;
     uint64_t ld_a;
     const float* d_a_scales;
