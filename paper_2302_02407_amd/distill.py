@@ -41,9 +41,9 @@ def quantize_table(w):
     whole[:n, :k] = w
     blocks = whole.view(nb, BLOCK, kb, BLOCK)
     scales = blocks.abs().amax(dim=(1, 3)) / F8_MAX
-    inverse = torch.where(scales > 0, 1 / scales, 0.0)[:, None, :, None]
+    by = torch.where(scales == 0, 1.0, scales)[:, None, :, None]         # a quotient: the inverse of the smallest scales is no number
     codes = _code_rows(n, k, w.device)
-    codes.copy_((blocks * inverse).clamp_(-F8_MAX, F8_MAX).reshape(nb * BLOCK, kb * BLOCK)[:n, :k].to(F8))
+    codes.copy_((blocks / by).clamp_(-F8_MAX, F8_MAX).reshape(nb * BLOCK, kb * BLOCK)[:n, :k].to(F8))
     return codes, scales
 
 
