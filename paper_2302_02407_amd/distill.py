@@ -98,5 +98,8 @@ class _DistillLoss(torch.autograd.Function):
 
 
 def distill_loss(ctx, z, answers, tau, labels=None, alpha=0.0):
-    """One loss for each row of the student's logits z, differentiable by z; tau as it was for the answers."""
+    """One loss for each row of the student's logits z, differentiable by z; tau as it was for the answers.  Labels are int32, or int64 as torch's
+    losses take them: a negative one is padding, one beyond the vocabulary is not there."""
+    if labels is not None and labels.dtype == torch.int64:
+        labels = labels.clamp(-1, z.shape[-1]).to(torch.int32)
     return _DistillLoss.apply(z if z.stride(-1) == 1 else z.contiguous(), ctx, answers, tau, labels, alpha)
