@@ -164,7 +164,7 @@ def _need(t, n, what):
 
 
 def _rows(t, what, rows, cols, dtypes):
-    """Pointer and row pitch of a matrix of plain numbers whose rows are contiguous, given that it is what the call needs."""
+    """Pointer and row pitch of a matrix of plain numbers whose rows are contiguous, given that it is what the call needs; a single row has any pitch."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
         raise TypeError("%s must be a CUDA tensor" % what)
     if t.dtype not in dtypes:
@@ -174,7 +174,7 @@ def _rows(t, what, rows, cols, dtypes):
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("%s: the elements of a row must be contiguous" % what)
-    return t.data_ptr(), ld if rows > 1 or ld > cols else cols
+    return t.data_ptr(), ld if rows > 1 else cols
 
 
 def _codes(t, what, rows, cols):
@@ -182,7 +182,7 @@ def _codes(t, what, rows, cols):
     ptr, ld = _rows(t, what, rows, cols, _CODES)
     if cols % 16:
         if rows <= 1:
-            ld = -(-ld // 16) * 16
+            ld = -(-cols // 16) * 16
         if rows and t.untyped_storage().nbytes() - t.storage_offset() < (rows - 1) * ld + -(-cols // 16) * 16:
             raise ValueError("%s: the last row ends before the next multiple of 16 bytes" % what)
     return ptr, ld

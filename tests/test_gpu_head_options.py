@@ -1,5 +1,4 @@
 """GPU: what the plaintext side's sequencing chooses for a caller, and takes from one."""
-import math
 
 import pytest
 import torch
@@ -51,3 +50,26 @@ def test_labels_of_64_bits(ctx):
         grads.append(d.grad)
     assert torch.equal(*losses) and torch.equal(*grads)
     assert (losses[0][[0, 2, 4]] == 0).all() and (losses[0][[1, 3, 5]] != 0).all()
+
+
+def test_one_row_of_any_pitch(ctx):
+    """How far a single row's next one would be does not matter."""
+    g = torch.Generator().manual_seed(3)
+    dim, n = 96, 40
+    x = torch.randn((3, 101), generator=g).cuda()[:1, :dim]
+    codes, scales = torch.zeros((3, 100), dtype=R.F8, device="cuda")[:1, :dim], torch.zeros((3, 7), device="cuda")[:1, :1]
+    ctx.he_rmsnorm_q8(x, codes, scales, 1e-6)
+    near = torch.zeros((1, dim), dtype=R.F8, device="cuda"), torch.zeros((1, 1), device="cuda")
+    ctx.he_rmsnorm_q8(x.contiguous(), *near, 1e-6)
+    assert torch.equal(codes.view(torch.uint8), near[0].view(torch.uint8)) and torch.equal(scales, near[1])
+    w, sw, out, want = torch.randn((n, dim), generator=g).to(R.F8).cuda(), torch.ones((1, 1), device="cuda"), torch.zeros((1, n), device="cuda"), torch.zeros((1, n), device="cuda")
+    ctx.he_matmul_q8(codes, scales, w, sw, out)
+    ctx.he_matmul_q8(*near, w, sw, want)
+    assert torch.equal(out, want)
+    one = w.as_strided((1, dim), (1 << 29, 1))                # a pitch that rows could not have
+    ctx.he_matmul_q8(codes, scales, one, sw, out[:, :1])
+    assert torch.equal(out[:, :1], want[:, :1])
+    z = torch.randn((2, 700), generator=g).cuda()
+    values, index = torch.zeros((1, 3), device="cuda"), torch.zeros((1, 3), dtype=torch.int32, device="cuda")
+    ctx.he_top_logits(z.as_strided((1, 700), (1 << 29, 1)), 1.0, values, index)
+    assert torch.equal(index.cpu().long(), R.top(z[:1].cpu(), 3, 1.0)[1])
