@@ -16,6 +16,7 @@ real ones look like limb by limb), generated on the device, so the timed region 
 everything resident in HBM.
 """
 import argparse
+import contextlib
 import gc
 import json
 import os
@@ -44,6 +45,18 @@ def _profile_constant(path, key, build_id):
         return val if stamp == build_id else None
     except OSError:
         return None
+
+
+@contextlib.contextmanager
+def without_collection():
+    """No garbage collection inside; afterwards as it was, also where the inside raises."""
+    was = gc.isenabled()
+    gc.disable()
+    try:
+        yield
+    finally:
+        if was:
+            gc.enable()
 
 
 def uniform_dev(torch, gen, moduli, N, lead=()):
@@ -205,13 +218,12 @@ def main():
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         fn()
         torch.cuda.synchronize()
-        gc.disable()                               # a full collection takes 37 ms, the calls below one or less
-        e0.record()
-        for _ in range(reps):
-            fn()
-        e1.record()
-        torch.cuda.synchronize()
-        gc.enable()
+        with without_collection():                 # a full one takes 37 ms, the calls below one or less
+            e0.record()
+            for _ in range(reps):
+                fn()
+            e1.record()
+            torch.cuda.synchronize()
         return e0.elapsed_time(e1) / reps
 
 
