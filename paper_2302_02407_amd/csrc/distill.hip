@@ -113,12 +113,13 @@ template <class T, int WAVES> __device__ __forceinline__ void named_entries(cons
 // GRAD alone takes the sums from the statistics.  16 bytes a lane at a time, sums against each lane's running reference.  Loss and gradient
 // together need the row twice: V pieces a lane stay in registers between (16 of them: 64 of 128 registers; with 512 threads a work group 128
 // KiB, two work groups to a compute unit, one of which reads or writes while the other adds up), what is beyond is read again, backwards,
-// so that the caches still have some of it, and the gradient of long rows is written past them.
+// so that the caches still have some of it (of the half that is read again a tenth in the die's own, counted), and the gradient of long rows
+// is written past them.
 //
-// 4096 x 131072 bf16, both: 467 us (4.6 TB/s of one read and one write).  With nothing kept 529 us, without its second pass going
-// backwards past the caches 483; all of the row kept, one work group of 1024 threads to a compute unit, 680: nothing runs beside its sums.
-// 4096 x 50021: 236 us, with nothing kept 283; 8192 x 10000, too short for it to matter: 92 us, with 16 pieces kept, fewer work
-// groups at a time, 138.
+// 4096 x 131072 bf16, both: 473 us (4.5 TB/s of one read and one write); 467 when an exponent was one multiply-add (above).  With that, nothing
+// kept 529 us, without its second pass going backwards past the caches 483; all of the row kept, one work group of 1024 threads to a compute
+// unit, 680: nothing runs beside its sums.  4096 x 50021: 243 us (236 then, with nothing kept 283); 8192 x 10000, too short for it to
+// matter: 94 us (92 then, with 16 pieces kept, fewer work groups at a time, 138).
 template <class T, class R_, int THREADS, int V, bool LOSS, bool GRAD, bool REST> __global__ __launch_bounds__(THREADS, THREADS == 1024 && V == 0 ? 8 : 4) void distill_kernel(DistillArgs a) {
     using raw = typename T::raw;
     constexpr int N = Vec<T>::N, WAVES = THREADS / 64;
@@ -390,7 +391,8 @@ template <bool LOSS, bool GRAD> static void launch(he_ctx* ctx, const he_distill
         const uint64_t bytes = (uint64_t)p->vocab * dtype_bytes(p->dtype);
         // A row of at most one piece a lane by one wavefront, where several have only barriers more; up to four pieces a lane, with the four a
         // work group had otherwise, once there are rows for every wavefront slot to have one.  Loss and gradient in one call, one
-        // wavefront and four: 6171 x 56 bf16 14.6 and 25.9 us, 4000 x 1000 f32 16.9 and 22.2, 256 x 1000 8.7 and 8.0.
+        // wavefront and four: 6171 x 56 bf16 14.6 and 25.9 us, 4000 x 1000 f32 16.9 and 22.2, 256 x 1000 8.7 and 8.0.  (1024 lies between: four
+        // wavefronts to each of 256 compute units; it was not measured.)
         const bool many = p->rows >= 1024;
         if (p->vocab < (uint32_t)Vec<T>::N) go(integral_constant<int, 64>{}, integral_constant<int, 0>{}, Of<ShortRow<T>>{});
         else if constexpr (LOSS && GRAD) {

@@ -43,7 +43,8 @@ __device__ __forceinline__ v4i keep(v4i v, int left) {
 // there are few of them, one launch's latency), and the pieces on the way of 32 wavefronts to a compute unit keep memory busy.  A and
 // the scales come from the caches, A's pieces once for the NT tiles.  Pieces of 16 bytes go to lanes so that four lanes side by side read
 // 64 bytes of a row; any assignment of columns to lanes gives the same products as long as both operands have it.  Codes go through
-// the matrix instruction of f16, which adds in 32 bits: exact, and not what bounds it.
+// the matrix instruction of f16, which adds in 32 bits: exact, and not what bounds it.  Every wavefront asks for one block more than it
+// multiplies, whichever is the last.
 template <class T, int NT, int MT> __global__ __launch_bounds__(1024) void matmul_q8_few_kernel(GemmArgs a) {
     using raw = typename T::raw;
     constexpr int PITCH = 20;
@@ -147,7 +148,8 @@ template <class T, int NT, int MT> __global__ __launch_bounds__(1024) void matmu
 
 // With up to 32 rows of A: products whose W has less than 32 MiB, where the tiles below would need a second launch for the parts of the
 // sum's axis (16 x 1000 x 2048: 6.8 us, there 9.7; 16 x 10007 x 4096: 22.6, there 13.4), and those of up to 4 rows with so many of W that
-// the tiles come in one round and a third (1 x 131072 x 4096: 107 us, there 131; with 16 rows 148, there 134).
+// the tiles come in one round and a third (1 x 131072 x 4096: 107 us, there 131; with 16 rows 148, there 134).  4 rows and 98304 were drawn
+// between these and 1 x 32768 x 4096, not measured; other W whose tiles end in a part of a round go by the same line.
 static bool few_rows(uint32_t m, uint32_t n, uint32_t k) { return m <= 32 && ((uint64_t)n * k < 1u << 25 || (m <= 4 && n > 98304)); }
 
 template <class T, int NT, int MT> static hipError_t launch_few(const GemmArgs& a, hipStream_t stream) {
@@ -178,8 +180,8 @@ template <class T> static hipError_t run_few(const GemmArgs& a, hipStream_t stre
 // sixteen of them, two rows of 128 bytes to a line of all 64 banks, cover every bank once.  The fills are spread over the first half of a
 // block's squares: all at once they wait for the cache's 64 bytes a cycle and hold the wavefront's matrix instructions back.
 //
-// 8192 x 32768 x 4096 to bf16 1.03 to 1.07 ms by card (2130 to 2060 TFLOP/s), exact sums to f32 2.07 ms (1060).  With no fills at all (on what lies there)
-// the first takes 0.91 ms; the matrix instructions alone are 45% of its cycles, the multiply-adds 30%, and of the two kinds about half can
+// 8192 x 32768 x 4096 to bf16 1.03 to 1.07 ms by card (2130 to 2060 TFLOP/s), exact sums to f32 2.07 to 2.12 ms (1060).  With no fills at all (on what lies there)
+// the first takes 0.91 ms; matrix instructions fill 52% of its cycles and the multiply-adds 26% (counted), and of the two kinds about half can
 // run at a time (a pair of the first and 16 of the second take 172 cycles, not 130, with two wavefronts to a unit).  So a square's
 // multiply-adds stand between the next one's two instructions: with them behind its own, 1.09 ms, and 777 x 10007 x 2040 38.5 us, not
 // 35.9.  A third buffer does not fit beside the largest tile, and beside the smaller ones it takes the room of a second work group, which
@@ -406,7 +408,8 @@ template <class T, bool FAST, int WN, int WM, int TN, int TM> static hipError_t 
 
 // How the other products are cut: rows of W and of A to a tile, parts of the sum's axis.  Tiles of 256 x 256 read least
 // and run fastest once there are enough of them for the 256 compute units; below, smaller ones, of which two or three share a unit, and
-// where these do not fill the card either, the sum's axis in parts of at least 4 blocks, joined by a second kernel.
+// where these do not fill the card either, the sum's axis in parts of at least 4 blocks, joined by a second kernel.  Exact sums go by the same
+// counts, though their largest tile has 128 rows of W: twice as many as the rule counts.
 struct Cut {
     uint32_t bn, bm, parts, per;
 };

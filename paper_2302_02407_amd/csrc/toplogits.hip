@@ -118,7 +118,7 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
 // summed anew from differences.  An element of -infinity can only be among the first k if its index is below k: of the first k
 // elements at most as many are larger as there are larger ones at all.
 //
-// 2048 x 131072 bf16, k = 64: 144 us (3.7 TB/s), 90% of its cycles vector instructions: about 16 for an element, of which 8 are the sum's (one
+// 2048 x 131072 bf16, k = 64: 144 us (3.7 TB/s), 88% of its cycles vector instructions: about 17 for an element, of which 8 are the sum's (one
 // exponential among them) and the rest maxima, thresholds and what is set aside.  As ten passes of a digit it took 3.1 ms.
 template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void top_logits_kernel(TopArgs a) {
     using raw = typename T::raw;
@@ -267,8 +267,11 @@ extern "C" int32_t he_top_logits(he_ctx* ctx, const he_top_plan* p) {
     const TopArgs a = {p->d_z, p->d_values, p->d_index, p->d_rest, p->ld_z, p->vocab, p->k, p->tau};
     with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        // Rows of at most a piece a lane go to one wavefront (4000 x 500 bf16, k = 20: 15 us, by four 83; 3090 x 48: 6.7 and 14), unless most of a
-        // row's elements are candidates, which four put in order sooner (256 x 500, k = 100: 21 us, by one 62).
+        // Rows of at most a piece a lane go to one wavefront (4000 x 500 bf16, k = 20: 15 us, by four 83; 3090 x 48, k of a few: 6.7 and 14), unless most of a
+        // row's elements are candidates, which four put in order sooner (256 x 500, k = 100: 21 us, by one 62).  Slow among those of four:
+        // elements of 16 bits, 513 to 1023 of them, and k above some 30.  One wavefront's lanes are full then, so a threshold takes k maxima one
+        // after another (256 x 1000, k = 64: 68 us); above 64 none is taken, all of the row stays, more than there is room for, and it is read
+        // ten times (k = 128: 64 us; f32, which there is room for: 24).
         const uint64_t bytes = (uint64_t)p->vocab * es;
         if (bytes > 32768) top_logits_kernel<T, 1024><<<p->rows, 1024, 0, ctx->stream>>>(a);
         else if (bytes <= 1024 && (p->k <= 32 || p->vocab <= 128)) top_logits_kernel<T, 64><<<p->rows, 64, 0, ctx->stream>>>(a);
