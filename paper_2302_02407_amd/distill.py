@@ -102,4 +102,5 @@ def distill_loss(ctx, z, answers, tau, labels=None, alpha=0.0):
     losses take them: a negative one is padding, one beyond the vocabulary is not there."""
     if labels is not None and labels.dtype == torch.int64:
         labels = labels.clamp(-1, z.shape[-1]).to(torch.int32)
-    return _DistillLoss.apply(z if z.stride(-1) == 1 else z.contiguous(), ctx, answers, tau, labels, alpha)
+    own = z.dim() == 2 and z.stride(1) == 1 and (z.shape[0] <= 1 or z.stride(0) >= z.shape[1])       # rows in one piece that share nothing
+    return _DistillLoss.apply(z if own else z.contiguous(), ctx, answers, tau, labels, alpha)

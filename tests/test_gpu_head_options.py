@@ -73,3 +73,24 @@ def test_one_row_of_any_pitch(ctx):
     values, index = torch.zeros((1, 3), device="cuda"), torch.zeros((1, 3), dtype=torch.int32, device="cuda")
     ctx.he_top_logits(z.as_strided((1, 700), (1 << 29, 1)), 1.0, values, index)
     assert torch.equal(index.cpu().long(), R.top(z[:1].cpu(), 3, 1.0)[1])
+
+
+def test_logits_that_are_not_rows_of_their_own(ctx):
+    """One student's row against several answers, and columns of a larger matrix: the gradient goes where the logits come from."""
+    from paper_2302_02407_amd.distill import Answers, distill_loss
+    g, rows, vocab, tau = torch.Generator().manual_seed(4), 7, 120, 2.0
+    values, index, rest = R.top(torch.randn((rows, vocab), generator=g), 5, tau)
+    answers = Answers(values.float().cuda(), index.to(torch.int32).cuda(), rest.float().cuda())
+    for shape, view in (((vocab,), lambda t: t.expand(rows, vocab)), ((1, vocab), lambda t: t.expand(rows, vocab)), ((rows, 2 * vocab), lambda t: t[:, ::2]),
+                        ((vocab, rows), lambda t: t.T), ((rows, vocab + 3), lambda t: t[:, 3:]), ((rows * vocab // 2 + vocab,), lambda t: t.as_strided((rows, vocab), (vocab // 2, 1)))):
+        z = torch.randn(shape, generator=g)
+        want, dz, size = R.distill(view(z), *(t.cpu() for t in answers), tau, None, 0.0)
+        ref = z.double().requires_grad_()
+        view(ref).backward(dz)
+        most = z.double().requires_grad_()
+        view(most).backward(size)
+        d = z.cuda().requires_grad_()
+        loss = distill_loss(ctx, view(d), answers, tau)
+        loss.sum().backward()
+        assert ((loss.detach().cpu().double() - want).abs() <= 1e-5 * tau ** 2 * (2 + want.abs())).all()
+        assert ((d.grad.cpu().double() - ref.grad).abs() <= 2e-5 * most.grad + 1e-38).all()
