@@ -394,7 +394,7 @@ int32_t he_rmsnorm_q8(he_ctx* ctx, const he_rmsnorm_plan* plan);
 
 /* out[m][n] = sum over k of A[m][k] * W[n][k], values being codes times scales: A has a scale for each row and 128 columns, W one
  * for each 128 rows and 128 columns ([ceil(N/128)][ceil(K/128)]).  out must not overlap an operand.  The products of a block are
- * exact and summed in 32 bits. */
+ * exact and summed in 32 bits, and the sum is taken times the product of its two scales, itself a number of 32 bits. */
 typedef struct {
     uint32_t m, n, k;              /* k from 1 to 2^20; m, n <= 2^20, m * n <= 2^33; ld_a, ld_w <= 2^23 */
     int32_t out_dtype;
