@@ -113,7 +113,7 @@ template <class T, int WAVES> __device__ __forceinline__ void named_entries(cons
 // GRAD alone takes the sums from the statistics.  16 bytes a lane at a time, sums against each lane's running reference.  Loss and gradient
 // together need the row twice: V pieces a lane stay in registers between (16 of them: 64 of 128 registers; with 512 threads a work group 128
 // KiB, two work groups to a compute unit, one of which reads or writes while the other adds up), what is beyond is read again, backwards,
-// so that the caches still have some of it (of the half that is read again a tenth in the die's own, counted), and the gradient of long rows
+// so that the caches still have some of it (of the half that is read again a fifth in the die's own, counted), and the gradient of long rows
 // is written past them.
 //
 // 4096 x 131072 bf16, both: 473 us (4.5 TB/s of one read and one write); 467 when an exponent was one multiply-add (above).  With that, nothing

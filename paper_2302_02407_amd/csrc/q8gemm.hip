@@ -181,7 +181,7 @@ template <class T> static hipError_t run_few(const GemmArgs& a, hipStream_t stre
 // block's squares: all at once they wait for the cache's 64 bytes a cycle and hold the wavefront's matrix instructions back.
 //
 // 8192 x 32768 x 4096 to bf16 1.03 to 1.07 ms by card (2130 to 2060 TFLOP/s), exact sums to f32 2.07 to 2.12 ms (1060).  With no fills at all (on what lies there)
-// the first takes 0.91 ms; matrix instructions fill 52% of its cycles and the multiply-adds 26% (counted), and of the two kinds about half can
+// the first takes 0.91 ms; matrix instructions fill 51% of its cycles and the multiply-adds 26% (counted), and of the two kinds about half can
 // run at a time (a pair of the first and 16 of the second take 172 cycles, not 130, with two wavefronts to a unit).  So a square's
 // multiply-adds stand between the next one's two instructions: with them behind its own, 1.09 ms, and 777 x 10007 x 2040 38.5 us, not
 // 35.9.  A third buffer does not fit beside the largest tile, and beside the smaller ones it takes the room of a second work group, which
