@@ -118,7 +118,7 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
 // summed anew from differences.  An element of -infinity can only be among the first k if its index is below k: of the first k
 // elements at most as many are larger as there are larger ones at all.
 //
-// 2048 x 131072 bf16, k = 64: 144 us (3.7 TB/s), 88% of its cycles vector instructions: about 17 for an element, of which 8 are the sum's (one
+// 2048 x 131072 bf16, k = 64: 144 us (3.7 TB/s), 87% of its cycles vector instructions: about 17 for an element, of which 8 are the sum's (one
 // exponential among them) and the rest maxima, thresholds and what is set aside.  As ten passes of a digit it took 3.1 ms.
 template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void top_logits_kernel(TopArgs a) {
     using raw = typename T::raw;
