@@ -469,6 +469,182 @@ typedef struct {
 int32_t he_distill_loss(he_ctx* ctx, const he_distill_plan* plan);
 int32_t he_distill_grad(he_ctx* ctx, const he_distill_plan* plan);
 
+/* ---- Plaintext side: a training step around that loss.
+ *
+ * What a network of low-degree activations, or its teacher, needs beside the loss while it is trained in the clear: layer norm, the
+ * polynomial activation and what a linear layer keeps for its weight's gradient, both kept in 8 bits, and log probabilities of
+ * given tokens; each with its gradient.  Elements, rows and alignment as above, rounding too; a parameter is a dense vector.
+ *
+ *  - Scratch memory: these calls do not use the context's workspace.  Where a call needs room between its launches the caller gives
+ *    it in the plan (d_work, aligned to 16 bytes, at least what the he_work_* query of the same plan says; nothing of it has to be set,
+ *    nothing in it is kept), so that calls captured in graphs hold memory of their own: two graphs that may run at the same time need
+ *    two of them, and a graph needs its own as long as it is replayed.  Queries read sizes and types, no pointers but whether
+ *    optional outputs are there, and touch no GPU.
+ *  - All sums are taken in a fixed order: the same call gives the same bits.
+ *  - A context's calls go to the GPU and stream that were given at its creation, whatever the current device is.
+ *  - Rows kept in 8 bits: e4m3 codes, and for each 128 columns (the last of what is left) one byte b: a value is its code times
+ *    2^(b-127).  2^(b-127) is the smallest power from 2^-110 on at which the block's largest value is at most 448; values are
+ *    divided by it, exactly, and rounded to nearest even.  So a value is a number of 16 bits (bfloat16), exactly, and off by at most
+ *    2^-4 of itself or 2^-10 of the power.  A block that holds an infinity or a NaN has b = 255 and codes 0x7f: all its values are NaN.
+ *    Rows of codes start at multiples of 16 bytes (pointer and ld), and the columns up to the next multiple of 16 are there, as above. */
+
+/* h = x + residual, rounded to dtype (without a residual h = x); mean and variance v of h's row, y = (h - mean) / sqrt(v + eps) * weight +
+ * bias.  Where v + eps is below 2^-120, 0 too, 1 / sqrt(v + eps) counts as 0.  d_stats, if given, receives for each row the mean as a
+ * number of 32 bits, what that lacks, 1 / sqrt(v + eps), and 0: what he_layernorm_grad reads.  d_residual and d_sum (h): both or
+ * neither; d_weight and d_bias may be NULL (ones; zeros).  d_sum may be d_x or d_residual, d_y may be d_x or d_residual, with the same ld; no output
+ * may overlap an input otherwise, or another output. */
+typedef struct {
+    uint32_t rows, dim;            /* dim from 1 to 65536 */
+    int32_t dtype;                 /* of x, residual, sum and y */
+    int32_t param_dtype;           /* of weight and bias: dtype, or HE_F32 */
+    float eps;                     /* >= 0 */
+    const void* d_x;
+    uint64_t ld_x;
+    const void* d_residual;
+    uint64_t ld_residual;
+    const void* d_weight;          /* [dim] */
+    const void* d_bias;            /* [dim] */
+    void* d_sum;
+    uint64_t ld_sum;
+    void* d_y;
+    uint64_t ld_y;
+    float* d_stats;                /* [rows][4], or NULL */
+} he_layernorm_plan;
+int32_t he_layernorm(he_ctx* ctx, const he_layernorm_plan* plan);
+
+/* From the gradient dy by y, with n = (h - mean) / sqrt(v + eps) and g = dy * weight:
+ *   dx = (g - mean(g) - n * mean(g n)) / sqrt(v + eps) + dsum        (by x and by the residual alike)
+ *   dweight = sum over rows of dy * n,   dbias = sum over rows of dy.
+ * dsum, the gradient that comes down to h itself, may be NULL (none); so may d_dweight and d_dbias (not wanted).  With no rows dweight and
+ * dbias are 0.  d_dx may be d_dy or d_dsum with the same ld; no output may overlap an input otherwise, another output or d_work. */
+typedef struct {
+    uint32_t rows, dim;
+    int32_t dtype;                 /* of h, dy, dsum and dx */
+    int32_t param_dtype;           /* of weight, dweight and dbias */
+    const void* d_h;               /* x, or where there was a residual the sum */
+    uint64_t ld_h;
+    const float* d_stats;          /* [rows][4] */
+    const void* d_dy;
+    uint64_t ld_dy;
+    const void* d_weight;
+    const void* d_dsum;
+    uint64_t ld_dsum;
+    void* d_dx;
+    uint64_t ld_dx;
+    void* d_dweight;
+    void* d_dbias;
+    void* d_work;
+    uint64_t work_bytes;
+} he_layernorm_grad_plan;
+int32_t he_layernorm_grad(he_ctx* ctx, const he_layernorm_grad_plan* plan);
+int32_t he_work_layernorm_grad(const he_ctx* ctx, const he_layernorm_grad_plan* plan, uint64_t* h_bytes);
+
+/* y = sum over i < n_coefs of coefs[i] * u^i, and u kept in 8 bits.  Without d_y (and then n_coefs = 0) u is kept and no more: what a
+ * linear layer does with its input.  d_y may be d_u with the same ld. */
+#define HE_POLY_MAX 9
+typedef struct {
+    uint32_t rows, dim, n_coefs;   /* dim from 1 to 65536, n_coefs <= HE_POLY_MAX */
+    int32_t dtype;                 /* of u and y */
+    const void* d_u;
+    uint64_t ld_u;
+    const float* d_coefs;          /* [n_coefs] */
+    void* d_y;
+    uint64_t ld_y;
+    uint8_t* d_codes;
+    uint64_t ld_codes;
+    uint8_t* d_exponents;          /* ceil(dim/128) a row */
+    uint64_t ld_exponents;
+} he_poly_plan;
+int32_t he_poly_q8(he_ctx* ctx, const he_poly_plan* plan);
+
+/* From the gradient dy by y, at the values v that are kept: du = dy * sum of i coefs[i] v^(i-1), dcoefs[i] = sum over all elements of dy * v^i
+ * (may be NULL; 0 where there are no rows; its sums are held in 64 bits across pieces of a few dozen elements).  d_du may be d_dy with the same ld. */
+typedef struct {
+    uint32_t rows, dim, n_coefs;   /* n_coefs from 1 to HE_POLY_MAX */
+    int32_t dtype;                 /* of dy and du */
+    const uint8_t* d_codes;
+    uint64_t ld_codes;
+    const uint8_t* d_exponents;
+    uint64_t ld_exponents;
+    const float* d_coefs;
+    const void* d_dy;
+    uint64_t ld_dy;
+    void* d_du;
+    uint64_t ld_du;
+    float* d_dcoefs;
+    void* d_work;
+    uint64_t work_bytes;
+} he_poly_grad_plan;
+int32_t he_poly_grad_q8(he_ctx* ctx, const he_poly_grad_plan* plan);
+int32_t he_work_poly_grad_q8(const he_ctx* ctx, const he_poly_grad_plan* plan, uint64_t* h_bytes);
+
+/* dw[n][k] = sum over m of dy[m][n] * v[m][k], v the values that are kept; with `accumulate` that is added to what dw holds.  Products are
+ * exact (dy is taken as the sum of as many bfloat16 numbers as its type needs: where that leaves 2^-126 behind, it is lost) and summed
+ * in 32 bits.  With m = 0 dw becomes 0, or stays.  dw must not overlap an operand or d_work. */
+typedef struct {
+    uint32_t m, n, k;              /* m up to 2^21, n and k up to 2^17 */
+    int32_t dtype;                 /* of dy */
+    int32_t out_dtype;             /* of dw */
+    uint32_t accumulate;
+    const void* d_dy;
+    uint64_t ld_dy;
+    const uint8_t* d_codes;
+    uint64_t ld_codes;
+    const uint8_t* d_exponents;
+    uint64_t ld_exponents;
+    void* d_dw;
+    uint64_t ld_dw;
+    void* d_work;
+    uint64_t work_bytes;
+} he_weight_grad_plan;
+int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* plan);
+int32_t he_work_weight_grad_q8(const he_ctx* ctx, const he_weight_grad_plan* plan, uint64_t* h_bytes);
+
+/* Of every row of logits z, with p = softmax(z / tau):
+ *   d_logp      log p[token]; 0 where the token is not one of 0..vocab-1 (padding, or none asked for), -infinity where it has no probability
+ *   d_entropy   - sum p log p
+ *   d_values, d_index   log p and index of the k largest logits, in the order of he_top_logits
+ *   d_stats     the largest logit that counts, the sum of exp((z - that) / tau), the entropy, and 0: what he_token_logprobs_grad reads.
+ * Each may be NULL (d_tokens and d_logp: both or neither; d_values and d_index with k > 0, both or neither; at least one is there).  Which
+ * logits count as -infinity is as in he_top_logits.  A row of nothing else has log probabilities of -infinity, entropy 0 and a sum of 0.  A row that
+ * holds a NaN, or a logit from 2^126 min(1, tau) up, has no distribution: log probability, entropy and values are NaN, the order stands. */
+typedef struct {
+    uint32_t rows, vocab, k;       /* vocab from 1 to 2^20, k <= min(vocab, HE_TOP_MAX) */
+    int32_t dtype;
+    float tau;                     /* from 2^-60 to 2^60 */
+    const void* d_z;
+    uint64_t ld_z;
+    const int32_t* d_tokens;       /* [rows] */
+    float* d_logp;                 /* [rows] */
+    float* d_entropy;              /* [rows] */
+    float* d_values;               /* [rows][k] */
+    int32_t* d_index;              /* [rows][k] */
+    float* d_stats;                /* [rows][4] */
+    void* d_work;
+    uint64_t work_bytes;
+} he_logprobs_plan;
+int32_t he_token_logprobs(he_ctx* ctx, const he_logprobs_plan* plan);
+int32_t he_work_token_logprobs(const he_ctx* ctx, const he_logprobs_plan* plan, uint64_t* h_bytes);
+
+/* grad = d_logp_weights[row] times the gradient of the row's log p[token] by z, plus d_entropy_weights[row] times that of its entropy:
+ *   (a ([i = token] - p_i) - b p_i (log p_i + entropy)) / tau.
+ * Either may be NULL (none); log probabilities need tokens.  A weight of 0, a token that is not there, and a row of a sum of 0 have no
+ * gradient, whatever the logits are; nor has a log probability of -infinity.  d_grad may be d_z with the same ld. */
+typedef struct {
+    uint32_t rows, vocab;
+    int32_t dtype;                 /* of z and of the gradient */
+    float tau;
+    const void* d_z;
+    uint64_t ld_z;
+    const int32_t* d_tokens;       /* [rows], or NULL */
+    const float* d_stats;          /* [rows][4] */
+    const float* d_logp_weights;   /* [rows], or NULL */
+    const float* d_entropy_weights;/* [rows], or NULL */
+    void* d_grad;
+    uint64_t ld_grad;
+} he_logprobs_grad_plan;
+int32_t he_token_logprobs_grad(he_ctx* ctx, const he_logprobs_grad_plan* plan);
+
 #ifdef __cplusplus
 }
 #endif

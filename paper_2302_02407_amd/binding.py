@@ -22,6 +22,8 @@ EXPORTS = [
     "he_conjugate", "he_ptct_mac", "he_add", "he_addpt", "he_mulct", "he_affine", "he_rescale", "he_conv2d", "he_raconv",
     "he_probe_alu", "he_build_id", "he_rotate_sum", "he_ws_query_raconv", "he_ca_ra_block", "he_ws_query_ca_ra_block", "he_ras", "he_ws_bytes", "he_ws_reserve", "he_ws_query_rotate_batch", "he_ws_query_conv2d", "he_rescale_noalloc", "he_ptct_mac_rot",
     "he_rmsnorm_q8", "he_matmul_q8", "he_top_logits", "he_distill_loss", "he_distill_grad", "he_ws_query_matmul_q8",
+    "he_layernorm", "he_layernorm_grad", "he_work_layernorm_grad", "he_poly_q8", "he_poly_grad_q8", "he_work_poly_grad_q8",
+    "he_weight_grad_q8", "he_work_weight_grad_q8", "he_token_logprobs", "he_work_token_logprobs", "he_token_logprobs_grad",
 ]
 
 
@@ -67,6 +69,7 @@ class BlockPlan(C.Structure):
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # he_dtype
 _CODES = (torch.uint8, torch.float8_e4m3fn)
+_EXPONENTS = (torch.uint8, torch.float8_e8m0fnu)
 _F32 = (torch.float32,)
 
 
@@ -75,6 +78,13 @@ _RMSNORM = struct.Struct("@IIifPQPQPPQPQPQ")
 _MATMUL = struct.Struct("@IIIiIPQPQPQPQPQ")
 _TOP = struct.Struct("@IIIifPQPPP")
 _DISTILL = struct.Struct("@IIIiffPQPPPPPPPPQ")
+_LAYERNORM = struct.Struct("@IIiifPQPQPPPQPQP")
+_LAYERNORM_GRAD = struct.Struct("@IIiiPQPPQPPQPQPPPQ")
+_POLY = struct.Struct("@IIIiPQPPQPQPQ")
+_POLY_GRAD = struct.Struct("@IIIiPQPQPPQPQPPQ")
+_WEIGHT_GRAD = struct.Struct("@IIIiiIPQPQPQPQPQ")
+_LOGPROBS = struct.Struct("@IIIifPQPPPPPPPQ")
+_LOGPROBS_GRAD = struct.Struct("@IIifPQPPPPPQ")
 
 
 _lib = None
@@ -134,6 +144,17 @@ def load():
         "he_top_logits": [vp, C.c_char_p],
         "he_distill_loss": [vp, C.c_char_p],
         "he_distill_grad": [vp, C.c_char_p],
+        "he_layernorm": [vp, C.c_char_p],
+        "he_layernorm_grad": [vp, C.c_char_p],
+        "he_work_layernorm_grad": [vp, C.c_char_p, u64p],
+        "he_poly_q8": [vp, C.c_char_p],
+        "he_poly_grad_q8": [vp, C.c_char_p],
+        "he_work_poly_grad_q8": [vp, C.c_char_p, u64p],
+        "he_weight_grad_q8": [vp, C.c_char_p],
+        "he_work_weight_grad_q8": [vp, C.c_char_p, u64p],
+        "he_token_logprobs": [vp, C.c_char_p],
+        "he_work_token_logprobs": [vp, C.c_char_p, u64p],
+        "he_token_logprobs_grad": [vp, C.c_char_p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -213,6 +234,23 @@ def _plain(t, what):
     return d
 
 
+def _parameter(t, what, dim, dtypes):
+    """Pointer of a parameter's vector, or of its gradient; None is a null pointer."""
+    if t is None:
+        return 0
+    if t.dtype not in dtypes:
+        raise TypeError("%s must be %s, not %s" % (what, " or ".join(str(d) for d in dtypes), t.dtype))
+    return _dense(t, what, (dim,), t.dtype)
+
+
+def _param_dtype(x, *params):
+    """The he_dtype of parameters beside rows x, all of one type: 32 bits or the rows' own."""
+    given = {t.dtype for t in params if t is not None}
+    if len(given) > 1:
+        raise TypeError("parameters and their gradients must be of one type, not %s" % " and ".join(sorted(str(d) for d in given)))
+    return _DTYPE.get(given.pop(), -1) if given else _DTYPE[x.dtype]
+
+
 def _u32arr(xs):
     xs = [int(x) for x in xs]
     return (C.c_uint32 * max(1, len(xs)))(*xs), len(xs)
@@ -237,6 +275,7 @@ class HEContext:
         if rc != HE_OK:
             raise HEError(rc, self._lib.he_last_error(None).decode())
         self._h = h
+        self._at = self.stream.device.index
         self._keys = {}   # keeps registered key tensors alive
 
     @classmethod
@@ -608,4 +647,146 @@ class HEContext:
     def he_distill_grad(self, z, values, index, rest, tau, stats, row_weights, grad, labels=None, alpha=0.0):
         """row_weights times the gradient of the loss by z, from the statistics that he_distill_loss left."""
         self._ck(self._lib.he_distill_grad(self._h, self._distill_plan(z, values, index, rest, tau, labels, alpha, None, stats, row_weights, grad)))
+        return grad
+
+    # ---- plaintext side: a training step around that loss
+    def _here(self, *tensors):
+        """They lie on the context's GPU."""
+        for t in tensors:
+            if t is not None and t.get_device() != self._at:
+                raise ValueError("a tensor on %s, the context's calls run on %s" % (t.device, self.stream.device))
+
+    def _work(self, query, plan, work):
+        """Pointer and size of a call's scratch memory: the caller's, or some that the stream's later work may have again once the call's is done."""
+        if work is not None:
+            if not (work.is_cuda and work.is_contiguous()):
+                raise ValueError("work must be a contiguous CUDA tensor")
+            return work, work.data_ptr(), work.untyped_storage().nbytes() - work.storage_offset() * work.element_size()
+        n = self._work_bytes(query, plan)
+        if not n:
+            return None, 0, 0
+        with torch.cuda.stream(self.stream):
+            work = torch.empty(n, dtype=torch.uint8, device=self.stream.device)
+        return work, work.data_ptr(), n
+
+    def _work_bytes(self, query, plan):
+        v = C.c_uint64()
+        self._ck(query(self._h, plan, C.byref(v)))
+        return v.value
+
+    def he_layernorm(self, x, y, eps, weight=None, bias=None, residual=None, sum_out=None, stats=None):
+        """Layer norm of x, or of x + residual, which goes to sum_out; weight and bias [dim], of x's type or float32; stats [rows][4] for the gradients."""
+        rows, dim = _matrix(x, "x")
+        d, t = _plain(x, "x"), (x.dtype,)
+        self._here(x, y, weight, bias, residual, sum_out, stats)
+        dx, ldx = _rows(x, "x", rows, dim, t)
+        dr, ldr = _rows(residual, "residual", rows, dim, t) if residual is not None else (0, 0)
+        ds, lds = _rows(sum_out, "sum_out", rows, dim, t) if sum_out is not None else (0, 0)
+        dy, ldy = _rows(y, "y", rows, dim, t)
+        own = (x.dtype, torch.float32)
+        self._ck(self._lib.he_layernorm(self._h, _LAYERNORM.pack(rows, dim, d, _param_dtype(x, weight, bias), eps, dx, ldx, dr, ldr, _parameter(weight, "weight", dim, own),
+                                                                 _parameter(bias, "bias", dim, own), ds, lds, dy, ldy, _dense(stats, "stats", (rows, 4), torch.float32))))
+        return y
+
+    def he_layernorm_grad(self, h, stats, dy, dx, weight=None, dsum=None, dweight=None, dbias=None, work=None):
+        """dx from dy, the gradient by the normed rows, h being what was normed (x, or sum_out); dsum, the gradient that comes down to the sum itself, is
+        added; dweight, dbias [dim] receive sums over the rows.  work: scratch memory, he_work_layernorm_grad bytes (None: allocated)."""
+        rows, dim = _matrix(h, "h")
+        d, t, own = _plain(h, "h"), (h.dtype,), (h.dtype, torch.float32)
+        self._here(h, stats, dy, dx, weight, dsum, dweight, dbias, work)
+        dh, ldh = _rows(h, "h", rows, dim, t)
+        ddy, lddy = _rows(dy, "dy", rows, dim, t)
+        dds, ldds = _rows(dsum, "dsum", rows, dim, t) if dsum is not None else (0, 0)
+        ddx, lddx = _rows(dx, "dx", rows, dim, t)
+        head = (rows, dim, d, _param_dtype(h, weight, dweight, dbias), dh, ldh, _dense(stats, "stats", (rows, 4), torch.float32), ddy, lddy, _parameter(weight, "weight", dim, own),
+                dds, ldds, ddx, lddx, _parameter(dweight, "dweight", dim, own), _parameter(dbias, "dbias", dim, own))
+        keep, at, n = self._work(self._lib.he_work_layernorm_grad, _LAYERNORM_GRAD.pack(*head, 0, 0), work)
+        self._ck(self._lib.he_layernorm_grad(self._h, _LAYERNORM_GRAD.pack(*head, at, n)))
+        return dx
+
+    def he_work_layernorm_grad(self, rows, dim, dtype=torch.bfloat16):
+        """Bytes of scratch memory for sums over the rows."""
+        d = _DTYPE[dtype]
+        return self._work_bytes(self._lib.he_work_layernorm_grad, _LAYERNORM_GRAD.pack(rows, dim, d, d, *[0] * 10, 1, 1, 0, 0))
+
+    def he_poly_q8(self, u, codes, exponents, coefs=None, y=None):
+        """u kept in 8 bits: codes (uint8 or float8_e4m3fn), exponents [rows][ceil(dim/128)] (uint8 or float8_e8m0fnu); with float32 coefs [n] also
+        y = sum of coefs[i] u^i."""
+        rows, dim = _matrix(u, "u")
+        d, t = _plain(u, "u"), (u.dtype,)
+        self._here(u, codes, exponents, coefs, y)
+        du, ldu = _rows(u, "u", rows, dim, t)
+        dc, ldc = _codes(codes, "codes", rows, dim)
+        de, lde = _rows(exponents, "exponents", rows, -(-dim // 128), _EXPONENTS)
+        dy, ldy = _rows(y, "y", rows, dim, t) if y is not None else (0, 0)
+        n = coefs.numel() if coefs is not None else 0
+        self._ck(self._lib.he_poly_q8(self._h, _POLY.pack(rows, dim, n, d, du, ldu, _dense(coefs, "coefs", (n,), torch.float32), dy, ldy, dc, ldc, de, lde)))
+        return y
+
+    def he_poly_grad_q8(self, codes, exponents, coefs, dy, du, dcoefs=None, work=None):
+        """du = dy times the polynomial's slope at the values that are kept; dcoefs [n] receives sums over all elements.  work: scratch memory,
+        he_work_poly_grad_q8 bytes (None: allocated)."""
+        rows, dim = _matrix(dy, "dy")
+        d, t = _plain(dy, "dy"), (dy.dtype,)
+        self._here(codes, exponents, coefs, dy, du, dcoefs, work)
+        dc, ldc = _codes(codes, "codes", rows, dim)
+        de, lde = _rows(exponents, "exponents", rows, -(-dim // 128), _EXPONENTS)
+        ddy, lddy = _rows(dy, "dy", rows, dim, t)
+        ddu, lddu = _rows(du, "du", rows, dim, t)
+        n = coefs.numel()
+        head = (rows, dim, n, d, dc, ldc, de, lde, _dense(coefs, "coefs", (n,), torch.float32), ddy, lddy, ddu, lddu, _dense(dcoefs, "dcoefs", (n,), torch.float32))
+        keep, at, size = self._work(self._lib.he_work_poly_grad_q8, _POLY_GRAD.pack(*head, 0, 0), work)
+        self._ck(self._lib.he_poly_grad_q8(self._h, _POLY_GRAD.pack(*head, at, size)))
+        return du
+
+    def he_work_poly_grad_q8(self, rows, dim, n):
+        """Bytes of scratch memory for the gradient of n coefficients."""
+        return self._work_bytes(self._lib.he_work_poly_grad_q8, _POLY_GRAD.pack(rows, dim, n, 0, *[0] * 9, 1, 0, 0))
+
+    def he_weight_grad_q8(self, dy, codes, exponents, dw, accumulate=False, work=None):
+        """dw [n][k] = dy [m][n] transposed times the values that are kept [m][k]; accumulate: added to what dw holds.  work: scratch memory,
+        he_work_weight_grad_q8 bytes (None: allocated)."""
+        (m, n), (_, k) = _matrix(dy, "dy"), _matrix(codes, "codes")
+        _matrix(dw, "dw")
+        d, o = _plain(dy, "dy"), _plain(dw, "dw")
+        self._here(dy, codes, exponents, dw, work)
+        ddy, lddy = _rows(dy, "dy", m, n, _DTYPE)
+        dc, ldc = _codes(codes, "codes", m, k)
+        de, lde = _rows(exponents, "exponents", m, -(-k // 128), _EXPONENTS)
+        ddw, lddw = _rows(dw, "dw", n, k, _DTYPE)
+        head = (m, n, k, d, o, 1 if accumulate else 0, ddy, lddy, dc, ldc, de, lde, ddw, lddw)
+        keep, at, size = self._work(self._lib.he_work_weight_grad_q8, _WEIGHT_GRAD.pack(*head, 0, 0), work)
+        self._ck(self._lib.he_weight_grad_q8(self._h, _WEIGHT_GRAD.pack(*head, at, size)))
+        return dw
+
+    def he_work_weight_grad_q8(self, m, n, k, dtype=torch.bfloat16):
+        return self._work_bytes(self._lib.he_work_weight_grad_q8, _WEIGHT_GRAD.pack(m, n, k, _DTYPE[dtype], *[0] * 12))
+
+    def he_token_logprobs(self, z, tau=1.0, tokens=None, logp=None, entropy=None, values=None, index=None, stats=None, work=None):
+        """Of softmax(z / tau): logp [rows] of int32 tokens, entropy [rows], log probability and index [rows][k] of the k largest, and the stats [rows][4]
+        that the gradient reads; each if it is given.  work: scratch memory, he_work_token_logprobs bytes (None: allocated)."""
+        rows, vocab = _matrix(z, "z")
+        d, k = _plain(z, "z"), _matrix(values, "values")[1] if values is not None else 0
+        self._here(z, tokens, logp, entropy, values, index, stats, work)
+        dz, ldz = _rows(z, "z", rows, vocab, _DTYPE)
+        f32, one = torch.float32, (rows,)
+        head = (rows, vocab, k, d, tau, dz, ldz, _dense(tokens, "tokens", one, torch.int32), _dense(logp, "logp", one, f32), _dense(entropy, "entropy", one, f32),
+                _dense(values, "values", (rows, k), f32), _dense(index, "index", (rows, k), torch.int32), _dense(stats, "stats", (rows, 4), f32))
+        keep, at, n = self._work(self._lib.he_work_token_logprobs, _LOGPROBS.pack(*head, 0, 0), work)
+        self._ck(self._lib.he_token_logprobs(self._h, _LOGPROBS.pack(*head, at, n)))
+        return logp
+
+    def he_work_token_logprobs(self, rows, vocab, k, dtype=torch.bfloat16):
+        return self._work_bytes(self._lib.he_work_token_logprobs, _LOGPROBS.pack(rows, vocab, k, _DTYPE[dtype], 1.0, *[0] * 10))
+
+    def he_token_logprobs_grad(self, z, tau, stats, grad, tokens=None, logp_weights=None, entropy_weights=None):
+        """grad = logp_weights [rows] times the gradient of each row's log probability by z, plus entropy_weights [rows] times that of its entropy."""
+        rows, vocab = _matrix(z, "z")
+        d, f32, one = _plain(z, "z"), torch.float32, (rows,)
+        self._here(z, stats, grad, tokens, logp_weights, entropy_weights)
+        dz, ldz = _rows(z, "z", rows, vocab, _DTYPE)
+        dg, ldg = _rows(grad, "grad", rows, vocab, (z.dtype,))
+        self._ck(self._lib.he_token_logprobs_grad(self._h, _LOGPROBS_GRAD.pack(rows, vocab, d, tau, dz, ldz, _dense(tokens, "tokens", one, torch.int32),
+                                                                               _dense(stats, "stats", (rows, 4), f32), _dense(logp_weights, "logp_weights", one, f32),
+                                                                               _dense(entropy_weights, "entropy_weights", one, f32), dg, ldg)))
         return grad

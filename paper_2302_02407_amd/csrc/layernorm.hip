@@ -1,0 +1,276 @@
+// Layer norm with a residual addition before it, and its gradients.
+#include "plain.h"
+
+struct LnArgs {
+    const void *x, *res, *weight, *bias;
+    void *sum, *y;
+    float4* stats;
+    u64 ld_x, ld_res, ld_sum, ld_y;
+    uint32_t rows, dim;
+    float eps;
+};
+
+// 1 / sqrt(v), or 0 where that is nothing to divide by
+__device__ __forceinline__ float inverse_root(float v) { return v < 0x1p-120f ? 0.0f : 1.0f / sqrtf(v); }
+
+// ROW threads a row, each with V pieces of 8 elements, piece p of a row with thread p % ROW, which stay in registers: everything is read and
+// written once.  Rows of up to 1024 columns take a wavefront each, four to a work group; longer ones a work group.  The mean is a number of 32
+// bits and what that lacks, the sum of the differences from it: so a row far from 0 keeps its variance, whose own sum is of those
+// differences, and its gradient.
+template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void layernorm_kernel(LnArgs a) {
+    using raw = typename T::raw;
+    constexpr int GROUP = ROW < 256 ? 256 : ROW, WAVES = ROW / 64;
+    __shared__ float room[2 * (GROUP / 64)];
+    const u64 row = (u64)blockIdx.x * (GROUP / ROW) + threadIdx.x / ROW;
+    if (row >= a.rows) return;                            // ROW = 64: a whole wavefront, and no barrier follows
+    const uint32_t t = threadIdx.x % ROW, dim = a.dim;
+    const raw* x = (const raw*)a.x + row * a.ld_x;
+    const raw* res = (const raw*)a.res + row * a.ld_res;
+    float h[V][8], s = 0;
+#pragma unroll
+    for (int p = 0; p < V; p++) {
+        const uint32_t at = (p * ROW + t) * 8;
+        load8<T>(x, at, dim, h[p]);
+        if (RES) {
+            float more[8];
+            load8<T>(res, at, dim, more);
+            Eight<T> sum;
+#pragma unroll
+            for (int i = 0; i < 8; i++) more[i] += h[p][i];
+            sum.set(more);
+#pragma unroll
+            for (int i = 0; i < 8; i++) h[p][i] = sum[i];
+            store8<T>((raw*)a.sum + row * a.ld_sum, at, dim, h[p]);       // over x or the residual at most what this thread has read
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) s += h[p][i];
+        if (V >= 8) __builtin_amdgcn_sched_barrier(0);    // one piece's loads at a time: the numbers fill the registers
+    }
+    float mean = group_sum<WAVES>(s, room) / (float)dim, low, var;
+    auto spread = [&]() {                                 // what the mean lacks, and the variance
+        float d1 = 0, d2 = 0;
+#pragma unroll
+        for (int p = 0; p < V; p++) {
+            const int left = (int)dim - (int)((p * ROW + t) * 8);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float d = i < left ? h[p][i] - mean : 0.0f;
+                d1 += d;
+                d2 = fmaf(d, d, d2);
+            }
+        }
+        group_sum2<WAVES>(d1, d2, room);
+        low = d1 / (float)dim;
+        var = d2 / (float)dim - low * low;
+        var = var < 0.0f ? 0.0f : var;                    // a NaN stays one
+    };
+    spread();
+    float r = inverse_root(var + a.eps);
+    float4 stats = {mean, low, r, 0};
+    if (!(var < 0x1p126f)) {                              // squares, or the sum, that 32 bits do not hold: by a power of two
+        float most = 0;
+#pragma unroll
+        for (int p = 0; p < V; p++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(h[p][i]));
+        most = group_max<WAVES>(most, room);
+        if (most < INFINITY) {
+            const int e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
+            s = 0;
+#pragma unroll
+            for (int p = 0; p < V; p++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) s += h[p][i] = ldexpf(h[p][i], -e);
+            mean = group_sum<WAVES>(s, room) / (float)dim;
+            spread();
+            r = inverse_root(var + ldexpf(a.eps, -2 * e));
+            stats = {ldexpf(mean, e), ldexpf(low, e), ldexpf(r, -e), 0};
+        }
+    }
+    if (a.stats && t == 0) a.stats[row] = stats;
+#pragma unroll
+    for (int p = 0; p < V; p++) {
+        const uint32_t at = (p * ROW + t) * 8;
+        if (at >= dim) break;
+        if (V >= 8) __builtin_amdgcn_sched_barrier(0);
+        float w[8], b[8];
+        if (a.weight) load8<P>((const typename P::raw*)a.weight, at, dim, w);
+        if (a.bias) load8<P>((const typename P::raw*)a.bias, at, dim, b);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float n = (h[p][i] - mean - low) * r;
+            h[p][i] = fmaf(n, a.weight ? w[i] : 1.0f, a.bias ? b[i] : 0.0f);
+        }
+        store8<T>((raw*)a.y + row * a.ld_y, at, dim, h[p]);
+    }
+}
+
+template <class T, class P, bool RES> static void launch_layernorm(const LnArgs& a, hipStream_t stream) {
+    auto go = [&](auto row, auto v) {
+        constexpr int ROW = decltype(row)::value, GROUP = ROW < 256 ? 256 : ROW;
+        layernorm_kernel<T, P, RES, ROW, decltype(v)::value><<<(a.rows + GROUP / ROW - 1) / (GROUP / ROW), GROUP, 0, stream>>>(a);
+    };
+    using std::integral_constant;
+    if (a.dim <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (a.dim <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (a.dim <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 8192) go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 16384) go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 32768) go(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    else go(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+}
+
+// Calls f with the types of rows and parameters
+template <class F> static void with_types(int32_t dtype, int32_t param_dtype, F&& f) {
+    with_dtype(dtype, [&](auto t) {
+        if (param_dtype == HE_F32) f(t, f32_t{});
+        else f(t, t);
+    });
+}
+
+extern "C" int32_t he_layernorm(he_ctx* ctx, const he_layernorm_plan* p) {
+    return he_guard(ctx, "he_layernorm: host allocation failed", [&]() -> int32_t {
+    if (!ctx) return HE_ERR_BADARG;
+    HE_REFUSE(ctx, "he_layernorm", refuse_layernorm(p));
+    if (p->rows == 0) return HE_OK;
+    const OnDevice device(ctx);
+    HE_HIP(ctx, device.status);
+    const LnArgs a = {p->d_x, p->d_residual, p->d_weight, p->d_bias, p->d_sum, p->d_y, (float4*)p->d_stats, p->ld_x, p->ld_residual, p->ld_sum, p->ld_y, p->rows, p->dim, p->eps};
+    with_types(p->dtype, p->param_dtype, [&](auto t, auto w) {
+        if (p->d_residual) launch_layernorm<decltype(t), decltype(w), true>(a, ctx->stream);
+        else launch_layernorm<decltype(t), decltype(w), false>(a, ctx->stream);
+    });
+    HE_LAUNCHED(ctx);
+    return HE_OK;
+    });
+}
+
+// ---- gradients
+
+struct LnGradArgs {
+    const void *h, *dy, *dsum, *weight;
+    const float4* stats;
+    void* dx;
+    float* parts;
+    u64 ld_h, ld_dy, ld_dsum, ld_dx;
+    uint32_t rows, dim, n_parts;
+};
+
+// A row a work group, in two passes: its two means, then its gradient
+template <class T, class P> __global__ __launch_bounds__(256) void layernorm_dx_kernel(LnGradArgs a) {
+    using raw = typename T::raw;
+    __shared__ float room[8];
+    const u64 row = blockIdx.x;
+    const raw *h = (const raw*)a.h + row * a.ld_h, *dy = (const raw*)a.dy + row * a.ld_dy, *dsum = (const raw*)a.dsum + row * a.ld_dsum;
+    const typename P::raw* w = (const typename P::raw*)a.weight;
+    const float4 stats = a.stats[row];
+    auto piece = [&](uint32_t at, float* n, float* g) {
+        load8<T>(h, at, a.dim, n);
+        load8<T>(dy, at, a.dim, g);
+        float f[8];
+        if (w) load8<P>(w, at, a.dim, f);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            n[i] = (n[i] - stats.x - stats.y) * stats.z;
+            if (w) g[i] *= f[i];
+        }
+    };
+    float s1 = 0, s2 = 0;
+    for (uint32_t at = threadIdx.x * 8; at < a.dim; at += 2048) {
+        float n[8], g[8];
+        piece(at, n, g);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            s1 += g[i];                                   // 0 past the row's end
+            s2 = fmaf(g[i], n[i], s2);
+        }
+    }
+    group_sum2<4>(s1, s2, room);
+    s1 /= (float)a.dim;
+    s2 /= (float)a.dim;
+    for (uint32_t at = threadIdx.x * 8; at < a.dim; at += 2048) {
+        float n[8], g[8], more[8];
+        piece(at, n, g);
+        if (a.dsum) load8<T>(dsum, at, a.dim, more);
+#pragma unroll
+        for (int i = 0; i < 8; i++) g[i] = fmaf(stats.z, g[i] - s1 - n[i] * s2, a.dsum ? more[i] : 0.0f);
+        store8<T>((raw*)a.dx + row * a.ld_dx, at, a.dim, g);
+    }
+}
+
+// Sums over a part of the rows, 512 columns a work group: each wavefront every fourth row, their sums joined in order
+template <class T> __global__ __launch_bounds__(256) void layernorm_columns_kernel(LnGradArgs a) {
+    using raw = typename T::raw;
+    __shared__ float sums[4][2][512];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = blockIdx.x * 512 + lane * 8;
+    const uint32_t from = (u64)a.rows * blockIdx.y / a.n_parts, to = (u64)a.rows * (blockIdx.y + 1) / a.n_parts;
+    float dw[8] = {}, db[8] = {};
+    if (at < a.dim)
+        for (uint32_t row = from + wave; row < to; row += 4) {
+            float n[8], g[8];
+            load8<T>((const raw*)a.h + row * a.ld_h, at, a.dim, n);
+            load8<T>((const raw*)a.dy + row * a.ld_dy, at, a.dim, g);
+            const float4 stats = a.stats[row];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                dw[i] = fmaf(g[i], (n[i] - stats.x - stats.y) * stats.z, dw[i]);
+                db[i] += g[i];
+            }
+        }
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        sums[wave][0][lane * 8 + i] = dw[i];
+        sums[wave][1][lane * 8 + i] = db[i];
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < 1024; i += 256) {
+        const uint32_t which = i >> 9, c = i & 511, column = blockIdx.x * 512 + c;
+        if (column < a.dim) a.parts[((u64)blockIdx.y * 2 + which) * a.dim + column] = sums[0][which][c] + sums[1][which][c] + sums[2][which][c] + sums[3][which][c];
+    }
+}
+
+// The parts' sums, in order
+template <class P> __global__ __launch_bounds__(256) void layernorm_join_kernel(const float* parts, uint32_t n_parts, uint32_t dim, void* dweight, void* dbias) {
+    const uint32_t column = blockIdx.x * 256 + threadIdx.x;
+    if (column >= dim) return;
+    float dw = 0, db = 0;
+    for (uint32_t p = 0; p < n_parts; p++) {
+        dw += parts[(u64)p * 2 * dim + column];
+        db += parts[((u64)p * 2 + 1) * dim + column];
+    }
+    if (dweight) ((typename P::raw*)dweight)[column] = from_float<P>(dw);
+    if (dbias) ((typename P::raw*)dbias)[column] = from_float<P>(db);
+}
+
+extern "C" int32_t he_work_layernorm_grad(const he_ctx* ctx, const he_layernorm_grad_plan* p, uint64_t* h_bytes) {
+    return he_guard(ctx, "he_work_layernorm_grad: host allocation failed", [&]() -> int32_t {
+    if (!ctx || !h_bytes) return HE_ERR_BADARG;
+    HE_REFUSE(const_cast<he_ctx*>(ctx), "he_work_layernorm_grad", refuse_layernorm_grad(p, true));
+    *h_bytes = layernorm_grad_work(p);
+    return HE_OK;
+    });
+}
+
+extern "C" int32_t he_layernorm_grad(he_ctx* ctx, const he_layernorm_grad_plan* p) {
+    return he_guard(ctx, "he_layernorm_grad: host allocation failed", [&]() -> int32_t {
+    if (!ctx) return HE_ERR_BADARG;
+    HE_REFUSE(ctx, "he_layernorm_grad", refuse_layernorm_grad(p));
+    const bool sums = p->d_dweight || p->d_dbias;
+    const OnDevice device(ctx);
+    HE_HIP(ctx, device.status);
+    const LnGradArgs a = {p->d_h, p->d_dy, p->d_dsum, p->d_weight, (const float4*)p->d_stats, p->d_dx, (float*)p->d_work, p->ld_h, p->ld_dy, p->ld_dsum, p->ld_dx,
+                          p->rows, p->dim, p->rows ? layernorm_parts(p->rows, p->dim) : 0};
+    with_types(p->dtype, p->param_dtype, [&](auto t, auto w) {
+        using T = decltype(t);
+        using P = decltype(w);
+        if (sums) {                                       // before dx, which may lie on dy
+            if (a.rows) layernorm_columns_kernel<T><<<dim3((a.dim + 511) / 512, a.n_parts), 256, 0, ctx->stream>>>(a);
+            layernorm_join_kernel<P><<<(a.dim + 255) / 256, 256, 0, ctx->stream>>>(a.parts, a.n_parts, a.dim, p->d_dweight, p->d_dbias);
+        }
+        if (a.rows) layernorm_dx_kernel<T, P><<<a.rows, 256, 0, ctx->stream>>>(a);
+    });
+    HE_LAUNCHED(ctx);
+    return HE_OK;
+    });
+}

@@ -5,6 +5,7 @@
 
 #include <type_traits>
 
+#include "checks.h"
 #include "he_internal.h"
 
 #define HE_LOG2E 1.44269504088896340736f
@@ -84,6 +85,26 @@ template <int WAVES, class F> __device__ __forceinline__ float group_reduce(floa
 template <int WAVES> __device__ __forceinline__ float group_sum(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return a + b; }); }
 template <int WAVES> __device__ __forceinline__ float group_max(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return fmaxf(a, b); }); }
 
+// Two sums at once; `room`: 2 * WAVES floats
+template <int WAVES> __device__ __forceinline__ void group_sum2(float& x, float& y, float* room) {
+    x = wave_sum(x);
+    y = wave_sum(y);
+    if (WAVES == 1) return;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        room[threadIdx.x >> 6] = x;
+        room[WAVES + (threadIdx.x >> 6)] = y;
+    }
+    __syncthreads();
+    x = room[0];
+    y = room[WAVES];
+#pragma unroll
+    for (int i = 1; i < WAVES; i++) {
+        x += room[i];
+        y += room[WAVES + i];
+    }
+}
+
 // Sixteen bytes of a row, which may start anywhere its elements may
 template <class T> struct Vec {
     using raw = typename T::raw;
@@ -125,6 +146,48 @@ template <class T> struct Vec {
         else w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (uint32_t)r << 16 : (w[i / 2] & 0xffff0000u) | r;
     }
 };
+
+// Eight elements of a row, as numbers
+template <class T> struct Eight {
+    using raw = typename T::raw;
+    static constexpr int VECS = 8 / Vec<T>::N;
+    Vec<T> v[VECS];
+    __device__ __forceinline__ void load(const raw* p) {
+#pragma unroll
+        for (int i = 0; i < VECS; i++) v[i].load(p + i * Vec<T>::N);
+    }
+    __device__ __forceinline__ void store(raw* p) const {
+#pragma unroll
+        for (int i = 0; i < VECS; i++) v[i].store(p + i * Vec<T>::N);
+    }
+    __device__ __forceinline__ float operator[](int i) const { return v[i / Vec<T>::N][i % Vec<T>::N]; }
+    __device__ __forceinline__ void set(const float* x) {
+#pragma unroll
+        for (int i = 0; i < VECS; i++) v[i].set(x + i * Vec<T>::N);
+    }
+};
+
+// Eight elements from `at` on of a row of n, zeros for those that are not there; and those of them that are there written
+template <class T> __device__ __forceinline__ void load8(const typename T::raw* p, uint32_t at, uint32_t n, float* x) {
+    if (at + 8 <= n) {
+        Eight<T> v;
+        v.load(p + at);
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = v[i];
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = at + i < n ? to_float<T>(p[at + i]) : 0.0f;
+}
+template <class T> __device__ __forceinline__ void store8(typename T::raw* p, uint32_t at, uint32_t n, const float* x) {
+    if (at + 8 <= n) {
+        Eight<T> v;
+        v.set(x);
+        v.store(p + at);
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (at + i < n) p[at + i] = from_float<T>(x[i]);
+}
 
 // A row of n >= N elements in pieces of 16 bytes, without a branch on the way to a load: piece v starts at base(v), the last one, and any
 // past it, where it still lies in the row.  The elements of those that belong to the piece before, or to nothing, are those below
@@ -189,21 +252,31 @@ template <class F> static inline void with_dtype(int32_t dtype, F&& f) {
     else if (dtype == HE_BF16) f(bf16_t{});
     else f(f16_t{});
 }
-static inline uint32_t dtype_bytes(int32_t dtype) { return dtype == HE_F32 ? 4 : 2; }
-static inline bool dtype_known(int32_t dtype) { return dtype == HE_F32 || dtype == HE_BF16 || dtype == HE_F16; }
-// Whether [a, a + na) and [b, b + nb) share a byte
-static inline bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-    return a && b && na && nb && (const char*)a < (const char*)b + nb && (const char*)b < (const char*)a + na;
-}
-// Bytes from the first to past the last element of `rows` rows of `cols` elements, `ld` elements apart
-static inline uint64_t span(uint64_t rows, uint64_t cols, uint64_t ld, uint64_t size) { return rows && cols ? ((rows - 1) * ld + cols) * size : 0; }
-// Rows of `cols` elements, ld apart: they do not overlap, and no offset of HE_ROWS_MAX of them leaves 64 bits
-static inline bool ld_fits(uint64_t ld, uint64_t cols) { return ld >= cols && ld <= (1u << 28); }
-// Temperatures of which log2(e) / tau and tau^2 are numbers, and at which a masked logit, from 2^126 on, is far from any other
-static inline bool tau_fits(float tau) { return tau >= 0x1p-60f && tau <= 0x1p60f; }
-#define HE_ROWS_MAX (1u << 21)     // a work group of at most 1024 threads a row: a launch's threads stay below 2^32
-#define HE_VOCAB_MAX (1u << 20)
 // Kernel arguments have been checked; what can still fail is the launch
 #define HE_LAUNCHED(ctx) HE_HIP(ctx, hipGetLastError())
+
+// The context's GPU is the current one while this lives
+class OnDevice {
+    int was_ = -1;
+
+public:
+    hipError_t status;
+    explicit OnDevice(const he_ctx* ctx) {
+        int now = -1;
+        status = hipGetDevice(&now);
+        if (status != hipSuccess || now == ctx->device) return;
+        status = hipSetDevice(ctx->device);
+        if (status == hipSuccess) was_ = now;
+    }
+    ~OnDevice() {
+        if (was_ >= 0) (void)hipSetDevice(was_);
+    }
+    OnDevice(const OnDevice&) = delete;
+};
+// What an operator with a check of its plan (checks.h) does first
+#define HE_REFUSE(ctx, name, why)                                                    \
+    do {                                                                             \
+        if (const char* why__ = (why)) return he_fail(ctx, HE_ERR_BADARG, "%s: %s", name, why__); \
+    } while (0)
 
 #endif

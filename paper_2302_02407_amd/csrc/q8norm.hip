@@ -17,26 +17,6 @@ struct NormArgs {
 // |y| as an integer: ordered like the numbers, infinity above them and NaN above that, so that a maximum keeps both
 __device__ __forceinline__ int32_t magnitude(float y) { return __builtin_bit_cast(int32_t, y) & 0x7fffffff; }
 
-// Eight elements of a row, as numbers
-template <class T> struct Eight {
-    using raw = typename T::raw;
-    static constexpr int VECS = 8 / Vec<T>::N;
-    Vec<T> v[VECS];
-    __device__ __forceinline__ void load(const raw* p) {
-#pragma unroll
-        for (int i = 0; i < VECS; i++) v[i].load(p + i * Vec<T>::N);
-    }
-    __device__ __forceinline__ void store(raw* p) const {
-#pragma unroll
-        for (int i = 0; i < VECS; i++) v[i].store(p + i * Vec<T>::N);
-    }
-    __device__ __forceinline__ float operator[](int i) const { return v[i / Vec<T>::N][i % Vec<T>::N]; }
-    __device__ __forceinline__ void set(const float* x) {
-#pragma unroll
-        for (int i = 0; i < VECS; i++) v[i].set(x + i * Vec<T>::N);
-    }
-};
-
 // ROW threads a row, each with V pieces of 8 elements, piece p of a row with thread p % ROW: what it adds stays in registers between the sum of
 // squares and the output, so that everything is read and written once.  16 lanes side by side hold a block of 128 columns and find its
 // largest element among themselves.  Rows of up to 1024 columns take a wavefront each, four to a work group; longer ones a work group.
