@@ -165,9 +165,12 @@ struct WeightCut {
 };
 static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k) {
     WeightCut c = {128, 128, 1, (m + 31) / 32};
-    const uint32_t steps = c.per, tiles = ((n + c.bn - 1) / c.bn) * ((k + c.bk - 1) / c.bk);
-    if (tiles < 512) {
-        uint32_t parts = (512 + tiles - 1) / tiles;
+    const uint32_t steps = c.per;
+    auto tiles = [&](uint32_t side) { return ((n + side - 1) / side) * ((k + side - 1) / side); };
+    if (tiles(256) >= 192) c.bn = c.bk = 256;
+    const uint32_t have = tiles(c.bn), want = c.bn == 256 ? 0 : 512;
+    if (have < want) {
+        uint32_t parts = (want + have - 1) / have;
         if (parts > steps / 8) parts = steps / 8;
         if (parts > 16) parts = 16;
         if (parts > 1) {

@@ -17,6 +17,7 @@ struct WeightArgs {
     uint32_t m, n, k;
     uint32_t per;              // steps of 32 rows a part takes
     u64 part;                  // elements from one part's sums to the next's
+    int32_t out_dtype;
     uint32_t accumulate;
 };
 
@@ -29,77 +30,232 @@ template <> struct Parts<f32_t> { static constexpr int N = 3; };
 __device__ __forceinline__ uint32_t upper(float& x) {
     const uint32_t b = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
     x = (b & 0x7fffffffu) == 0x7f800000u && x == x ? 0.0f : x - __builtin_bit_cast(float, b);
-    return b >> 16;
+    return b;
 }
 
-template <class T, class O> __global__ __launch_bounds__(256) void weight_grad_kernel(WeightArgs a) {
+// A work group owns BN columns of dy by BK columns of what is kept and goes through the rows 32 at a time.
+template <class T, int WN, int WK, int TN> struct WeightTile {
+    static constexpr int PARTS = Parts<T>::N, BN = WN * TN * 32, BK = WK * 128, THREADS = 64 * WN * WK;
+    static constexpr int PLANE = 32 * BN * 2, X = PARTS * PLANE, S = X + 32 * BK, BYTES = S + 32 * WK * 4, LDS = 2 * BYTES;
+    static constexpr int FY = 4 * BN / THREADS, FX = 2 * BK / THREADS;       // pieces of 8 elements of dy, of 16 codes, a thread
+};
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s* lds_v4s;
+typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
+
+// Both operands lie in LDS as they lie in memory, a row of m after another.  dy's fragments, eight rows of a column a lane, come by reads
+// that transpose: sixteen lanes name four rows of sixteen columns and each gets a column of four.  Those rows would lie in the same banks, so the
+// 16-byte piece p of row r lies at p ^ 4 (r & 3).  What is kept stays codes until it is used: a lane reads four columns of each of its eight rows,
+// turns each row's into bfloat16 by that row's power, and puts pairs of rows together: the fragments of four squares, in which lane l
+// holds columns 4 l .. 4 l + 3, so that results are written 16 bytes a lane.  Rows r and r + 8 go to the two halves of a wavefront
+// and are 128 bytes, half of the banks, apart.
+template <class T, int WN, int WK, int TN> __global__ __launch_bounds__(64 * WN * WK, 1) void weight_grad_kernel(WeightArgs a) {
     using raw = typename T::raw;
-    constexpr int PARTS = Parts<T>::N, PITCH = 80;               // 32 rows of m, 2 bytes each, and 16 more against bank conflicts
-    __shared__ __align__(16) uint8_t lds[(PARTS + 1) * 128 * PITCH];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 31, g = lane >> 5;
-    const uint32_t tiles_k = (a.k + 127) / 128, n0 = blockIdx.x / tiles_k * 128, k0 = blockIdx.x % tiles_k * 128;
-    const uint32_t steps = min((a.m + 31) / 32 - blockIdx.y * a.per, a.per), first = blockIdx.y * a.per * 32;
-    const raw* dy = (const raw*)a.dy;
-    v16f acc[2][2];
+    using G = WeightTile<T, WN, WK, TN>;
+    constexpr int PARTS = G::PARTS;
+    extern __shared__ __align__(1024) uint8_t lds[];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane & 31, g = lane >> 5;
+    const uint32_t wn = wave / WK, wk = wave % WK;
+    const uint32_t tiles_k = (a.k + G::BK - 1) / G::BK, n_own = blockIdx.x / tiles_k * G::BN, k0 = blockIdx.x % tiles_k * G::BK;
+    // the last tile begins earlier, so that all its columns are there; the rows of dw that another one has are left to that
+    const uint32_t n0 = a.n >= (uint32_t)G::BN ? min(n_own, a.n - G::BN) : 0;
+    const uint32_t first = blockIdx.y * a.per * 32, steps = min((a.m - first + 31) / 32, a.per);
+    const uint32_t codes_end = (a.k + 15) / 16 * 16, blocks = (a.k + 127) / 128;
+
+    struct Stage {
+        Eight<T> y[G::FY];
+        uint4 x[G::FX];
+        uint32_t e;
+    };
+    auto load = [&](uint32_t step, Stage& st) {
+        const uint32_t m0 = first + step * 32;
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+        for (int f = 0; f < G::FY; f++) {
+            const uint32_t i = f * G::THREADS + tid, r = i / (G::BN / 8), at = n0 + i % (G::BN / 8) * 8, row = min(m0 + r, a.m - 1);
+            const raw* from = (const raw*)a.dy + (u64)row * a.ld_dy;
+            if (a.n >= (uint32_t)G::BN) st.y[f].load(from + at);
+            else {                                        // columns past the end are anything that is no harm: their sums are not written
+                float x[8];
+                load8<T>(from, min(at, a.n - 1), a.n, x);
+                st.y[f].set(x);
+            }
+        }
 #pragma unroll
-        for (int j = 0; j < 2; j++)
+        for (int f = 0; f < G::FX; f++) {
+            const uint32_t i = f * G::THREADS + tid, r = i / (G::BK / 16), at = k0 + i % (G::BK / 16) * 16, row = min(m0 + r, a.m - 1);
+            st.x[f] = *(const uint4*)(a.codes + (u64)row * a.ld_codes + min(at, codes_end - 16));
+        }
+        if (tid < 32 * WK) {
+            const uint32_t row = min(m0 + tid % 32, a.m - 1), block = min(k0 / 128 + tid / 32, blocks - 1);
+            st.e = a.exponents[(u64)row * a.ld_exponents + block];
+        }
+    };
+    auto store = [&](uint32_t step, Stage& st) {
+        uint8_t* buf = lds + (step & 1) * G::BYTES;
+        const uint32_t left = a.m - first - step * 32;    // rows from the 32's first on
+        if (left < 32) {                                  // past the last row: zeros, in both operands
+#pragma unroll
+            for (int f = 0; f < G::FY; f++)
+                if ((f * G::THREADS + tid) / (G::BN / 8) >= left)
+#pragma unroll
+                    for (int v = 0; v < Eight<T>::VECS; v++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) st.y[f].v[v].w[i] = 0;
+#pragma unroll
+            for (int f = 0; f < G::FX; f++)
+                if ((f * G::THREADS + tid) / (G::BK / 16) >= left) st.x[f] = make_uint4(0, 0, 0, 0);
+            if (tid % 32 >= left) st.e = 127;
+        }
+#pragma unroll
+        for (int f = 0; f < G::FY; f++) {
+            const uint32_t i = f * G::THREADS + tid, r = i / (G::BN / 8), p = i % (G::BN / 8);
+            uint8_t* to = buf + r * (G::BN * 2) + ((p ^ (4 * (r & 3))) * 16);
+            if constexpr (PARTS == 1) *(uint4*)to = make_uint4(st.y[f].v[0].w[0], st.y[f].v[0].w[1], st.y[f].v[0].w[2], st.y[f].v[0].w[3]);
+            else {
+                uint32_t w[PARTS][4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    float x = st.y[f][2 * j], y = st.y[f][2 * j + 1];
+#pragma unroll
+                    for (int q = 0; q < PARTS; q++) {
+                        const uint32_t lo = upper(x), hi = upper(y);
+                        w[q][j] = lo >> 16 | hi;
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < PARTS; q++) *(uint4*)(to + q * G::PLANE) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < G::FX; f++) {
+            const uint32_t i = f * G::THREADS + tid, r = i / (G::BK / 16), c = i % (G::BK / 16) * 16;
+            *(uint4*)(buf + G::X + ((r * G::BK + c) ^ ((r >> 3 & 1) * 128))) = st.x[f];
+        }
+        if (tid < 32 * WK) ((uint32_t*)(buf + G::S))[tid] = st.e == 255 ? 0x7fc00000u : st.e << 23;
+    };
+
+    // half h of a step: sixteen rows, eight a lane
+    struct Half {
+        v4s y[PARTS][TN][2];
+        uint32_t x[8];
+        v4f s[2];
+    };
+    uint32_t y_at[TN], x_at[2];
+#pragma unroll
+    for (int q = 0; q < TN; q++)
+        y_at[q] = (8 * g + (lane & 15) / 4) * (G::BN * 2) + (((wn * TN * 4 + 4 * q + (lane >> 4 & 1) * 2 + (lane & 3) / 2) ^ 4 * ((lane & 15) / 4)) * 16) + (lane & 1) * 8;
+#pragma unroll
+    for (int i = 0; i < 2; i++) x_at[i] = G::X + (((8 * g + i) * G::BK + wk * 128 + 4 * l) ^ (g * 128));
+    auto read = [&](uint32_t step, int h, Half& f) {
+        const uint32_t buf = (step & 1) * G::BYTES;
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+#pragma unroll
+            for (int i = 0; i < 2; i++) f.x[2 * u + i] = *(const uint32_t*)(lds + buf + x_at[i] + (16 * h + 2 * u) * G::BK);
+#pragma unroll
+        for (int i = 0; i < 2; i++) f.s[i] = *(const v4f*)(lds + buf + G::S + (wk * 32 + 16 * h + 8 * g + 4 * i) * 4);
+#pragma unroll
+        for (int q = PARTS - 1; q >= 0; q--)
+#pragma unroll
+            for (int i = 0; i < TN; i++)
+#pragma unroll
+                for (int t = 0; t < 2; t++)
+                    f.y[q][i][t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)((lds_ptr)lds + buf + y_at[i] + (q * 32 + 16 * h + 4 * t) * (G::BN * 2)));
+    };
+    v16f acc[TN][4];
+#pragma unroll
+    for (int i = 0; i < TN; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0;
-    for (uint32_t s = 0; s < steps; s++) {
-        // eight rows of two columns a thread, each column's eight together
-        const uint32_t m0 = first + s * 32 + wave * 8;
-        __syncthreads();
+    auto multiply = [&](const Half& f) {
+        uint32_t c[8][2], x[4][4];
 #pragma unroll
-        for (int c = 0; c < 2; c++) {
-            const uint32_t col = 2 * lane + c, n = n0 + col, k = k0 + col;
-            uint16_t y[PARTS][8], x[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                float v = n < a.n && m0 + i < a.m ? to_float<T>(dy[(u64)(m0 + i) * a.ld_dy + n]) : 0.0f;
-#pragma unroll
-                for (int q = 0; q < PARTS; q++) y[q][i] = (uint16_t)upper(v);
-                float u = 0;
-                if (k < a.k && m0 + i < a.m) {
-                    const uint32_t byte = a.exponents[(u64)(m0 + i) * a.ld_exponents + k / 128], code = a.codes[(u64)(m0 + i) * a.ld_codes + k];
-                    u = __builtin_amdgcn_cvt_f32_fp8(code, 0) * __builtin_bit_cast(float, byte == 255 ? 0x7fc00000u : byte << 23);
-                }
-                x[i] = (uint16_t)(__builtin_bit_cast(uint32_t, u) >> 16);
-            }
-#pragma unroll
-            for (int q = 0; q < PARTS; q++) __builtin_memcpy(__builtin_assume_aligned(lds + (q * 128 + col) * PITCH + wave * 16, 16), y[q], 16);
-            __builtin_memcpy(__builtin_assume_aligned(lds + (PARTS * 128 + col) * PITCH + wave * 16, 16), x, 16);
+        for (int i = 0; i < 8; i++) {
+            const float s = f.s[i / 4][i % 4];
+            c[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.x[i], s, false));
+            c[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.x[i], s, true));
         }
-        __syncthreads();
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            v8b xf[2];
+        for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) xf[j] = *(const v8b*)(lds + (PARTS * 128 + (wave & 1) * 64 + j * 32 + l) * PITCH + (2 * h + g) * 16);
+            for (int u = 0; u < 4; u++) x[j][u] = __builtin_amdgcn_perm(c[2 * u + 1][j / 2], c[2 * u][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-            for (int q = PARTS - 1; q >= 0; q--)
+        for (int q = PARTS - 1; q >= 0; q--)
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    const v8b yf = *(const v8b*)(lds + (q * 128 + (wave >> 1) * 64 + i * 32 + l) * PITCH + (2 * h + g) * 16);
+            for (int i = 0; i < TN; i++) {
+                const v8b y = __builtin_bit_cast(v8b, __builtin_shufflevector(f.y[q][i][0], f.y[q][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                    for (int j = 0; j < 2; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yf, xf[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < 4; j++) {
+                    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, __builtin_bit_cast(v8b, u4{x[j][0], x[j][1], x[j][2], x[j][3]}), acc[i][j], 0, 0, 0);
                 }
+            }
+    };
+    // What a wavefront has written to LDS is there for the others, and what it has asked for has come
+    auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+    Stage st;
+    load(0, st);
+    store(0, st);
+    if (steps > 1) load(1, st);
+    meet();
+    if constexpr (PARTS < 3) {
+        // a half is read while the one before is multiplied, the first of a step right behind the barrier that its rows wait for
+        Half one, two;
+        read(0, 0, one);
+        for (uint32_t b = 0; b < steps; b++) {
+            read(b, 1, two);
+            multiply(one);
+            if (b + 1 < steps) store(b + 1, st);          // the other buffer: its last reads lie before the last barrier
+            if (b + 2 < steps) load(b + 2, st);
+            meet();
+            if (b + 1 < steps) read(b + 1, 0, one);
+            multiply(two);
+        }
+    } else {                                              // three matrix products to a half hide its reads; two halves' fragments do not fit the registers
+        Half half;
+        for (uint32_t b = 0; b < steps; b++) {
+            read(b, 0, half);
+            multiply(half);
+            if (b + 1 < steps) store(b + 1, st);
+            read(b, 1, half);
+            multiply(half);
+            if (b + 2 < steps) load(b + 2, st);
+            meet();
         }
     }
-    // element e of a square: row 8 (e / 4) + 4 g + e % 4, column l
-    typename O::raw* dw = (typename O::raw*)a.dw + blockIdx.y * a.part;
+    // element e of a square: row 8 (e / 4) + 4 g + e % 4, square j column 4 l + j
+    const uint32_t k = k0 + wk * 128 + 4 * l;
+    auto put = [&](auto o, u64 at, const float* x) {
+        using O = decltype(o);
+        typename O::raw *to = (typename O::raw*)a.dw + at, v[4];
+        if (k + 4 <= a.k) {
+            if (a.accumulate) __builtin_memcpy(v, to, sizeof v);
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+            for (int j = 0; j < 4; j++) v[j] = from_float<O>(a.accumulate ? to_float<O>(v[j]) + x[j] : x[j]);
+            __builtin_memcpy(to, v, sizeof v);
+        } else
 #pragma unroll
-        for (int j = 0; j < 2; j++)
+            for (int j = 0; j < 4; j++)
+                if (k + j < a.k) to[j] = from_float<O>(a.accumulate ? to_float<O>(to[j]) + x[j] : x[j]);
+    };
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const uint32_t n = n0 + (wave >> 1) * 64 + i * 32 + 8 * (e / 4) + 4 * g + e % 4, k = k0 + (wave & 1) * 64 + j * 32 + l;
-                if (n >= a.n || k >= a.k) continue;
-                typename O::raw* to = dw + n * a.ld_dw + k;
-                *to = from_float<O>(a.accumulate ? to_float<O>(*to) + acc[i][j][e] : acc[i][j][e]);
+    for (int i = 0; i < TN; i++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            const uint32_t n = n0 + (wn * TN + i) * 32 + 8 * (e / 4) + 4 * g + e % 4;
+            const float x[4] = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+            const u64 at = blockIdx.y * a.part + n * a.ld_dw + k;
+            if (n >= n_own && n < a.n && k < a.k) {
+                if (a.out_dtype == HE_F32) put(f32_t{}, at, x);
+                else if (a.out_dtype == HE_BF16) put(bf16_t{}, at, x);
+                else put(f16_t{}, at, x);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
 }
 
 // Sums the parts, in order
@@ -115,6 +271,15 @@ template <class O> __global__ __launch_bounds__(256) void weight_join_kernel(con
             typename O::raw* to = dw + blockIdx.y * ld_dw + i + e;
             *to = from_float<O>(accumulate ? to_float<O>(*to) + x[e] : x[e]);
         }
+}
+
+template <class T, int WN, int WK, int TN> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
+    using G = WeightTile<T, WN, WK, TN>;
+    const auto kernel = weight_grad_kernel<T, WN, WK, TN>;
+    const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+    if (ready != hipSuccess) return ready;
+    kernel<<<dim3(((a.n + G::BN - 1) / G::BN) * ((a.k + G::BK - 1) / G::BK), c.parts), G::THREADS, G::LDS, stream>>>(a);
+    return hipGetLastError();
 }
 
 extern "C" int32_t he_work_weight_grad_q8(const he_ctx* ctx, const he_weight_grad_plan* p, uint64_t* h_bytes) {
@@ -135,25 +300,25 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     HE_HIP(ctx, device.status);
     const WeightCut c = weight_cut(p->m, p->n, p->k);
     const bool joined = p->m == 0 || c.parts > 1;
-    WeightArgs a = {p->d_dy, p->d_codes, p->d_exponents, p->d_dw, p->ld_dy, p->ld_codes, p->ld_exponents, p->ld_dw, p->m, p->n, p->k, c.per, 0, p->accumulate};
+    WeightArgs a = {p->d_dy, p->d_codes, p->d_exponents, p->d_dw, p->ld_dy, p->ld_codes, p->ld_exponents, p->ld_dw, p->m, p->n, p->k, c.per, 0, p->out_dtype, p->accumulate};
     if (joined) {
         a.dw = p->d_work;
         a.ld_dw = weight_pitch(p->k);
         a.part = p->n * a.ld_dw;
+        a.out_dtype = HE_F32;
         a.accumulate = 0;
     }
-    const dim3 grid(((p->n + 127) / 128) * ((p->k + 127) / 128), c.parts);
-    with_dtype(p->out_dtype, [&](auto o) {
+    hipError_t err = hipSuccess;
+    if (p->m) with_dtype(p->dtype, [&](auto t) {
+        using T = decltype(t);
+        err = c.bn == 256 ? launch_weight_grad<T, 4, 2, 2>(a, c, ctx->stream) : launch_weight_grad<T, 2, 1, 2>(a, c, ctx->stream);
+    });
+    HE_HIP(ctx, err);
+    if (joined) with_dtype(p->out_dtype, [&](auto o) {
         using O = decltype(o);
-        if (p->m) with_dtype(p->dtype, [&](auto t) {
-            using T = decltype(t);
-            if (joined) weight_grad_kernel<T, f32_t><<<grid, 256, 0, ctx->stream>>>(a);
-            else weight_grad_kernel<T, O><<<grid, 256, 0, ctx->stream>>>(a);
-        });
-        if (joined)
-            for (uint32_t r = 0; r < p->n; r += 65535)    // a grid's second side
-                weight_join_kernel<O><<<dim3((p->k + 1023) / 1024, min(p->n - r, 65535u)), 256, 0, ctx->stream>>>(
-                    (const float*)p->d_work + r * a.ld_dw, p->m ? c.parts : 0, a.part, a.ld_dw, (typename O::raw*)p->d_dw + r * p->ld_dw, p->ld_dw, p->k, p->accumulate);
+        for (uint32_t r = 0; r < p->n; r += 65535)        // a grid's second side
+            weight_join_kernel<O><<<dim3((p->k + 1023) / 1024, min(p->n - r, 65535u)), 256, 0, ctx->stream>>>(
+                (const float*)p->d_work + r * a.ld_dw, p->m ? c.parts : 0, a.part, a.ld_dw, (typename O::raw*)p->d_dw + r * p->ld_dw, p->ld_dw, p->k, p->accumulate);
     });
     HE_LAUNCHED(ctx);
     return HE_OK;

@@ -71,6 +71,21 @@ def test_whole_numbers_are_exact(ctx, dtype, m, n, k):
     assert torch.equal(run(ctx, dy, codes, exponents, torch.float32).double(), want)
 
 
+@pytest.mark.parametrize("m,n,k", [(70, 4100, 2900), (33, 3585, 3590), (31, 250, 70000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_whole_numbers_of_large_gradients(ctx, dtype, m, n, k):
+    """Enough results for the largest tiles, the last of which begin earlier than where they are counted."""
+    g = T.rng(n)
+    dy, v = torch.randint(-100, 101, (m, n), generator=g).to(dtype), torch.randint(-8, 9, (m, k), generator=g).float()
+    codes, exponents = T.keep(v)
+    exponents[::3] += 1
+    kept = T.kept(codes, exponents).float()
+    want = dy.float().T @ kept                                            # whole numbers below 2^24: exact
+    assert torch.equal(run(ctx, dy, codes, exponents, torch.float32, 1, 1), want)
+    onto = torch.randint(-100, 101, (n, k), generator=g).float()
+    assert torch.equal(run(ctx, dy, codes, exponents, torch.float32, 0, 0, onto), want + onto)
+
+
 def test_numbers_of_all_sizes(ctx):
     """32 bits of dy count, far powers of what is kept too: one product a sum, which is added up from three parts of it, so off by at most 3 2^-24 of itself
     and by what is below the smallest normal numbers; what 32 bits do not hold is infinite."""
