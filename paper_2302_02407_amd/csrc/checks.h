@@ -167,7 +167,7 @@ static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k) {
     WeightCut c = {128, 128, 1, (m + 31) / 32};
     const uint32_t steps = c.per;
     auto tiles = [&](uint32_t side) { return ((n + side - 1) / side) * ((k + side - 1) / side); };
-    if (tiles(256) >= 192) c.bn = c.bk = 256;
+    if (n >= 256 && tiles(256) >= 192) c.bn = c.bk = 256;
     const uint32_t have = tiles(c.bn), want = c.bn == 256 ? 0 : 512;
     if (have < want) {
         uint32_t parts = (want + have - 1) / have;

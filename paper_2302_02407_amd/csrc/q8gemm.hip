@@ -205,18 +205,6 @@ __device__ __forceinline__ v8i fragment(const uint8_t* r0, uint32_t c, uint32_t 
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Which tile a work group owns.  Work groups go to the 8 dies in turn and each die has a cache of its own, so die x takes the x-th
-// eighth of the tiles, in stripes of 8 tiles of A's rows: its 32 compute units then work on about 8 x 4 tiles at a time, which read
-// 12 strips of rows instead of 33.
-__device__ __forceinline__ bool tile_of(uint32_t tiles_n, uint32_t tiles_m, uint32_t& n, uint32_t& m) {
-    const uint32_t all = tiles_n * tiles_m, each = (all + 7) / 8, t = blockIdx.x % 8 * each + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= each || t >= all) return false;
-    const uint32_t stripe = t / (8 * tiles_n), high = min(8u, tiles_m - 8 * stripe), r = t - stripe * 8 * tiles_n;
-    m = 8 * stripe + r % high;
-    n = r / high;
-    return true;
-}
-
 // A tile's rows from one column on, for loads that check their bounds: what lies past the last row, or past the last row's k columns (to a
 // multiple of 16), comes as zeros.  So no lane holds an offset for every row it loads, and there is room for the results of two squares.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const uint8_t* p, uint32_t rows, uint32_t ld, uint32_t k) {

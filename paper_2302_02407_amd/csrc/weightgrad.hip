@@ -26,11 +26,16 @@ template <> struct Parts<bf16_t> { static constexpr int N = 1; };
 template <> struct Parts<f16_t> { static constexpr int N = 2; };
 template <> struct Parts<f32_t> { static constexpr int N = 3; };
 
-// The upper half of a number of 32 bits, and what it leaves: nothing of an infinity
-__device__ __forceinline__ uint32_t upper(float& x) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
-    x = (b & 0x7fffffffu) == 0x7f800000u && x == x ? 0.0f : x - __builtin_bit_cast(float, b);
-    return b;
+// A number's bfloat16 parts, in the upper halves: 8 significant bits each, cut off; nothing but itself of an infinity
+template <int PARTS> __device__ __forceinline__ void parts_of(float x, uint32_t (&w)[PARTS]) {
+    w[0] = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
+    float rest = x - __builtin_bit_cast(float, w[0]);
+    if (__builtin_isinf(x)) rest = 0.0f;
+#pragma unroll
+    for (int q = 1; q < PARTS; q++) {
+        w[q] = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
+        rest -= __builtin_bit_cast(float, w[q]);
+    }
 }
 
 // A work group owns BN columns of dy by BK columns of what is kept and goes through the rows 32 at a time.
@@ -50,16 +55,19 @@ typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 // turns each row's into bfloat16 by that row's power, and puts pairs of rows together: the fragments of four squares, in which lane l
 // holds columns 4 l .. 4 l + 3, so that results are written 16 bytes a lane.  Rows r and r + 8 go to the two halves of a wavefront
 // and are 128 bytes, half of the banks, apart.
-template <class T, int WN, int WK, int TN> __global__ __launch_bounds__(64 * WN * WK, 1) void weight_grad_kernel(WeightArgs a) {
+template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_bounds__(64 * WN * WK, WN * WK > 4 ? 2 : 1) void weight_grad_kernel(WeightArgs a) {
     using raw = typename T::raw;
     using G = WeightTile<T, WN, WK, TN>;
     constexpr int PARTS = G::PARTS;
     extern __shared__ __align__(1024) uint8_t lds[];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane & 31, g = lane >> 5;
     const uint32_t wn = wave / WK, wk = wave % WK;
-    const uint32_t tiles_k = (a.k + G::BK - 1) / G::BK, n_own = blockIdx.x / tiles_k * G::BN, k0 = blockIdx.x % tiles_k * G::BK;
+    uint32_t n_own, k0;
+    if (!tile_of((a.n + G::BN - 1) / G::BN, (a.k + G::BK - 1) / G::BK, n_own, k0)) return;
+    n_own *= G::BN;
+    k0 *= G::BK;
     // the last tile begins earlier, so that all its columns are there; the rows of dw that another one has are left to that
-    const uint32_t n0 = a.n >= (uint32_t)G::BN ? min(n_own, a.n - G::BN) : 0;
+    const uint32_t n0 = NARROW ? 0 : min(n_own, a.n - G::BN);
     const uint32_t first = blockIdx.y * a.per * 32, steps = min((a.m - first + 31) / 32, a.per);
     const uint32_t codes_end = (a.k + 15) / 16 * 16, blocks = (a.k + 127) / 128;
 
@@ -74,7 +82,7 @@ template <class T, int WN, int WK, int TN> __global__ __launch_bounds__(64 * WN 
         for (int f = 0; f < G::FY; f++) {
             const uint32_t i = f * G::THREADS + tid, r = i / (G::BN / 8), at = n0 + i % (G::BN / 8) * 8, row = min(m0 + r, a.m - 1);
             const raw* from = (const raw*)a.dy + (u64)row * a.ld_dy;
-            if (a.n >= (uint32_t)G::BN) st.y[f].load(from + at);
+            if constexpr (!NARROW) st.y[f].load(from + at);
             else {                                        // columns past the end are anything that is no harm: their sums are not written
                 float x[8];
                 load8<T>(from, min(at, a.n - 1), a.n, x);
@@ -86,10 +94,8 @@ template <class T, int WN, int WK, int TN> __global__ __launch_bounds__(64 * WN 
             const uint32_t i = f * G::THREADS + tid, r = i / (G::BK / 16), at = k0 + i % (G::BK / 16) * 16, row = min(m0 + r, a.m - 1);
             st.x[f] = *(const uint4*)(a.codes + (u64)row * a.ld_codes + min(at, codes_end - 16));
         }
-        if (tid < 32 * WK) {
-            const uint32_t row = min(m0 + tid % 32, a.m - 1), block = min(k0 / 128 + tid / 32, blocks - 1);
-            st.e = a.exponents[(u64)row * a.ld_exponents + block];
-        }
+        const uint32_t row = min(m0 + tid % 32, a.m - 1), block = min(k0 / 128 + tid / 32 % WK, blocks - 1);
+        st.e = a.exponents[(u64)row * a.ld_exponents + block];
     };
     auto store = [&](uint32_t step, Stage& st) {
         uint8_t* buf = lds + (step & 1) * G::BYTES;
@@ -116,12 +122,11 @@ template <class T, int WN, int WK, int TN> __global__ __launch_bounds__(64 * WN 
                 uint32_t w[PARTS][4];
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    float x = st.y[f][2 * j], y = st.y[f][2 * j + 1];
+                    uint32_t lo[PARTS], hi[PARTS];
+                    parts_of(st.y[f][2 * j], lo);
+                    parts_of(st.y[f][2 * j + 1], hi);
 #pragma unroll
-                    for (int q = 0; q < PARTS; q++) {
-                        const uint32_t lo = upper(x), hi = upper(y);
-                        w[q][j] = lo >> 16 | hi;
-                    }
+                    for (int q = 0; q < PARTS; q++) w[q][j] = __builtin_amdgcn_perm(hi[q], lo[q], 0x07060302u);
                 }
 #pragma unroll
                 for (int q = 0; q < PARTS; q++) *(uint4*)(to + q * G::PLANE) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
@@ -273,12 +278,12 @@ template <class O> __global__ __launch_bounds__(256) void weight_join_kernel(con
         }
 }
 
-template <class T, int WN, int WK, int TN> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
+template <class T, int WN, int WK, int TN, bool NARROW> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
     using G = WeightTile<T, WN, WK, TN>;
-    const auto kernel = weight_grad_kernel<T, WN, WK, TN>;
+    const auto kernel = weight_grad_kernel<T, WN, WK, TN, NARROW>;
     const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
     if (ready != hipSuccess) return ready;
-    kernel<<<dim3(((a.n + G::BN - 1) / G::BN) * ((a.k + G::BK - 1) / G::BK), c.parts), G::THREADS, G::LDS, stream>>>(a);
+    kernel<<<dim3((((a.n + G::BN - 1) / G::BN) * ((a.k + G::BK - 1) / G::BK) + 7) / 8 * 8, c.parts), G::THREADS, G::LDS, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -311,7 +316,9 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     hipError_t err = hipSuccess;
     if (p->m) with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        err = c.bn == 256 ? launch_weight_grad<T, 4, 2, 2>(a, c, ctx->stream) : launch_weight_grad<T, 2, 1, 2>(a, c, ctx->stream);
+        if (c.bn == 256) err = launch_weight_grad<T, 4, 2, 2, false>(a, c, ctx->stream);
+        else if (p->n >= 128) err = launch_weight_grad<T, 2, 1, 2, false>(a, c, ctx->stream);
+        else err = launch_weight_grad<T, 2, 1, 2, true>(a, c, ctx->stream);
     });
     HE_HIP(ctx, err);
     if (joined) with_dtype(p->out_dtype, [&](auto o) {
