@@ -76,8 +76,10 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
         uint4 x[G::FX];
         uint32_t e;
     };
+    // The last 32 rows, of which some may not be there, come first, so that it is before the loop that they are made zeros.  Past the last step:
+    // one that is there again, for nothing.
     auto load = [&](uint32_t step, Stage& st) {
-        const uint32_t m0 = first + step * 32;
+        const uint32_t m0 = first + (step == 0 || step >= steps ? steps - 1 : step - 1) * 32;
 #pragma unroll
         for (int f = 0; f < G::FY; f++) {
             const uint32_t i = f * G::THREADS + tid, r = i / (G::BN / 8), at = n0 + i % (G::BN / 8) * 8, row = min(m0 + r, a.m - 1);
@@ -97,22 +99,22 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
         const uint32_t row = min(m0 + tid % 32, a.m - 1), block = min(k0 / 128 + tid / 32 % WK, blocks - 1);
         st.e = a.exponents[(u64)row * a.ld_exponents + block];
     };
+    auto cut = [&](Stage& st) {                           // zeros past the last row, in both operands
+        const uint32_t left = a.m - first - (steps - 1) * 32;
+#pragma unroll
+        for (int f = 0; f < G::FY; f++)
+            if ((f * G::THREADS + tid) / (G::BN / 8) >= left)
+#pragma unroll
+                for (int v = 0; v < Eight<T>::VECS; v++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) st.y[f].v[v].w[i] = 0;
+#pragma unroll
+        for (int f = 0; f < G::FX; f++)
+            if ((f * G::THREADS + tid) / (G::BK / 16) >= left) st.x[f] = make_uint4(0, 0, 0, 0);
+        if (tid % 32 >= left) st.e = 127;
+    };
     auto store = [&](uint32_t step, Stage& st) {
         uint8_t* buf = lds + (step & 1) * G::BYTES;
-        const uint32_t left = a.m - first - step * 32;    // rows from the 32's first on
-        if (left < 32) {                                  // past the last row: zeros, in both operands
-#pragma unroll
-            for (int f = 0; f < G::FY; f++)
-                if ((f * G::THREADS + tid) / (G::BN / 8) >= left)
-#pragma unroll
-                    for (int v = 0; v < Eight<T>::VECS; v++)
-#pragma unroll
-                        for (int i = 0; i < 4; i++) st.y[f].v[v].w[i] = 0;
-#pragma unroll
-            for (int f = 0; f < G::FX; f++)
-                if ((f * G::THREADS + tid) / (G::BK / 16) >= left) st.x[f] = make_uint4(0, 0, 0, 0);
-            if (tid % 32 >= left) st.e = 127;
-        }
 #pragma unroll
         for (int f = 0; f < G::FY; f++) {
             const uint32_t i = f * G::THREADS + tid, r = i / (G::BN / 8), p = i % (G::BN / 8);
@@ -137,7 +139,7 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
             const uint32_t i = f * G::THREADS + tid, r = i / (G::BK / 16), c = i % (G::BK / 16) * 16;
             *(uint4*)(buf + G::X + ((r * G::BK + c) ^ ((r >> 3 & 1) * 128))) = st.x[f];
         }
-        if (tid < 32 * WK) ((uint32_t*)(buf + G::S))[tid] = st.e == 255 ? 0x7fc00000u : st.e << 23;
+        ((uint32_t*)(buf + G::S))[tid % (32 * WK)] = st.e == 255 ? 0x7fc00000u : st.e << 23;      // several threads the same
     };
 
     // half h of a step: sixteen rows, eight a lane
@@ -175,8 +177,12 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
         for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0;
-    auto multiply = [&](const Half& f) {
-        uint32_t c[8][2], x[4][4];
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    struct Kept {
+        u4 x[4];                                          // of each square
+    };
+    auto convert = [&](const Half& f, Kept& to) {
+        uint32_t c[8][2];
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const float s = f.s[i / 4][i % 4];
@@ -186,49 +192,74 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
 #pragma unroll
         for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int u = 0; u < 4; u++) x[j][u] = __builtin_amdgcn_perm(c[2 * u + 1][j / 2], c[2 * u][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+            for (int u = 0; u < 4; u++) to.x[j][u] = __builtin_amdgcn_perm(c[2 * u + 1][j / 2], c[2 * u][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+    };
+    auto multiply = [&](const Half& f, const Kept& kept) {
 #pragma unroll
         for (int q = PARTS - 1; q >= 0; q--)
 #pragma unroll
             for (int i = 0; i < TN; i++) {
                 const v8b y = __builtin_bit_cast(v8b, __builtin_shufflevector(f.y[q][i][0], f.y[q][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, __builtin_bit_cast(v8b, u4{x[j][0], x[j][1], x[j][2], x[j][3]}), acc[i][j], 0, 0, 0);
-                }
+                for (int j = 0; j < 4; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, __builtin_bit_cast(v8b, kept.x[j]), acc[i][j], 0, 0, 0);
             }
     };
     // What a wavefront has written to LDS is there for the others, and what it has asked for has come
     auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
     Stage st;
-    load(0, st);
-    store(0, st);
-    if (steps > 1) load(1, st);
-    meet();
-    if constexpr (PARTS < 3) {
-        // a half is read while the one before is multiplied, the first of a step right behind the barrier that its rows wait for
-        Half one, two;
-        read(0, 0, one);
-        for (uint32_t b = 0; b < steps; b++) {
-            read(b, 1, two);
-            multiply(one);
-            if (b + 1 < steps) store(b + 1, st);          // the other buffer: its last reads lie before the last barrier
-            if (b + 2 < steps) load(b + 2, st);
-            meet();
-            if (b + 1 < steps) read(b + 1, 0, one);
-            multiply(two);
+    // between two matrix instructions a few of what turns the next half's codes
+    auto interleave = [&]() {
+#pragma unroll
+        for (int i = 0; i < TN * 4; i++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 32 / (TN * 4), 0);
         }
-    } else {                                              // three matrix products to a half hide its reads; two halves' fragments do not fit the registers
+    };
+    load(0, st);
+    cut(st);
+    store(0, st);
+    load(1, st);
+    meet();
+    if constexpr (PARTS == 1) {
+        // Three halves are on their way: one is multiplied while the next is turned into bfloat16 and the one behind that is read; so a step's
+        // rows are read while the step before is multiplied, and the buffer of that takes the step after.
+        Half one, two;
+        Kept k_one, k_two;
+        read(0, 0, one);
+        read(0, 1, two);
+        store(1, st);
+        load(2, st);
+        convert(one, k_one);
+        meet();
+        for (uint32_t b = 0; b < steps; b++) {
+            Half half, next;
+            read(b + 1, 0, half);
+            multiply(one, k_one);
+            convert(two, k_two);
+            interleave();
+            store(b + 2, st);
+            load(b + 3, st);
+            read(b + 1, 1, next);
+            multiply(two, k_two);
+            convert(half, k_one);
+            interleave();
+            one = half;
+            two = next;
+            meet();
+        }
+    } else {                                              // several matrix products to a half hide its reads
         Half half;
+        Kept kept;
         for (uint32_t b = 0; b < steps; b++) {
             read(b, 0, half);
-            multiply(half);
-            if (b + 1 < steps) store(b + 1, st);
+            convert(half, kept);
+            multiply(half, kept);
+            store(b + 1, st);                             // the other buffer: its last reads lie before the last barrier
             read(b, 1, half);
-            multiply(half);
-            if (b + 2 < steps) load(b + 2, st);
+            convert(half, kept);
+            multiply(half, kept);
+            load(b + 2, st);
             meet();
         }
     }
