@@ -39,9 +39,9 @@ template <int PARTS> __device__ __forceinline__ void parts_of(float x, uint32_t 
 }
 
 // A work group owns BN columns of dy by BK columns of what is kept and goes through the rows 32 at a time.
-template <class T, int WN, int WK, int TN> struct WeightTile {
-    static constexpr int PARTS = Parts<T>::N, BN = WN * TN * 32, BK = WK * 128, THREADS = 64 * WN * WK;
-    static constexpr int PLANE = 32 * BN * 2, X = PARTS * PLANE, S = X + 32 * BK, BYTES = S + 32 * WK * 4, LDS = 2 * BYTES;
+template <class T, int WN, int WK, int TN, int TK> struct WeightTile {
+    static constexpr int PARTS = Parts<T>::N, BN = WN * TN * 32, BK = WK * TK * 32, BLOCKS = BK / 128, THREADS = 64 * WN * WK;
+    static constexpr int PLANE = 32 * BN * 2, X = PARTS * PLANE, S = X + 32 * BK, BYTES = S + 32 * BLOCKS * 4, LDS = 2 * BYTES;
     static constexpr int FY = 4 * BN / THREADS, FX = 2 * BK / THREADS;       // pieces of 8 elements of dy, of 16 codes, a thread
 };
 
@@ -55,9 +55,10 @@ typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 // turns each row's into bfloat16 by that row's power, and puts pairs of rows together: the fragments of four squares, in which lane l
 // holds columns 4 l .. 4 l + 3, so that results are written 16 bytes a lane.  Rows r and r + 8 go to the two halves of a wavefront
 // and are 128 bytes, half of the banks, apart.
-template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_bounds__(64 * WN * WK, WN * WK > 4 ? 2 : 1) void weight_grad_kernel(WeightArgs a) {
+template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __launch_bounds__(64 * WN * WK, 2) void weight_grad_kernel(WeightArgs a) {
     using raw = typename T::raw;
-    using G = WeightTile<T, WN, WK, TN>;
+    using G = WeightTile<T, WN, WK, TN, TK>;
+    using codes_t = std::conditional_t<TK == 4, uint32_t, uint16_t>;         // a lane's columns of a row
     constexpr int PARTS = G::PARTS;
     extern __shared__ __align__(1024) uint8_t lds[];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane & 31, g = lane >> 5;
@@ -76,28 +77,43 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
         uint4 x[G::FX];
         uint32_t e;
     };
-    // The last 32 rows, of which some may not be there, come first, so that it is before the loop that they are made zeros.  Past the last step:
-    // one that is there again, for nothing.
-    auto load = [&](uint32_t step, Stage& st) {
-        const uint32_t m0 = first + (step == 0 || step >= steps ? steps - 1 : step - 1) * 32;
+    // The last 32 rows, of which some may not be there, come first, so that it is before the loop that they are made zeros; then the others.  Past the
+    // last step: one that is there again, for nothing.
+    const raw* y_from[G::FY];
+    const uint8_t *x_from[G::FX], *e_from;
+    auto place = [&](uint32_t m0) {
 #pragma unroll
         for (int f = 0; f < G::FY; f++) {
-            const uint32_t i = f * G::THREADS + tid, r = i / (G::BN / 8), at = n0 + i % (G::BN / 8) * 8, row = min(m0 + r, a.m - 1);
-            const raw* from = (const raw*)a.dy + (u64)row * a.ld_dy;
-            if constexpr (!NARROW) st.y[f].load(from + at);
-            else {                                        // columns past the end are anything that is no harm: their sums are not written
-                float x[8];
-                load8<T>(from, min(at, a.n - 1), a.n, x);
-                st.y[f].set(x);
-            }
+            const uint32_t i = f * G::THREADS + tid, row = min(m0 + i / (G::BN / 8), a.m - 1);
+            y_from[f] = (const raw*)a.dy + (u64)row * a.ld_dy + (NARROW ? 0 : n0 + i % (G::BN / 8) * 8);
         }
 #pragma unroll
         for (int f = 0; f < G::FX; f++) {
-            const uint32_t i = f * G::THREADS + tid, r = i / (G::BK / 16), at = k0 + i % (G::BK / 16) * 16, row = min(m0 + r, a.m - 1);
-            st.x[f] = *(const uint4*)(a.codes + (u64)row * a.ld_codes + min(at, codes_end - 16));
+            const uint32_t i = f * G::THREADS + tid, row = min(m0 + i / (G::BK / 16), a.m - 1);
+            x_from[f] = a.codes + (u64)row * a.ld_codes + min(k0 + i % (G::BK / 16) * 16, codes_end - 16);
         }
-        const uint32_t row = min(m0 + tid % 32, a.m - 1), block = min(k0 / 128 + tid / 32 % WK, blocks - 1);
-        st.e = a.exponents[(u64)row * a.ld_exponents + block];
+        const uint32_t row = min(m0 + tid % 32, a.m - 1), block = min(k0 / 128 + tid / 32 % G::BLOCKS, blocks - 1);
+        e_from = a.exponents + (u64)row * a.ld_exponents + block;
+    };
+    auto load = [&](uint32_t step, Stage& st) {
+        const u64 on = step != 0 && step + 1 < steps ? 32 : 0;       // rows to the next step's
+#pragma unroll
+        for (int f = 0; f < G::FY; f++) {
+            if constexpr (!NARROW) st.y[f].load(y_from[f]);
+            else {                                        // columns past the end are anything that is no harm: their sums are not written
+                float x[8];
+                load8<T>(y_from[f], min((f * G::THREADS + tid) % (G::BN / 8) * 8, a.n - 1), a.n, x);
+                st.y[f].set(x);
+            }
+            y_from[f] += on * a.ld_dy;
+        }
+#pragma unroll
+        for (int f = 0; f < G::FX; f++) {
+            st.x[f] = *(const uint4*)x_from[f];
+            x_from[f] += on * a.ld_codes;
+        }
+        st.e = *e_from;
+        e_from += on * a.ld_exponents;
     };
     auto cut = [&](Stage& st) {                           // zeros past the last row, in both operands
         const uint32_t left = a.m - first - (steps - 1) * 32;
@@ -139,7 +155,7 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
             const uint32_t i = f * G::THREADS + tid, r = i / (G::BK / 16), c = i % (G::BK / 16) * 16;
             *(uint4*)(buf + G::X + ((r * G::BK + c) ^ ((r >> 3 & 1) * 128))) = st.x[f];
         }
-        ((uint32_t*)(buf + G::S))[tid % (32 * WK)] = st.e == 255 ? 0x7fc00000u : st.e << 23;      // several threads the same
+        ((uint32_t*)(buf + G::S))[tid % (32 * G::BLOCKS)] = st.e == 255 ? 0x7fc00000u : st.e << 23;      // several threads the same
     };
 
     // half h of a step: sixteen rows, eight a lane
@@ -153,15 +169,15 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
     for (int q = 0; q < TN; q++)
         y_at[q] = (8 * g + (lane & 15) / 4) * (G::BN * 2) + (((wn * TN * 4 + 4 * q + (lane >> 4 & 1) * 2 + (lane & 3) / 2) ^ 4 * ((lane & 15) / 4)) * 16) + (lane & 1) * 8;
 #pragma unroll
-    for (int i = 0; i < 2; i++) x_at[i] = G::X + (((8 * g + i) * G::BK + wk * 128 + 4 * l) ^ (g * 128));
+    for (int i = 0; i < 2; i++) x_at[i] = G::X + (((8 * g + i) * G::BK + (wk * 32 + l) * TK) ^ (g * 128));
     auto read = [&](uint32_t step, int h, Half& f) {
         const uint32_t buf = (step & 1) * G::BYTES;
 #pragma unroll
         for (int u = 0; u < 4; u++)
 #pragma unroll
-            for (int i = 0; i < 2; i++) f.x[2 * u + i] = *(const uint32_t*)(lds + buf + x_at[i] + (16 * h + 2 * u) * G::BK);
+            for (int i = 0; i < 2; i++) f.x[2 * u + i] = *(const codes_t*)(lds + buf + x_at[i] + (16 * h + 2 * u) * G::BK);
 #pragma unroll
-        for (int i = 0; i < 2; i++) f.s[i] = *(const v4f*)(lds + buf + G::S + (wk * 32 + 16 * h + 8 * g + 4 * i) * 4);
+        for (int i = 0; i < 2; i++) f.s[i] = *(const v4f*)(lds + buf + G::S + (wk * TK / 4 * 32 + 16 * h + 8 * g + 4 * i) * 4);
 #pragma unroll
         for (int q = PARTS - 1; q >= 0; q--)
 #pragma unroll
@@ -170,27 +186,27 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
                 for (int t = 0; t < 2; t++)
                     f.y[q][i][t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)((lds_ptr)lds + buf + y_at[i] + (q * 32 + 16 * h + 4 * t) * (G::BN * 2)));
     };
-    v16f acc[TN][4];
+    v16f acc[TN][TK];
 #pragma unroll
     for (int i = 0; i < TN; i++)
 #pragma unroll
-        for (int j = 0; j < 4; j++)
+        for (int j = 0; j < TK; j++)
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0;
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
     struct Kept {
-        u4 x[4];                                          // of each square
+        u4 x[TK];                                         // of each square
     };
     auto convert = [&](const Half& f, Kept& to) {
-        uint32_t c[8][2];
+        uint32_t c[8][TK / 2];
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const float s = f.s[i / 4][i % 4];
             c[i][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.x[i], s, false));
-            c[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.x[i], s, true));
+            if constexpr (TK == 4) c[i][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.x[i], s, true));
         }
 #pragma unroll
-        for (int j = 0; j < 4; j++)
+        for (int j = 0; j < TK; j++)
 #pragma unroll
             for (int u = 0; u < 4; u++) to.x[j][u] = __builtin_amdgcn_perm(c[2 * u + 1][j / 2], c[2 * u][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
     };
@@ -201,7 +217,7 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
             for (int i = 0; i < TN; i++) {
                 const v8b y = __builtin_bit_cast(v8b, __builtin_shufflevector(f.y[q][i][0], f.y[q][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, __builtin_bit_cast(v8b, kept.x[j]), acc[i][j], 0, 0, 0);
+                for (int j = 0; j < TK; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, __builtin_bit_cast(v8b, kept.x[j]), acc[i][j], 0, 0, 0);
             }
     };
     // What a wavefront has written to LDS is there for the others, and what it has asked for has come
@@ -211,14 +227,16 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
     // between two matrix instructions a few of what turns the next half's codes
     auto interleave = [&]() {
 #pragma unroll
-        for (int i = 0; i < TN * 4; i++) {
+        for (int i = 0; i < TN * TK; i++) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 32 / (TN * 4), 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 8 / TN, 0);
         }
     };
+    place(first + (steps - 1) * 32);
     load(0, st);
     cut(st);
     store(0, st);
+    if (steps > 1) place(first);
     load(1, st);
     meet();
     if constexpr (PARTS == 1) {
@@ -263,19 +281,19 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
             meet();
         }
     }
-    // element e of a square: row 8 (e / 4) + 4 g + e % 4, square j column 4 l + j
-    const uint32_t k = k0 + wk * 128 + 4 * l;
+    // element e of a square: row 8 (e / 4) + 4 g + e % 4, square j column TK l + j
+    const uint32_t k = k0 + (wk * 32 + l) * TK;
     auto put = [&](auto o, u64 at, const float* x) {
         using O = decltype(o);
-        typename O::raw *to = (typename O::raw*)a.dw + at, v[4];
-        if (k + 4 <= a.k) {
+        typename O::raw *to = (typename O::raw*)a.dw + at, v[TK];
+        if (k + TK <= a.k) {
             if (a.accumulate) __builtin_memcpy(v, to, sizeof v);
 #pragma unroll
-            for (int j = 0; j < 4; j++) v[j] = from_float<O>(a.accumulate ? to_float<O>(v[j]) + x[j] : x[j]);
+            for (int j = 0; j < TK; j++) v[j] = from_float<O>(a.accumulate ? to_float<O>(v[j]) + x[j] : x[j]);
             __builtin_memcpy(to, v, sizeof v);
         } else
 #pragma unroll
-            for (int j = 0; j < 4; j++)
+            for (int j = 0; j < TK; j++)
                 if (k + j < a.k) to[j] = from_float<O>(a.accumulate ? to_float<O>(to[j]) + x[j] : x[j]);
     };
 #pragma unroll
@@ -283,7 +301,9 @@ template <class T, int WN, int WK, int TN, bool NARROW> __global__ __launch_boun
 #pragma unroll
         for (int e = 0; e < 16; e++) {
             const uint32_t n = n0 + (wn * TN + i) * 32 + 8 * (e / 4) + 4 * g + e % 4;
-            const float x[4] = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+            float x[TK];
+#pragma unroll
+            for (int j = 0; j < TK; j++) x[j] = acc[i][j][e];
             const u64 at = blockIdx.y * a.part + n * a.ld_dw + k;
             if (n >= n_own && n < a.n && k < a.k) {
                 if (a.out_dtype == HE_F32) put(f32_t{}, at, x);
@@ -309,9 +329,9 @@ template <class O> __global__ __launch_bounds__(256) void weight_join_kernel(con
         }
 }
 
-template <class T, int WN, int WK, int TN, bool NARROW> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
-    using G = WeightTile<T, WN, WK, TN>;
-    const auto kernel = weight_grad_kernel<T, WN, WK, TN, NARROW>;
+template <class T, int WN, int WK, int TN, int TK, bool NARROW> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
+    using G = WeightTile<T, WN, WK, TN, TK>;
+    const auto kernel = weight_grad_kernel<T, WN, WK, TN, TK, NARROW>;
     const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
     if (ready != hipSuccess) return ready;
     kernel<<<dim3((((a.n + G::BN - 1) / G::BN) * ((a.k + G::BK - 1) / G::BK) + 7) / 8 * 8, c.parts), G::THREADS, G::LDS, stream>>>(a);
@@ -347,9 +367,9 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     hipError_t err = hipSuccess;
     if (p->m) with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        if (c.bn == 256) err = launch_weight_grad<T, 4, 2, 2, false>(a, c, ctx->stream);
-        else if (p->n >= 128) err = launch_weight_grad<T, 2, 1, 2, false>(a, c, ctx->stream);
-        else err = launch_weight_grad<T, 2, 1, 2, true>(a, c, ctx->stream);
+        if (c.bn == 256) err = launch_weight_grad<T, 4, 2, 2, 4, false>(a, c, ctx->stream);
+        else if (p->n >= 128) err = launch_weight_grad<T, 2, 2, 2, 2, false>(a, c, ctx->stream);
+        else err = launch_weight_grad<T, 2, 2, 2, 2, true>(a, c, ctx->stream);
     });
     HE_HIP(ctx, err);
     if (joined) with_dtype(p->out_dtype, [&](auto o) {
