@@ -244,20 +244,22 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
         // rows are read while the step before is multiplied, and the buffer of that takes the step after.
         Half one, two;
         Kept k_one, k_two;
+        Stage other;
         read(0, 0, one);
         read(0, 1, two);
+        load(2, other);
         store(1, st);
-        load(2, st);
+        load(3, st);
         convert(one, k_one);
         meet();
-        for (uint32_t b = 0; b < steps; b++) {
+        auto body = [&](uint32_t b, Stage& now) {         // `now`: what was asked for two steps ago
             Half half, next;
             read(b + 1, 0, half);
             multiply(one, k_one);
             convert(two, k_two);
             interleave();
-            store(b + 2, st);
-            load(b + 3, st);
+            store(b + 2, now);
+            load(b + 4, now);
             read(b + 1, 1, next);
             multiply(two, k_two);
             convert(half, k_one);
@@ -265,6 +267,10 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
             one = half;
             two = next;
             meet();
+        };
+        for (uint32_t b = 0; b < steps; b += 2) {
+            body(b, other);
+            if (b + 1 < steps) body(b + 1, st);
         }
     } else {                                              // several matrix products to a half hide its reads
         Half half;
