@@ -759,7 +759,8 @@ class HEContext:
         self._ck(self._lib.he_weight_grad_q8(self._h, _WEIGHT_GRAD.pack(*head, at, size)))
         return dw
 
-    def he_work_weight_grad_q8(self, m, n, k, dtype=torch.bfloat16):
+    def he_work_weight_grad_q8(self, m, n, k, dtype):
+        """Bytes of scratch memory; dtype: dy's."""
         return self._work_bytes(self._lib.he_work_weight_grad_q8, _WEIGHT_GRAD.pack(m, n, k, _DTYPE[dtype], *[0] * 12))
 
     def he_token_logprobs(self, z, tau=1.0, tokens=None, logp=None, entropy=None, values=None, index=None, stats=None, work=None):

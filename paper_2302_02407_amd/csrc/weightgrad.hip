@@ -85,7 +85,8 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
 #pragma unroll
         for (int f = 0; f < G::FY; f++) {
             const uint32_t i = f * G::THREADS + tid, row = min(m0 + i / (G::BN / 8), a.m - 1);
-            y_from[f] = (const raw*)a.dy + (u64)row * a.ld_dy + (NARROW ? 0 : n0 + i % (G::BN / 8) * 8);
+            const uint32_t at = n0 + i % (G::BN / 8) * 8;
+            y_from[f] = (const raw*)a.dy + (u64)row * a.ld_dy + (!NARROW ? at : a.n >= 8 ? min(at, a.n - 8) : 0);
         }
 #pragma unroll
         for (int f = 0; f < G::FX; f++) {
@@ -99,10 +100,10 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
         const u64 on = step != 0 && step + 1 < steps ? 32 : 0;       // rows to the next step's
 #pragma unroll
         for (int f = 0; f < G::FY; f++) {
-            if constexpr (!NARROW) st.y[f].load(y_from[f]);
-            else {                                        // columns past the end are anything that is no harm: their sums are not written
+            if (!NARROW || a.n >= 8) st.y[f].load(y_from[f]);
+            else {
                 float x[8];
-                load8<T>(y_from[f], min((f * G::THREADS + tid) % (G::BN / 8) * 8, a.n - 1), a.n, x);
+                load8<T>(y_from[f], 0, a.n, x);
                 st.y[f].set(x);
             }
             y_from[f] += on * a.ld_dy;
@@ -134,6 +135,21 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
 #pragma unroll
         for (int f = 0; f < G::FY; f++) {
             const uint32_t i = f * G::THREADS + tid, r = i / (G::BN / 8), p = i % (G::BN / 8);
+            if (NARROW && a.n > 8 && a.n % 8) {           // the last piece was read from inside the row: its own elements to the front
+                const uint32_t on = p * 8 + 8 > a.n ? p * 8 + 8 - a.n : 0;
+                constexpr int WORDS = 4 * Eight<T>::VECS;
+                uint32_t w[WORDS + 8];
+#pragma unroll
+                for (int j = 0; j < WORDS + 8; j++) w[j] = j < WORDS ? st.y[f].v[j / 4].w[j % 4] : 0;
+#pragma unroll
+                for (int by = 4; by; by /= 2) {
+                    const uint32_t bits = by * sizeof(raw) * 8;
+#pragma unroll
+                    for (int j = 0; j < WORDS; j++) w[j] = !(on & by) ? w[j] : bits >= 32 ? w[j + bits / 32] : w[j] >> 16 | w[j + 1] << 16;
+                }
+#pragma unroll
+                for (int j = 0; j < WORDS; j++) st.y[f].v[j / 4].w[j % 4] = w[j];
+            }
             uint8_t* to = buf + r * (G::BN * 2) + ((p ^ (4 * (r & 3))) * 16);
             if constexpr (PARTS == 1) *(uint4*)to = make_uint4(st.y[f].v[0].w[0], st.y[f].v[0].w[1], st.y[f].v[0].w[2], st.y[f].v[0].w[3]);
             else {
@@ -244,22 +260,16 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
         // rows are read while the step before is multiplied, and the buffer of that takes the step after.
         Half one, two;
         Kept k_one, k_two;
-        Stage other;
         read(0, 0, one);
         read(0, 1, two);
-        load(2, other);
-        store(1, st);
-        load(3, st);
-        convert(one, k_one);
-        meet();
-        auto body = [&](uint32_t b, Stage& now) {         // `now`: what was asked for two steps ago
+        auto body = [&](uint32_t b, Stage& now, uint32_t ahead) {
             Half half, next;
             read(b + 1, 0, half);
             multiply(one, k_one);
             convert(two, k_two);
             interleave();
             store(b + 2, now);
-            load(b + 4, now);
+            load(b + ahead, now);
             read(b + 1, 1, next);
             multiply(two, k_two);
             convert(half, k_one);
@@ -268,9 +278,23 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
             two = next;
             meet();
         };
-        for (uint32_t b = 0; b < steps; b += 2) {
-            body(b, other);
-            if (b + 1 < steps) body(b + 1, st);
+        if constexpr (G::THREADS > 256) {                 // rows are asked for two steps ahead
+            Stage other;
+            load(2, other);
+            store(1, st);
+            load(3, st);
+            convert(one, k_one);
+            meet();
+            for (uint32_t b = 0; b < steps; b += 2) {
+                body(b, other, 4);
+                if (b + 1 < steps) body(b + 1, st, 4);
+            }
+        } else {                                          // one step: three work groups share a compute unit then
+            store(1, st);
+            load(2, st);
+            convert(one, k_one);
+            meet();
+            for (uint32_t b = 0; b < steps; b++) body(b, st, 3);
         }
     } else {                                              // several matrix products to a half hide its reads
         Half half;
@@ -320,19 +344,36 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
         }
 }
 
-// Sums the parts, in order
-template <class O> __global__ __launch_bounds__(256) void weight_join_kernel(const float* parts, uint32_t n_parts, u64 part, u64 ld_part, typename O::raw* dw, u64 ld_dw, uint32_t k, uint32_t accumulate) {
-    const uint32_t i = (blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= k) return;
-    const float* p = parts + blockIdx.y * ld_part + i;
+// Sums the parts, in a fixed order: four elements a thread, LANES of which take every LANES-th part of the same four.  Parts lie as dw does, their rows
+// ld_part apart, a multiple of 4.
+template <class O, int LANES> __global__ __launch_bounds__(256) void weight_join_kernel(const float* parts, uint32_t n_parts, u64 part, uint32_t ld_part, typename O::raw* dw, u64 ld_dw, uint32_t k, uint32_t accumulate) {
+    constexpr int GROUP = 256 / LANES;
+    __shared__ v4f sums[LANES][GROUP];
+    const u64 i = ((u64)blockIdx.x * GROUP + threadIdx.x % GROUP) * 4;
+    const uint32_t lane = threadIdx.x / GROUP;
     v4f x = {0, 0, 0, 0};
-    for (uint32_t q = 0; q < n_parts; q++) x += *(const v4f*)(p + q * part);
+    if (i < part)
+#pragma unroll 4
+        for (uint32_t q = lane; q < n_parts; q += LANES) x += *(const v4f*)(parts + q * part + i);
+    if (LANES > 1) {
+        sums[lane][threadIdx.x % GROUP] = x;
+        __syncthreads();
+        if (lane) return;
 #pragma unroll
-    for (uint32_t e = 0; e < 4; e++)
-        if (i + e < k) {
-            typename O::raw* to = dw + blockIdx.y * ld_dw + i + e;
-            *to = from_float<O>(accumulate ? to_float<O>(*to) + x[e] : x[e]);
-        }
+        for (int j = 1; j < LANES; j++) x += sums[j][threadIdx.x];
+    }
+    if (i >= part) return;
+    const uint32_t row = (uint32_t)(i / ld_part), at = (uint32_t)(i - (u64)row * ld_part);
+    typename O::raw *to = dw + row * ld_dw + at, v[4];
+    if (at + 4 <= k) {
+        if (accumulate) __builtin_memcpy(v, to, sizeof v);
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = from_float<O>(accumulate ? to_float<O>(v[e]) + x[e] : x[e]);
+        __builtin_memcpy(to, v, sizeof v);
+    } else
+#pragma unroll
+        for (uint32_t e = 0; e < 4; e++)
+            if (at + e < k) to[e] = from_float<O>(accumulate ? to_float<O>(to[e]) + x[e] : x[e]);
 }
 
 template <class T, int WN, int WK, int TN, int TK, bool NARROW> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
@@ -360,7 +401,7 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     if (p->n == 0 || p->k == 0 || (p->m == 0 && p->accumulate)) return HE_OK;
     const OnDevice device(ctx);
     HE_HIP(ctx, device.status);
-    const WeightCut c = weight_cut(p->m, p->n, p->k);
+    const WeightCut c = weight_cut(p->m, p->n, p->k, p->dtype);
     const bool joined = p->m == 0 || c.parts > 1;
     WeightArgs a = {p->d_dy, p->d_codes, p->d_exponents, p->d_dw, p->ld_dy, p->ld_codes, p->ld_exponents, p->ld_dw, p->m, p->n, p->k, c.per, 0, p->out_dtype, p->accumulate};
     if (joined) {
@@ -373,16 +414,22 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     hipError_t err = hipSuccess;
     if (p->m) with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        if (c.bn == 256) err = launch_weight_grad<T, 4, 2, 2, 4, false>(a, c, ctx->stream);
+        if (c.side == 256) err = launch_weight_grad<T, 4, 2, 2, 4, false>(a, c, ctx->stream);
         else if (p->n >= 128) err = launch_weight_grad<T, 2, 2, 2, 2, false>(a, c, ctx->stream);
         else err = launch_weight_grad<T, 2, 2, 2, 2, true>(a, c, ctx->stream);
     });
     HE_HIP(ctx, err);
     if (joined) with_dtype(p->out_dtype, [&](auto o) {
         using O = decltype(o);
-        for (uint32_t r = 0; r < p->n; r += 65535)        // a grid's second side
-            weight_join_kernel<O><<<dim3((p->k + 1023) / 1024, min(p->n - r, 65535u)), 256, 0, ctx->stream>>>(
-                (const float*)p->d_work + r * a.ld_dw, p->m ? c.parts : 0, a.part, a.ld_dw, (typename O::raw*)p->d_dw + r * p->ld_dw, p->ld_dw, p->k, p->accumulate);
+        const u64 all = (u64)p->n * a.ld_dw;              // below 2^34: fewer than 2^31 threads
+        const uint32_t parts = p->m ? c.parts : 0;
+        auto go = [&](auto lanes) {
+            constexpr int LANES = decltype(lanes)::value;
+            weight_join_kernel<O, LANES><<<(all + 1024 / LANES - 1) / (1024 / LANES), 256, 0, ctx->stream>>>(
+                (const float*)p->d_work, parts, all, (uint32_t)a.ld_dw, (typename O::raw*)p->d_dw, p->ld_dw, p->k, p->accumulate);
+        };
+        if (parts > 8) go(std::integral_constant<int, 8>{});
+        else go(std::integral_constant<int, 1>{});
     });
     HE_LAUNCHED(ctx);
     return HE_OK;

@@ -191,10 +191,14 @@ int main() {
     for (uint32_t m : sizes)
         for (uint32_t n : sizes)
             for (uint32_t k : sizes) {
-                const WeightCut c = weight_cut(m, n, k);
+                for (int32_t t = 0; t < 3; t++) {
+                const WeightCut c = weight_cut(m, n, k, t);
                 const uint32_t steps = (m + 31) / 32;
                 if (c.parts < 1 || c.parts > 65535 || c.per < 1 || (uint64_t)(c.parts - 1) * c.per >= steps || (uint64_t)c.parts * c.per < steps) { bad++; printf("cut of %u %u %u\n", m, n, k); }
+                if (c.side != 128 && (c.side != 256 || n < 256)) { bad++; printf("tile of %u %u %u\n", m, n, k); }
+                }
             }
+    if (weight_cut(0, 5, 7, HE_F32).parts != 1 || weight_cut(0, 5, 7, HE_F32).per != 0) { bad++; printf("cut of no rows\n"); }
     for (uint32_t rows : sizes)
         for (uint32_t dim : sizes)
             if (dim <= HE_DIM_MAX && (layernorm_parts(rows, dim) < 1 || layernorm_parts(rows, dim) > rows || layernorm_parts(rows, dim) > 65535 || poly_groups(rows, dim) < 1)) { bad++; printf("parts of %u %u\n", rows, dim); }
