@@ -629,7 +629,7 @@ int32_t he_work_token_logprobs(const he_ctx* ctx, const he_logprobs_plan* plan, 
 /* grad = d_logp_weights[row] times the gradient of the row's log p[token] by z, plus d_entropy_weights[row] times that of its entropy:
  *   (a ([i = token] - p_i) - b p_i (log p_i + entropy)) / tau.
  * Either may be NULL (none); log probabilities need tokens.  A weight of 0, a token that is not there, and a row of a sum of 0 have no
- * gradient, whatever the logits are; nor has a log probability of -infinity.  d_grad may be d_z with the same ld. */
+ * gradient, whatever the logits are.  d_grad may be d_z with the same ld. */
 typedef struct {
     uint32_t rows, vocab;
     int32_t dtype;                 /* of z and of the gradient */

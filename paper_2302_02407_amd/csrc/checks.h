@@ -222,9 +222,23 @@ static inline const char* logits_sizes(uint32_t rows, uint32_t vocab, int32_t dt
     if (rows > HE_ROWS_MAX) return "more than 2^21 rows";
     return nullptr;
 }
+// A row's parts, each a work group's, and the elements of one
+struct LogprobCut {
+    uint32_t parts, len;
+};
+// Few long rows are cut in up to 32 parts of at least 8 KiB, which are joined by a second launch
+static inline LogprobCut logprobs_cut(uint32_t rows, uint32_t vocab, int32_t dtype) {
+    const uint32_t piece = 8192 / dtype_bytes(dtype);
+    uint32_t parts = rows ? 256 / rows : 1;
+    if (parts > vocab / piece) parts = vocab / piece;
+    if (parts > 32) parts = 32;
+    if (parts < 4) return {1, vocab};
+    const uint32_t len = ((vocab + parts - 1) / parts + 15) & ~15u;
+    return {(vocab + len - 1) / len, len};
+}
 static inline uint64_t logprobs_work(const he_logprobs_plan* p) {
-    (void)p;
-    return 0;
+    const uint32_t parts = logprobs_cut(p->rows, p->vocab, p->dtype).parts;
+    return parts > 1 ? (uint64_t)p->rows * parts * (16 + 8ull * p->k) : 0;
 }
 static inline const char* refuse_logprobs(const he_logprobs_plan* p, bool query = false) {
     if (!p) return "null plan";

@@ -1,5 +1,5 @@
 // The k largest logits of a row in order, and the log-sum-exp of the others.
-#include "plain.h"
+#include "top.h"
 
 struct TopArgs {
     const void* z;
@@ -9,30 +9,6 @@ struct TopArgs {
     u64 ld_z;
     uint32_t vocab, k;
     float tau;
-};
-
-// Ordered like the numbers: NaN above infinity, -0 with +0
-__device__ __forceinline__ uint32_t order_key(float z) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, z == 0.0f ? 0.0f : z);
-    return z != z ? 0xffffffffu : b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-
-__device__ __forceinline__ float value_of(uint32_t key) {
-    return key == 0xffffffffu ? NAN : __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key);
-}
-__device__ __forceinline__ u64 place_of(float z, uint32_t i) { return (u64)order_key(z) << 32 | (uint32_t)~i; }
-
-// An element's place in the order is one number of 64 bits, its key above the complement of its index, all different.
-
-template <int THREADS> struct TopShared {
-    static constexpr int ROOM = THREADS == 1024 ? 1024 : THREADS == 64 ? 64 : 512, KEEP = 512;
-    uint4 aside[ROOM];                         // 16 bytes of the row each, and which
-    uint32_t which[ROOM];                      // index of the first of its elements, and above 24 bits how many are another's
-    u64 keep[KEEP], more, last;                // last: the k-th place
-    uint32_t bins[256];
-    int32_t tw[2][THREADS / 64];
-    float room[THREADS / 64];
-    uint32_t digit, left, got, kept;
 };
 
 // A sum times a power of two: what is beside nothing is nothing, also where it had become infinite
@@ -54,47 +30,18 @@ template <class T, int THREADS> __device__ __forceinline__ void rest_of(const To
     if (threadIdx.x == 0) a.rest[row] = at >= -low ? sum : logf(sum) + at / a.tau;
 }
 
-// A row by reading it as often as it takes: the k-th largest place is found a digit of 8 bits at a time, from the row's counts of that digit
-// among the elements that agree with the digits before; then the elements from it on are gathered and the rest is summed against its own
-// maximum.  For rows with so many equal elements, or elements in such an order, that setting aside (below) has not enough room, and for rows
-// with NaN.
+// A row by reading it as often as it takes; the rest is summed against its own maximum.  For rows with so many equal elements, or elements in such an
+// order, that setting aside (below) has not enough room, and for rows with NaN.
 template <class T, int THREADS> __device__ __forceinline__ void exact_row(const TopArgs& a, TopShared<THREADS>& s, u64 row) {
     using raw = typename T::raw;
     const raw* z = (const raw*)a.z + row * a.ld_z;
     const uint32_t t = threadIdx.x;
-    u64 prefix = 0;
-    uint32_t want = a.k;                       // how many of the elements that agree with `prefix` are still wanted
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        __syncthreads();
-        for (uint32_t i = t; i < 256; i += THREADS) s.bins[i] = 0;
-        __syncthreads();
-        for (uint32_t i = t; i < a.vocab; i += THREADS) {
-            const u64 c = place_of(to_float<T>(z[i]), i);
-            if (shift == 56 || c >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&s.bins[(uint32_t)(c >> shift) & 255], 1u);
-        }
-        __syncthreads();
-        if (t == 0) {
-            uint32_t n = want, d = 255;
-            while (s.bins[d] < n) n -= s.bins[d--];
-            s.digit = d;
-            s.left = n;
-        }
-        __syncthreads();
-        prefix |= (u64)s.digit << shift;
-        want = s.left;
-    }
-    if (t == 0) s.got = 0;
-    __syncthreads();
     const float low = masked_from(a.tau);
     float most = -INFINITY;
-    for (uint32_t i = t; i < a.vocab; i += THREADS) {
-        const float v = to_float<T>(z[i]);
-        const u64 c = place_of(v, i);
-        if (c >= prefix) s.keep[atomicAdd(&s.got, 1u)] = c;     // exactly k
-        else if (!(v <= low)) most = fmaxf(most, v);
-    }
+    const u64 prefix = exact_keep<T, THREADS>(z, a.vocab, a.k, 0, s, [&](float v) {
+        if (!(v <= low)) most = fmaxf(most, v);
+    });
     most = group_max<THREADS / 64>(most, s.room);
-    __syncthreads();
     for (uint32_t i0 = t; i0 < a.k; i0 += THREADS) {
         const u64 c = s.keep[i0];
         uint32_t place = 0;
@@ -135,16 +82,7 @@ template <class T, int THREADS> __global__ __launch_bounds__(THREADS, THREADS ==
     if (t == 0) s.got = s.kept = 0, s.more = 0;
     float m = low, sum = 0, high = -INFINITY, least = -INFINITY;
     auto raise = [&](int32_t* tw) {
-        int32_t w = ordered(high), best = INT32_MIN;
-        if (r <= 64)
-            for (uint32_t i = 0; i < r; i++) {
-                best = wave_max(w);
-                if (lane == (uint32_t)__builtin_ctzll(__ballot(w == best))) w = INT32_MIN;
-            }
-        if (lane == 0) tw[wave] = wave < full ? best : INT32_MAX;
-        __syncthreads();
-        const int32_t all = __builtin_amdgcn_readfirstlane(row_min(tw[lane % WAVES]));
-        least = r <= 64 ? fmaxf(unordered(all), -INFINITY) : -INFINITY;      // no NaN: lanes that have run out
+        least = reached_by_all<WAVES>(high, r, full, lane, wave, tw);
     };
     auto turn = [&](uint32_t p, Vec<T>& buf) {           // two buffers in turn, each refilled as soon as it is taken
         const uint32_t v = p * THREADS + t;

@@ -116,7 +116,7 @@ def logprobs_grad(z, tau, tokens, a, b):
     grad, size = torch.zeros(rows, vocab, dtype=torch.float64), torch.zeros(rows, vocab, dtype=torch.float64)
     for r in range(rows):
         y = -1 if tokens is None else int(tokens[r])
-        wa = float(a[r]) if a is not None and 0 <= y < vocab and logp[r, y] > -math.inf else 0.0
+        wa = float(a[r]) if a is not None and 0 <= y < vocab and (p[r] > 0).any() else 0.0
         wb = float(b[r]) if b is not None else 0.0
         lp = torch.where(p[r] > 0, logp[r], 0.0)
         grad[r] = -(wa * p[r] + wb * p[r] * (lp + entropy[r])) / tau
