@@ -57,10 +57,11 @@ template <class T> __device__ __forceinline__ void write_row(const LogprobArgs& 
 // One row, or a part of one, a work group, read once, 16 bytes a lane at a time: every element into its lane's sums against the lane's running maximum,
 // (z - M) c by a difference and a product, so that logits of any size lose nothing.  TOP: pieces with an element that reaches a threshold are also set
 // aside, as top_logits_kernel does (toplogits.hip); what is set aside only has to be put in order, the sums have it already.
-template <class T, int THREADS, bool TOP, bool PARTED> __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void logprobs_kernel(LogprobArgs a) {
+template <class T, int THREADS, int ROOM, bool PARTED> __global__ __launch_bounds__(THREADS, 4) void logprobs_kernel(LogprobArgs a) {
     using raw = typename T::raw;
-    constexpr int N = Vec<T>::N, WAVES = THREADS / 64, ROOM = TopShared<THREADS>::ROOM, KEEP = TopShared<THREADS>::KEEP;
-    __shared__ std::conditional_t<TOP, TopShared<THREADS>, char> shared;
+    constexpr int N = Vec<T>::N, WAVES = THREADS / 64;
+    constexpr bool TOP = ROOM != 0;
+    __shared__ std::conditional_t<TOP, TopShared<THREADS, TOP ? ROOM : 1>, char> shared;
     __shared__ float room[2 * WAVES];
     const u64 row = PARTED ? blockIdx.y : blockIdx.x;
     const uint32_t part = PARTED ? blockIdx.x : 0, from = PARTED ? part * a.len : 0, n = PARTED ? min(a.len, a.vocab - from) : a.vocab;
@@ -137,15 +138,15 @@ template <class T, int THREADS, bool TOP, bool PARTED> __global__ __launch_bound
                 const uint32_t which = shared.which[i / N], at = (which & 0xffffff) + i % N;
                 if (!(v < least) && i % N >= which >> 24) {
                     const uint32_t to = atomicAdd(&shared.kept, 1u);
-                    if (to < KEEP) shared.keep[to] = place_of(v, from + at);
+                    if (to < shared.KEEP) shared.keep[to] = place_of(v, from + at);
                 }
             }
             __syncthreads();
             kept = shared.kept;
-            exact = kept > KEEP;
+            exact = kept > shared.KEEP;
         }
         if (exact) {
-            exact_keep<T, THREADS>(z, n, a.k, from, shared, [](float) {});
+            exact_keep<T>(z, n, a.k, from, shared, [](float) {});
             kept = a.k;
         }
         for (uint32_t i = t; i < kept; i += THREADS) {
@@ -269,24 +270,30 @@ extern "C" int32_t he_token_logprobs(he_ctx* ctx, const he_logprobs_plan* p) {
             logprobs_short_kernel<T><<<(p->rows + 255) / 256, 256, 0, ctx->stream>>>(a, p->rows);
             return;
         }
-        auto go = [&](auto threads) {
-            constexpr int THREADS = decltype(threads)::value;
-            if constexpr (THREADS > 64)                   // a part has 8 KiB or more
-                if (cut.parts > 1) {
-                    const dim3 grid(cut.parts, p->rows);
-                    if (p->k) logprobs_kernel<T, THREADS, true, true><<<grid, THREADS, 0, ctx->stream>>>(a);
-                    else logprobs_kernel<T, THREADS, false, true><<<grid, THREADS, 0, ctx->stream>>>(a);
-                    logprobs_join_kernel<T><<<p->rows, 256, 0, ctx->stream>>>(a);
-                    return;
-                }
-            if (p->k) logprobs_kernel<T, THREADS, true, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
-            else logprobs_kernel<T, THREADS, false, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
+        auto run = [&](auto threads, auto room) {
+            constexpr int THREADS = decltype(threads)::value, ROOM = decltype(room)::value;
+            if (THREADS > 64 && cut.parts > 1) {
+                logprobs_kernel<T, THREADS, ROOM, THREADS != 64><<<dim3(cut.parts, p->rows), THREADS, 0, ctx->stream>>>(a);
+                logprobs_join_kernel<T><<<p->rows, 256, 0, ctx->stream>>>(a);
+            } else logprobs_kernel<T, THREADS, ROOM, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
         };
         using std::integral_constant;
+        // Room for what is set aside: of rows in no particular order some k (1 + ln(turns)) pieces are, twice that where the lanes' maxima fall badly
+        // (2048 x 131072 with 512 threads: k = 64 122 us in 1024 places, with 512 it overflowed and took 2355); a row of one wavefront fits whole.
+        auto go = [&](auto threads) {
+            if (p->k == 0) run(threads, integral_constant<int, 0>{});
+            else if (p->k <= 64) run(threads, integral_constant<int, 1024>{});
+            else run(threads, integral_constant<int, 2048>{});
+        };
+        // Several work groups to a compute unit, one of which reads while another puts in order: 2048 x 131072 bf16, k = 8, takes 107 us with 512 threads, 110 with
+        // 256 and 123 with 1024, 4096 x 50021 100, 95 and 132, 8192 x 20000 97, 84 and 146.  From k = 65 on thresholds of few wavefronts take long: 512 then
+        // (4096 x 50021, k = 128: 171 us, 241 with 256).  Short rows by a wavefront each once there are rows for all: 8192 x 1000, k = 8, 16.6 us, by four 31.
         const uint64_t bytes = (uint64_t)cut.len * dtype_bytes(p->dtype);
-        if (bytes > 32768) go(integral_constant<int, 1024>{});
-        else if (bytes <= 1024 && (p->k <= 32 || p->vocab <= 128)) go(integral_constant<int, 64>{});
-        else go(integral_constant<int, 256>{});
+        const bool few = p->k <= 32 || p->vocab <= 128;
+        if (bytes > 131072 || (bytes > 32768 && p->k > 64)) go(integral_constant<int, 512>{});
+        else if (bytes > 4096 || !few || (bytes > 1024 && p->rows < 1024)) go(integral_constant<int, 256>{});
+        else if (p->k == 0) run(integral_constant<int, 64>{}, integral_constant<int, 0>{});
+        else run(integral_constant<int, 64>{}, integral_constant<int, 256>{});
     });
     HE_LAUNCHED(ctx);
     return HE_OK;

@@ -17,8 +17,8 @@ __device__ __forceinline__ u64 place_of(float z, uint32_t i) { return (u64)order
 
 // An element's place in the order is one number of 64 bits, its key above the complement of its index, all different.
 
-template <int THREADS> struct TopShared {
-    static constexpr int ROOM = THREADS == 1024 ? 1024 : THREADS == 64 ? 64 : 512, KEEP = 512;
+template <int THREADS, int ROOM_ = THREADS == 1024 ? 1024 : THREADS == 64 ? 64 : 512> struct TopShared {
+    static constexpr int ROOM = ROOM_, KEEP = 512;
     uint4 aside[ROOM];                         // 16 bytes of the row each, and which
     uint32_t which[ROOM];                      // index of the first of its elements, and above 24 bits how many are another's
     u64 keep[KEEP], more, last;                // last: the k-th place
@@ -46,7 +46,7 @@ template <int WAVES> __device__ __forceinline__ float reached_by_all(float high,
 // The k-th largest place of n elements, whose indices begin at `offset`, and in s.keep, in any order, the k places from it on; others(v) is called for every
 // other element.  They are read as often as it takes: a digit of 8 bits at a time is found from the counts of that digit among the elements that agree with the
 // digits before.
-template <class T, int THREADS, class F> __device__ __forceinline__ u64 exact_keep(const typename T::raw* z, uint32_t n, uint32_t k, uint32_t offset, TopShared<THREADS>& s, F&& others) {
+template <class T, int THREADS, int ROOM, class F> __device__ __forceinline__ u64 exact_keep(const typename T::raw* z, uint32_t n, uint32_t k, uint32_t offset, TopShared<THREADS, ROOM>& s, F&& others) {
     const uint32_t t = threadIdx.x;
     u64 prefix = 0;
     uint32_t want = k;                         // how many of the elements that agree with `prefix` are still wanted

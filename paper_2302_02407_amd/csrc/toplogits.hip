@@ -38,7 +38,7 @@ template <class T, int THREADS> __device__ __forceinline__ void exact_row(const 
     const uint32_t t = threadIdx.x;
     const float low = masked_from(a.tau);
     float most = -INFINITY;
-    const u64 prefix = exact_keep<T, THREADS>(z, a.vocab, a.k, 0, s, [&](float v) {
+    const u64 prefix = exact_keep<T>(z, a.vocab, a.k, 0, s, [&](float v) {
         if (!(v <= low)) most = fmaxf(most, v);
     });
     most = group_max<THREADS / 64>(most, s.room);
