@@ -485,7 +485,7 @@ int32_t he_distill_grad(he_ctx* ctx, const he_distill_plan* plan);
  *  - Rows kept in 8 bits: e4m3 codes, and for each 128 columns (the last of what is left) one byte b: a value is its code times
  *    2^(b-127).  2^(b-127) is the smallest power from 2^-110 on at which the block's largest value is at most 448; values are
  *    divided by it, exactly, and rounded to nearest even.  So a value is a number of 16 bits (bfloat16), exactly, and off by at most
- *    2^-4 of itself or 2^-10 of the power.  A block that holds an infinity or a NaN has b = 255 and codes 0x7f: all its values are NaN.
+ *    2^-4 of itself or 2^-10 of the power.  A block of zeros has b = 118 (2^-9).  A block that holds an infinity or a NaN has b = 255 and codes 0x7f: all its values are NaN.
  *    Rows of codes start at multiples of 16 bytes (pointer and ld), and the columns up to the next multiple of 16 are there, as above. */
 
 /* h = x + residual, rounded to dtype (without a residual h = x); mean and variance v of h's row, y = (h - mean) / sqrt(v + eps) * weight +

@@ -251,6 +251,12 @@ def _param_dtype(x, *params):
     return _DTYPE.get(given.pop(), -1) if given else _DTYPE[x.dtype]
 
 
+def _current_raw_stream(device):
+    """The current stream's handle; torch.cuda.current_stream takes longer than a short call."""
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(device) if get else torch.cuda.current_stream(device).cuda_stream
+
+
 def _u32arr(xs):
     xs = [int(x) for x in xs]
     return (C.c_uint32 * max(1, len(xs)))(*xs), len(xs)
@@ -275,7 +281,7 @@ class HEContext:
         if rc != HE_OK:
             raise HEError(rc, self._lib.he_last_error(None).decode())
         self._h = h
-        self._at = self.stream.device.index
+        self._at, self._raw_stream, self._work_sizes = self.stream.device.index, self.stream.cuda_stream, {}
         self._keys = {}   # keeps registered key tensors alive
 
     @classmethod
@@ -656,17 +662,25 @@ class HEContext:
             if t is not None and t.get_device() != self._at:
                 raise ValueError("a tensor on %s, the context's calls run on %s" % (t.device, self.stream.device))
 
-    def _work(self, query, plan, work):
-        """Pointer and size of a call's scratch memory: the caller's, or some that the stream's later work may have again once the call's is done."""
+    def _work(self, work, query, plan, *sizes):
+        """Pointer and size of a call's scratch memory: the caller's, or some that the stream's later work may have again once the call's is done.  `plan()`
+        is asked only for sizes that have not been asked for before."""
         if work is not None:
             if not (work.is_cuda and work.is_contiguous()):
                 raise ValueError("work must be a contiguous CUDA tensor")
-            return work, work.data_ptr(), work.untyped_storage().nbytes() - work.storage_offset() * work.element_size()
-        n = self._work_bytes(query, plan)
+            return work, work.data_ptr(), work.numel() * work.element_size()
+        n = self._work_sizes.get((query, sizes))
+        if n is None:
+            if len(self._work_sizes) >= 4096:
+                self._work_sizes.clear()
+            n = self._work_sizes[query, sizes] = self._work_bytes(getattr(self._lib, query), plan())
         if not n:
             return None, 0, 0
-        with torch.cuda.stream(self.stream):
+        if _current_raw_stream(self._at) == self._raw_stream:
             work = torch.empty(n, dtype=torch.uint8, device=self.stream.device)
+        else:
+            with torch.cuda.stream(self.stream):
+                work = torch.empty(n, dtype=torch.uint8, device=self.stream.device)
         return work, work.data_ptr(), n
 
     def _work_bytes(self, query, plan):
@@ -700,7 +714,7 @@ class HEContext:
         ddx, lddx = _rows(dx, "dx", rows, dim, t)
         head = (rows, dim, d, _param_dtype(h, weight, dweight, dbias), dh, ldh, _dense(stats, "stats", (rows, 4), torch.float32), ddy, lddy, _parameter(weight, "weight", dim, own),
                 dds, ldds, ddx, lddx, _parameter(dweight, "dweight", dim, own), _parameter(dbias, "dbias", dim, own))
-        keep, at, n = self._work(self._lib.he_work_layernorm_grad, _LAYERNORM_GRAD.pack(*head, 0, 0), work)
+        keep, at, n = self._work(work, "he_work_layernorm_grad", lambda: _LAYERNORM_GRAD.pack(*head, 0, 0), rows, dim, dweight is None and dbias is None)
         self._ck(self._lib.he_layernorm_grad(self._h, _LAYERNORM_GRAD.pack(*head, at, n)))
         return dx
 
@@ -735,7 +749,7 @@ class HEContext:
         ddu, lddu = _rows(du, "du", rows, dim, t)
         n = coefs.numel()
         head = (rows, dim, n, d, dc, ldc, de, lde, _dense(coefs, "coefs", (n,), torch.float32), ddy, lddy, ddu, lddu, _dense(dcoefs, "dcoefs", (n,), torch.float32))
-        keep, at, size = self._work(self._lib.he_work_poly_grad_q8, _POLY_GRAD.pack(*head, 0, 0), work)
+        keep, at, size = self._work(work, "he_work_poly_grad_q8", lambda: _POLY_GRAD.pack(*head, 0, 0), rows, dim, n, dcoefs is None)
         self._ck(self._lib.he_poly_grad_q8(self._h, _POLY_GRAD.pack(*head, at, size)))
         return du
 
@@ -755,7 +769,7 @@ class HEContext:
         de, lde = _rows(exponents, "exponents", m, -(-k // 128), _EXPONENTS)
         ddw, lddw = _rows(dw, "dw", n, k, _DTYPE)
         head = (m, n, k, d, o, 1 if accumulate else 0, ddy, lddy, dc, ldc, de, lde, ddw, lddw)
-        keep, at, size = self._work(self._lib.he_work_weight_grad_q8, _WEIGHT_GRAD.pack(*head, 0, 0), work)
+        keep, at, size = self._work(work, "he_work_weight_grad_q8", lambda: _WEIGHT_GRAD.pack(*head, 0, 0), m, n, k, d)
         self._ck(self._lib.he_weight_grad_q8(self._h, _WEIGHT_GRAD.pack(*head, at, size)))
         return dw
 
@@ -773,7 +787,7 @@ class HEContext:
         f32, one = torch.float32, (rows,)
         head = (rows, vocab, k, d, tau, dz, ldz, _dense(tokens, "tokens", one, torch.int32), _dense(logp, "logp", one, f32), _dense(entropy, "entropy", one, f32),
                 _dense(values, "values", (rows, k), f32), _dense(index, "index", (rows, k), torch.int32), _dense(stats, "stats", (rows, 4), f32))
-        keep, at, n = self._work(self._lib.he_work_token_logprobs, _LOGPROBS.pack(*head, 0, 0), work)
+        keep, at, n = self._work(work, "he_work_token_logprobs", lambda: _LOGPROBS.pack(*head, 0, 0), rows, vocab, k, d)
         self._ck(self._lib.he_token_logprobs(self._h, _LOGPROBS.pack(*head, at, n)))
         return logp
 

@@ -72,13 +72,18 @@ static inline const char* refuse_layernorm(const he_layernorm_plan* p) {
     return apart(in, out, {3, 3, 0});
 }
 
-// Parts of the rows, each with a sum of its own for every column
+// Rows whose gradient, and the sums over them, one kernel takes: at least a piece of 8 elements, at most what 512 threads keep in registers
+static inline bool layernorm_one_pass(uint32_t dim) { return dim >= 8 && dim <= 16384; }
+// Parts of the rows, each a work group's with a sum of its own for every column.  More of them keep more rows on the way, and have more to join: 16384 x 4096 bf16 takes
+// 124 us with 256, 103 with 512 and 114 with 1024; 4096 x 16384 81, 96 and 130; 60000 x 100 f32 56, 34 and 28.
 static inline uint32_t layernorm_parts(uint32_t rows, uint32_t dim) {
-    (void)dim;
-    return rows < 256 ? rows : 256;
+    if (!layernorm_one_pass(dim)) return rows < 256 ? rows : 256;
+    const uint32_t slots = dim <= 256 ? 16 : dim <= 1024 ? 4 : 1, groups = (rows + slots - 1) / slots, most = dim <= 512 ? 1024 : dim <= 4096 ? 512 : 256;
+    return groups < most ? groups : most;
 }
+static inline uint32_t layernorm_pitch(uint32_t dim) { return (dim + 7) & ~7u; }
 static inline uint64_t layernorm_grad_work(const he_layernorm_grad_plan* p) {
-    return p->rows && (p->d_dweight || p->d_dbias) ? 8ull * p->dim * layernorm_parts(p->rows, p->dim) : 0;
+    return p->rows && (p->d_dweight || p->d_dbias) ? 8ull * layernorm_pitch(p->dim) * layernorm_parts(p->rows, p->dim) : 0;
 }
 static inline const char* refuse_layernorm_grad(const he_layernorm_grad_plan* p, bool query = false) {
     if (!p) return "null plan";
@@ -128,12 +133,14 @@ static inline const char* refuse_poly(const he_poly_plan* p) {
     return apart(in, out, {1, 0, 0});
 }
 
-// Work groups, each with sums of its own
-static inline uint32_t poly_groups(uint32_t rows, uint32_t dim) {
-    const uint64_t groups = ((uint64_t)rows * blocks_of(dim) + 15) / 16;                // of 256 threads, 16 to a block of 128 columns
-    return groups < 2048 ? (uint32_t)groups : 2048;
+// Work groups of 256 threads, 16 to a block of 128 columns.  What sums nothing has one for every sixteen blocks (16384 x 8192 bf16, degree 3: 112 us; 2048 that go on: 142).  Sums
+// want few, as many as are there at a time: the gradients of that take 127 us with 1024, 129 with 2048 and 177 with 512; of 777 x 10007 f16, degree 7, 19, 24 and 20.
+#define HE_POLY_GROUPS 1024u
+static inline uint32_t poly_groups(uint32_t rows, uint32_t dim, uint32_t most) {
+    const uint64_t groups = ((uint64_t)rows * blocks_of(dim) + 15) / 16;
+    return groups < most ? (uint32_t)groups : most;
 }
-static inline uint64_t poly_grad_work(const he_poly_grad_plan* p) { return p->rows && p->d_dcoefs ? 8ull * p->n_coefs * poly_groups(p->rows, p->dim) : 0; }
+static inline uint64_t poly_grad_work(const he_poly_grad_plan* p) { return p->rows && p->d_dcoefs ? 8ull * p->n_coefs * poly_groups(p->rows, p->dim, HE_POLY_GROUPS) : 0; }
 static inline const char* refuse_poly_grad(const he_poly_grad_plan* p, bool query = false) {
     if (!p) return "null plan";
     if (const char* w = poly_sizes(p->rows, p->dim, p->dtype)) return w;

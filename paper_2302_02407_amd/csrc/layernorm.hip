@@ -14,7 +14,7 @@ struct LnArgs {
 __device__ __forceinline__ float inverse_root(float v) { return v < 0x1p-120f ? 0.0f : 1.0f / sqrtf(v); }
 
 // ROW threads a row, each with V pieces of 8 elements, piece p of a row with thread p % ROW, which stay in registers: everything is read and
-// written once.  Rows of up to 1024 columns take a wavefront each, four to a work group; longer ones a work group.  The mean is a number of 32
+// written once.  Rows of up to 256 columns take 16 lanes each, sixteen to a work group, rows of up to 1024 a wavefront, four to a work group; longer ones a work group.  The mean is a number of 32
 // bits and what that lacks, the sum of the differences from it: so a row far from 0 keeps its variance, whose own sum is of those
 // differences, and its gradient.
 template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void layernorm_kernel(LnArgs a) {
@@ -22,7 +22,7 @@ template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds
     constexpr int GROUP = ROW < 256 ? 256 : ROW, WAVES = ROW / 64;
     __shared__ float room[2 * (GROUP / 64)];
     const u64 row = (u64)blockIdx.x * (GROUP / ROW) + threadIdx.x / ROW;
-    if (row >= a.rows) return;                            // ROW = 64: a whole wavefront, and no barrier follows
+    if (row >= a.rows) return;                            // ROW <= 64: no barrier follows, and sums are among the row's own lanes
     const uint32_t t = threadIdx.x % ROW, dim = a.dim;
     const raw* x = (const raw*)a.x + row * a.ld_x;
     const raw* res = (const raw*)a.res + row * a.ld_res;
@@ -46,7 +46,8 @@ template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds
         for (int i = 0; i < 8; i++) s += h[p][i];
         if (V >= 8) __builtin_amdgcn_sched_barrier(0);    // one piece's loads at a time: the numbers fill the registers
     }
-    float mean = group_sum<WAVES>(s, room) / (float)dim, low, var;
+    auto total = [&](float v) { return ROW == 16 ? row_sum(v) : group_sum<WAVES ? WAVES : 1>(v, room); };
+    float mean = total(s) / (float)dim, low, var;
     auto spread = [&]() {                                 // what the mean lacks, and the variance
         float d1 = 0, d2 = 0;
 #pragma unroll
@@ -73,15 +74,15 @@ template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds
         for (int p = 0; p < V; p++)
 #pragma unroll
             for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(h[p][i]));
-        most = group_max<WAVES>(most, room);
+        most = ROW == 16 ? __builtin_bit_cast(float, row_max(__builtin_bit_cast(int32_t, most))) : group_max<WAVES ? WAVES : 1>(most, room);
         if (most < INFINITY) {
-            const int e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(most));
+            const int e = __builtin_amdgcn_frexp_expf(most);
             s = 0;
 #pragma unroll
             for (int p = 0; p < V; p++)
 #pragma unroll
                 for (int i = 0; i < 8; i++) s += h[p][i] = ldexpf(h[p][i], -e);
-            mean = group_sum<WAVES>(s, room) / (float)dim;
+            mean = total(s) / (float)dim;
             spread();
             r = inverse_root(var + ldexpf(a.eps, -2 * e));
             stats = {ldexpf(mean, e), ldexpf(low, e), ldexpf(r, -e), 0};
@@ -111,7 +112,9 @@ template <class T, class P, bool RES> static void launch_layernorm(const LnArgs&
         layernorm_kernel<T, P, RES, ROW, decltype(v)::value><<<(a.rows + GROUP / ROW - 1) / (GROUP / ROW), GROUP, 0, stream>>>(a);
     };
     using std::integral_constant;
-    if (a.dim <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    if (a.dim <= 128) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (a.dim <= 256) go(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
     else if (a.dim <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     else if (a.dim <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     else if (a.dim <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
@@ -152,12 +155,155 @@ struct LnGradArgs {
     const void *h, *dy, *dsum, *weight;
     const float4* stats;
     void* dx;
-    float* parts;
+    float* sums;                   // [parts][2][pitch]: of dy n and of dy, or null
     u64 ld_h, ld_dy, ld_dsum, ld_dx;
-    uint32_t rows, dim, n_parts;
+    uint32_t rows, dim, parts, pitch;
 };
 
-// A row a work group, in two passes: its two means, then its gradient
+// Everything in one pass: a work group takes every parts-th row (of 64 threads a row: every parts-th four; of 16: every parts-th sixteen), whose two means it needs at once, and keeps the sums
+// over its rows for its columns in registers; they go to memory once, for the join.  The next row is asked for before this one's means are there (but for four
+// pieces a thread, whose registers it does not fit).  Pieces are of 8
+// elements; the last one lies where it still fits the row, and what of it belongs to the one before has a gradient of 0 here and is not written.
+template <class T, class P, bool DSUM, int ROW, int V> __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void layernorm_grad_kernel(LnGradArgs a) {
+    using raw = typename T::raw;
+    constexpr int GROUP = ROW < 256 ? 256 : ROW, SLOTS = GROUP / ROW, WAVES = ROW / 64;
+    constexpr bool AHEAD = V <= 2;
+    __shared__ float room[2][2 * WAVES + 1];
+    const uint32_t t = threadIdx.x % ROW, slot = threadIdx.x / ROW, step = a.parts * SLOTS;
+    const typename P::raw* w = (const typename P::raw*)a.weight;
+    uint32_t base[V], past[V];
+    Eight<P> weight[V];
+    float dw[V][8], db[V][8];
+#pragma unroll
+    for (int p = 0; p < V; p++) {
+        const uint32_t at = (p * ROW + t) * 8;
+        base[p] = min(at, a.dim - 8);
+        past[p] = at - base[p];
+        if (w) weight[p].load(w + base[p]);
+        else {
+            const float ones[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+            weight[p].set(ones);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) dw[p][i] = db[p][i] = 0;
+    }
+    struct Line {
+        Eight<T> h[V], dy[V], dsum[DSUM ? V : 1];
+        float4 stats;
+    };
+    auto load = [&](uint32_t row, Line& l) {
+        const raw *h = (const raw*)a.h + (u64)row * a.ld_h, *dy = (const raw*)a.dy + (u64)row * a.ld_dy, *dsum = (const raw*)a.dsum + (u64)row * a.ld_dsum;
+        l.stats = a.stats[row];
+#pragma unroll
+        for (int p = 0; p < V; p++) {
+            l.h[p].load(h + base[p]);
+            l.dy[p].load(dy + base[p]);
+            if (DSUM && AHEAD) l.dsum[p].load(dsum + base[p]);
+        }
+    };
+    uint32_t row = blockIdx.x * SLOTS + slot, turn = 0;
+    Line now, next;
+    if (AHEAD && row < a.rows) load(row, now);
+    // ROW <= 64: a wavefront has rows of its own and no barrier; otherwise there is one slot, and all of the work group are here as often
+    for (; row < a.rows; row += step, turn ^= 1) {
+        if (!AHEAD) load(row, now);
+        else if (row + step < a.rows) load(row + step, next);
+        const float mean = now.stats.x, low = now.stats.y, r = now.stats.z;
+        float s1 = 0, s2 = 0;
+#pragma unroll
+        for (int p = 0; p < V; p++) {
+            if (past[p])
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if ((uint32_t)i < past[p]) now.dy[p].v[i / Vec<T>::N].set(i % Vec<T>::N, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float d = now.dy[p][i], n = (now.h[p][i] - mean - low) * r, g = d * weight[p][i];
+                dw[p][i] = fmaf(d, n, dw[p][i]);
+                db[p][i] += d;
+                s1 += g;
+                s2 = fmaf(g, n, s2);
+            }
+        }
+        s1 = ROW == 16 ? row_sum(s1) : wave_sum(s1);
+        s2 = ROW == 16 ? row_sum(s2) : wave_sum(s2);
+        if (WAVES > 1) {                                  // two rooms in turn: one barrier
+            if ((threadIdx.x & 63) == 0) {
+                room[turn][threadIdx.x >> 6] = s1;
+                room[turn][WAVES + (threadIdx.x >> 6)] = s2;
+            }
+            __syncthreads();
+            s1 = room[turn][0];
+            s2 = room[turn][WAVES];
+#pragma unroll
+            for (int i = 1; i < WAVES; i++) {
+                s1 += room[turn][i];
+                s2 += room[turn][WAVES + i];
+            }
+        }
+        s1 /= (float)a.dim;
+        s2 /= (float)a.dim;
+        raw* dx = (raw*)a.dx + (u64)row * a.ld_dx;
+#pragma unroll
+        for (int p = 0; p < V; p++) {
+            float y[8];
+            if (DSUM && !AHEAD) now.dsum[p].load((const raw*)a.dsum + (u64)row * a.ld_dsum + base[p]);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float n = (now.h[p][i] - mean - low) * r, g = now.dy[p][i] * weight[p][i];
+                y[i] = fmaf(r, g - s1 - n * s2, DSUM ? now.dsum[p][i] : 0.0f);
+            }
+            if (past[p] == 0) {
+                Eight<T> out;
+                out.set(y);
+#pragma unroll
+                for (int v = 0; v < Eight<T>::VECS; v++) out.v[v].store_past(dx + base[p] + v * Vec<T>::N);
+            } else
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if ((uint32_t)i >= past[p]) dx[base[p] + i] = from_float<T>(y[i]);
+        }
+        if (AHEAD) now = next;
+    }
+    if (!a.sums) return;
+    float* to = a.sums + (u64)blockIdx.x * 2 * a.pitch;
+    if constexpr (SLOTS > 1) {                            // the wavefronts' sums, one after another
+        __shared__ float sums[2][V * ROW * 8];
+#pragma unroll
+        for (int k = 0; k < SLOTS; k++) {
+            if (slot == (uint32_t)k)
+#pragma unroll
+                for (int p = 0; p < V; p++)
+                    if (past[p] < 8)
+#pragma unroll
+                        for (int i = 0; i < 8; i++)
+                            if ((uint32_t)i >= past[p]) {
+                                sums[0][base[p] + i] = k ? sums[0][base[p] + i] + dw[p][i] : dw[p][i];
+                                sums[1][base[p] + i] = k ? sums[1][base[p] + i] + db[p][i] : db[p][i];
+                            }
+            __syncthreads();
+        }
+        for (uint32_t i = threadIdx.x; i < 2 * a.dim; i += GROUP) {
+            const uint32_t which = i >= a.dim, column = i - which * a.dim;
+            to[which * a.pitch + column] = sums[which][column];
+        }
+    } else
+#pragma unroll
+        for (int p = 0; p < V; p++) {
+            if (past[p] == 0) {
+                __builtin_memcpy(to + base[p], dw[p], 32);
+                __builtin_memcpy(to + a.pitch + base[p], db[p], 32);
+            } else
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if ((uint32_t)i >= past[p]) {
+                        to[base[p] + i] = dw[p][i];
+                        to[a.pitch + base[p] + i] = db[p][i];
+                    }
+        }
+}
+
+// Rows too long for a work group's registers, or shorter than a piece: a row a work group, in two passes, its two means, then its gradient
 template <class T, class P> __global__ __launch_bounds__(256) void layernorm_dx_kernel(LnGradArgs a) {
     using raw = typename T::raw;
     __shared__ float room[8];
@@ -199,12 +345,12 @@ template <class T, class P> __global__ __launch_bounds__(256) void layernorm_dx_
     }
 }
 
-// Sums over a part of the rows, 512 columns a work group: each wavefront every fourth row, their sums joined in order
+// Their sums over a part of the rows, 512 columns a work group: each wavefront every fourth row, their sums joined in order
 template <class T> __global__ __launch_bounds__(256) void layernorm_columns_kernel(LnGradArgs a) {
     using raw = typename T::raw;
     __shared__ float sums[4][2][512];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = blockIdx.x * 512 + lane * 8;
-    const uint32_t from = (u64)a.rows * blockIdx.y / a.n_parts, to = (u64)a.rows * (blockIdx.y + 1) / a.n_parts;
+    const uint32_t from = (u64)a.rows * blockIdx.y / a.parts, to = (u64)a.rows * (blockIdx.y + 1) / a.parts;
     float dw[8] = {}, db[8] = {};
     if (at < a.dim)
         for (uint32_t row = from + wave; row < to; row += 4) {
@@ -226,21 +372,46 @@ template <class T> __global__ __launch_bounds__(256) void layernorm_columns_kern
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < 1024; i += 256) {
         const uint32_t which = i >> 9, c = i & 511, column = blockIdx.x * 512 + c;
-        if (column < a.dim) a.parts[((u64)blockIdx.y * 2 + which) * a.dim + column] = sums[0][which][c] + sums[1][which][c] + sums[2][which][c] + sums[3][which][c];
+        if (column < a.dim) a.sums[((u64)blockIdx.y * 2 + which) * a.pitch + column] = sums[0][which][c] + sums[1][which][c] + sums[2][which][c] + sums[3][which][c];
     }
 }
 
-// The parts' sums, in order
-template <class P> __global__ __launch_bounds__(256) void layernorm_join_kernel(const float* parts, uint32_t n_parts, uint32_t dim, void* dweight, void* dbias) {
-    const uint32_t column = blockIdx.x * 256 + threadIdx.x;
-    if (column >= dim) return;
-    float dw = 0, db = 0;
-    for (uint32_t p = 0; p < n_parts; p++) {
-        dw += parts[(u64)p * 2 * dim + column];
-        db += parts[((u64)p * 2 + 1) * dim + column];
-    }
-    if (dweight) ((typename P::raw*)dweight)[column] = from_float<P>(dw);
-    if (dbias) ((typename P::raw*)dbias)[column] = from_float<P>(db);
+// The parts' sums, in a fixed order: 32 threads four columns, each every 32nd part
+template <class P> __global__ __launch_bounds__(256) void layernorm_join_kernel(const float* parts, uint32_t n_parts, uint32_t dim, uint32_t pitch, void* dweight, void* dbias) {
+    typedef float v4f __attribute__((ext_vector_type(4)));
+    __shared__ v4f sums[32][8];
+    const uint32_t lane = threadIdx.x / 8, at = (blockIdx.x * 8 + threadIdx.x % 8) * 4;      // of 2 * pitch
+    v4f x = {0, 0, 0, 0};
+    if (at < 2 * pitch)
+#pragma unroll 4
+        for (uint32_t p = lane; p < n_parts; p += 32) x += *(const v4f*)(parts + (u64)p * 2 * pitch + at);
+    sums[lane][threadIdx.x % 8] = x;
+    __syncthreads();
+    if (lane || at >= 2 * pitch) return;
+#pragma unroll
+    for (int j = 1; j < 32; j++) x += sums[j][threadIdx.x];
+    const uint32_t column = at % pitch;                   // a multiple of 4, as the pitch is
+    typename P::raw* to = (typename P::raw*)(at < pitch ? dweight : dbias);
+    if (!to) return;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        if (column + i < dim) to[column + i] = from_float<P>(x[i]);
+}
+
+template <class T, class P, bool DSUM> static void launch_layernorm_grad(const LnGradArgs& a, hipStream_t stream) {
+    auto go = [&](auto row, auto v) {
+        constexpr int ROW = decltype(row)::value;
+        layernorm_grad_kernel<T, P, DSUM, ROW, decltype(v)::value><<<a.parts, ROW < 256 ? 256 : ROW, 0, stream>>>(a);
+    };
+    using std::integral_constant;
+    if (a.dim <= 128) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (a.dim <= 256) go(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (a.dim <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (a.dim <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else if (a.dim <= 8192) go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    else go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
 }
 
 extern "C" int32_t he_work_layernorm_grad(const he_ctx* ctx, const he_layernorm_grad_plan* p, uint64_t* h_bytes) {
@@ -259,16 +430,19 @@ extern "C" int32_t he_layernorm_grad(he_ctx* ctx, const he_layernorm_grad_plan* 
     const bool sums = p->d_dweight || p->d_dbias;
     const OnDevice device(ctx);
     HE_HIP(ctx, device.status);
-    const LnGradArgs a = {p->d_h, p->d_dy, p->d_dsum, p->d_weight, (const float4*)p->d_stats, p->d_dx, (float*)p->d_work, p->ld_h, p->ld_dy, p->ld_dsum, p->ld_dx,
-                          p->rows, p->dim, p->rows ? layernorm_parts(p->rows, p->dim) : 0};
+    const LnGradArgs a = {p->d_h, p->d_dy, p->d_dsum, p->d_weight, (const float4*)p->d_stats, p->d_dx, sums ? (float*)p->d_work : nullptr, p->ld_h, p->ld_dy, p->ld_dsum, p->ld_dx,
+                          p->rows, p->dim, p->rows ? layernorm_parts(p->rows, p->dim) : 0, layernorm_pitch(p->dim)};
     with_types(p->dtype, p->param_dtype, [&](auto t, auto w) {
         using T = decltype(t);
         using P = decltype(w);
-        if (sums) {                                       // before dx, which may lie on dy
-            if (a.rows) layernorm_columns_kernel<T><<<dim3((a.dim + 511) / 512, a.n_parts), 256, 0, ctx->stream>>>(a);
-            layernorm_join_kernel<P><<<(a.dim + 255) / 256, 256, 0, ctx->stream>>>(a.parts, a.n_parts, a.dim, p->d_dweight, p->d_dbias);
+        if (a.rows && layernorm_one_pass(a.dim)) {
+            if (a.dsum) launch_layernorm_grad<T, P, true>(a, ctx->stream);
+            else launch_layernorm_grad<T, P, false>(a, ctx->stream);
+        } else if (a.rows) {                              // sums before dx, which may lie on dy
+            if (sums) layernorm_columns_kernel<T><<<dim3((a.dim + 511) / 512, a.parts), 256, 0, ctx->stream>>>(a);
+            layernorm_dx_kernel<T, P><<<a.rows, 256, 0, ctx->stream>>>(a);
         }
-        if (a.rows) layernorm_dx_kernel<T, P><<<a.rows, 256, 0, ctx->stream>>>(a);
+        if (sums) layernorm_join_kernel<P><<<(2 * a.pitch + 31) / 32, 256, 0, ctx->stream>>>((const float*)p->d_work, a.parts, a.dim, a.pitch, p->d_dweight, p->d_dbias);
     });
     HE_LAUNCHED(ctx);
     return HE_OK;

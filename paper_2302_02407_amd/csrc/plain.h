@@ -69,6 +69,15 @@ template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) {
 __device__ __forceinline__ float wave_sum(float v) { return wave_reduce(v, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float wave_max(float v) { return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
 
+// Over each row of 16 lanes
+__device__ __forceinline__ float row_sum(float v) {
+    const auto turned = [&](auto ctrl) { return __builtin_bit_cast(float, rotated<decltype(ctrl)::value>(__builtin_bit_cast(int32_t, v))); };
+    v += turned(std::integral_constant<int, 0x128>{});
+    v += turned(std::integral_constant<int, 0x124>{});
+    v += turned(std::integral_constant<int, 0x122>{});
+    return v + turned(std::integral_constant<int, 0x121>{});
+}
+
 // Over a work group of WAVES wavefronts: every thread gets the result, in a fixed order.  `room`: WAVES floats that nothing else uses
 // between the two barriers.
 template <int WAVES, class F> __device__ __forceinline__ float group_reduce(float v, float* room, F f) {
@@ -85,8 +94,13 @@ template <int WAVES, class F> __device__ __forceinline__ float group_reduce(floa
 template <int WAVES> __device__ __forceinline__ float group_sum(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return a + b; }); }
 template <int WAVES> __device__ __forceinline__ float group_max(float v, float* room) { return group_reduce<WAVES>(v, room, [](float a, float b) { return fmaxf(a, b); }); }
 
-// Two sums at once; `room`: 2 * WAVES floats
+// Two sums at once; `room`: 2 * WAVES floats.  WAVES = 0: over rows of 16 lanes
 template <int WAVES> __device__ __forceinline__ void group_sum2(float& x, float& y, float* room) {
+    if constexpr (WAVES == 0) {
+        x = row_sum(x);
+        y = row_sum(y);
+        return;
+    }
     x = wave_sum(x);
     y = wave_sum(y);
     if (WAVES == 1) return;

@@ -143,6 +143,16 @@ def test_grad(ctx, dtype, params, rows, dim):
         check_grad(run_grad(ctx, x, 1e-5, dy, w_, ds_, params, dim + n, n, over, sums), x, 1e-5, dy, w_, ds_, params)
 
 
+@pytest.mark.parametrize("rows,dim", [(17000, 20), (16500, 200), (1030, 500), (2100, 700), (1100, 1500), (600, 5000), (300, 12001)])
+@pytest.mark.parametrize("dtype,params", T.PAIRS[:4:3])
+def test_grad_of_more_rows_than_parts(ctx, dtype, params, rows, dim):
+    g = T.rng(rows)
+    x, ds, w, _ = inputs(rows, dim, dtype, params, dim)
+    dy = torch.randn((rows, dim), generator=g).to(dtype)
+    for n, (ds_, over) in enumerate(((ds, "dsum"), (None, "dy"), (ds, None))):
+        check_grad(run_grad(ctx, x, 1e-5, dy, w, ds_, params, dim + n, n, over), x, 1e-5, dy, w, ds_, params)
+
+
 def test_grad_of_hard_rows(ctx):
     """Rows far from 0, whose normed values need what the mean lacks; and rows without a variance, which have a gradient by the bias alone."""
     g = T.rng(3)

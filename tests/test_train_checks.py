@@ -201,7 +201,7 @@ int main() {
     if (weight_cut(0, 5, 7, HE_F32).parts != 1 || weight_cut(0, 5, 7, HE_F32).per != 0) { bad++; printf("cut of no rows\n"); }
     for (uint32_t rows : sizes)
         for (uint32_t dim : sizes)
-            if (dim <= HE_DIM_MAX && (layernorm_parts(rows, dim) < 1 || layernorm_parts(rows, dim) > rows || layernorm_parts(rows, dim) > 65535 || poly_groups(rows, dim) < 1)) { bad++; printf("parts of %u %u\n", rows, dim); }
+            if (dim <= HE_DIM_MAX && (layernorm_parts(rows, dim) < 1 || layernorm_parts(rows, dim) > rows || layernorm_parts(rows, dim) > 65535 || poly_groups(rows, dim, 1024) < 1)) { bad++; printf("parts of %u %u\n", rows, dim); }
     printf("%d bad\n", bad);
     return bad != 0;
 }

@@ -62,6 +62,7 @@ def keep(u):
             e = torch.where(some & (F8_MAX * 2.0 ** (e - 1) >= most) & (e > -110), e - 1, e)
         for _ in range(2):
             e = torch.where(some & (F8_MAX * 2.0 ** e < most), e + 1, e)
+        e = torch.where(most == 0, -9.0, e)                   # zeros
         scaled = part / (2.0 ** e)[:, None]
         codes.append(torch.where(fine[:, None], scaled.float().to(F8).float(), math.nan).to(F8))
         bytes_.append(torch.where(fine, e + 127, 255.0).to(torch.uint8))
