@@ -169,6 +169,7 @@ static inline const char* refuse_poly_grad(const he_poly_grad_plan* p, bool quer
 // Tiles of `side` rows by as many columns of dw, the sum over the rows of dy in `parts` parts of `per` steps of 32 rows, joined by a second kernel
 struct WeightCut {
     uint32_t side, parts, per;
+    bool ahead;                // small tiles of bf16, at most two to a compute unit: rows are asked for four steps ahead, for which three have no registers (65536 x 256 x 256: 28 us, 30)
 };
 // The cut that costs least, by what was measured of steps and joins (bf16; in fifths of a step of a compute unit's three small tiles, 0.19 us): a step of a
 // unit takes 5.5 with a tile of 256 x 256, and 3, 4, 5 with one, two, three of 128 x 128; a step of f16 1.4 times that and one of f32 2 times, their matrix
@@ -176,7 +177,7 @@ struct WeightCut {
 // on eleven shapes from 500 x 100 x 100 to 65536 x 256 x 256; shapes between go by the same line.
 static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k, int32_t dtype) {
     const uint64_t steps = (m + 31) / 32, kind = dtype == HE_BF16 ? 10 : dtype == HE_F16 ? 14 : 20;
-    WeightCut best = {128, 1, (uint32_t)steps};
+    WeightCut best = {128, 1, (uint32_t)steps, false};
     if (steps == 0) return best;
     uint64_t least = ~0ull;
     for (uint32_t side = 128; side <= 256; side += 128) {
@@ -188,7 +189,7 @@ static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k, int32_t d
             const uint64_t per = (steps + want - 1) / want, parts = (steps + per - 1) / per, each = (tiles * parts + 255) / 256;
             const uint64_t step = side == 256 ? 11 * each : 2 * (each / 3 * 5 + (each % 3 ? each % 3 + 2 : 0));
             const uint64_t cost = per * step * kind + (parts > 1 ? 320 + parts * n * k / 5350 : 0);          // in twentieths
-            if (cost < least) least = cost, best = {side, (uint32_t)parts, (uint32_t)per};
+            if (cost < least) least = cost, best = {side, (uint32_t)parts, (uint32_t)per, each <= 2};
         }
     }
     return best;

@@ -256,12 +256,15 @@ template <class T> struct ShortRow {
 // Which tile a work group owns.  Work groups go to the 8 dies in turn and each die has a cache of its own, so die x takes the x-th
 // eighth of the tiles, in stripes of 8 tiles of the second operand: its 32 compute units then work on about 8 x 4 tiles at a time, which read
 // 12 strips instead of 33.
-__device__ __forceinline__ bool tile_of(uint32_t tiles_n, uint32_t tiles_m, uint32_t& n, uint32_t& m) {
-    const uint32_t all = tiles_n * tiles_m, each = (all + 7) / 8, t = blockIdx.x % 8 * each + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= each || t >= all) return false;
+__device__ __forceinline__ void tile_in_order(uint32_t t, uint32_t tiles_n, uint32_t tiles_m, uint32_t& n, uint32_t& m) {
     const uint32_t stripe = t / (8 * tiles_n), high = min(8u, tiles_m - 8 * stripe), r = t - stripe * 8 * tiles_n;
     m = 8 * stripe + r % high;
     n = r / high;
+}
+__device__ __forceinline__ bool tile_of(uint32_t tiles_n, uint32_t tiles_m, uint32_t& n, uint32_t& m) {
+    const uint32_t all = tiles_n * tiles_m, each = (all + 7) / 8, t = blockIdx.x % 8 * each + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= each || t >= all) return false;
+    tile_in_order(t, tiles_n, tiles_m, n, m);
     return true;
 }
 

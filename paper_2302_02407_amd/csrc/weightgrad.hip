@@ -15,7 +15,7 @@ struct WeightArgs {
     void* dw;
     u64 ld_dy, ld_codes, ld_exponents, ld_dw;
     uint32_t m, n, k;
-    uint32_t per;              // steps of 32 rows a part takes
+    uint32_t parts, per;       // steps of 32 rows a part takes
     u64 part;                  // elements from one part's sums to the next's
     int32_t out_dtype;
     uint32_t accumulate;
@@ -55,7 +55,7 @@ typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 // turns each row's into bfloat16 by that row's power, and puts pairs of rows together: the fragments of four squares, in which lane l
 // holds columns 4 l .. 4 l + 3, so that results are written 16 bytes a lane.  Rows r and r + 8 go to the two halves of a wavefront
 // and are 128 bytes, half of the banks, apart.
-template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __launch_bounds__(64 * WN * WK, 2) void weight_grad_kernel(WeightArgs a) {
+template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __global__ __launch_bounds__(64 * WN * WK, 2) void weight_grad_kernel(WeightArgs a) {
     using raw = typename T::raw;
     using G = WeightTile<T, WN, WK, TN, TK>;
     using codes_t = std::conditional_t<TK == 4, uint32_t, uint16_t>;         // a lane's columns of a row
@@ -63,13 +63,18 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
     extern __shared__ __align__(1024) uint8_t lds[];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane & 31, g = lane >> 5;
     const uint32_t wn = wave / WK, wk = wave % WK;
+    // All tiles of a part, then those of the next: a die takes an eighth of that, and its cache holds the rows that the tiles of a part share.  (With the parts on
+    // another axis of the grid and fewer tiles than dies, some dies had nothing: 65536 x 256 x 256 bf16 43 us, 28 now.)
     uint32_t n_own, k0;
-    if (!tile_of((a.n + G::BN - 1) / G::BN, (a.k + G::BK - 1) / G::BK, n_own, k0)) return;
+    const uint32_t tiles_n = (a.n + G::BN - 1) / G::BN, tiles_k = (a.k + G::BK - 1) / G::BK, tiles = tiles_n * tiles_k, all = tiles * a.parts, each = (all + 7) / 8;
+    const uint32_t item = blockIdx.x % 8 * each + blockIdx.x / 8, part = item / tiles;
+    if (blockIdx.x / 8 >= each || item >= all) return;
+    tile_in_order(item - part * tiles, tiles_n, tiles_k, n_own, k0);
     n_own *= G::BN;
     k0 *= G::BK;
     // the last tile begins earlier, so that all its columns are there; the rows of dw that another one has are left to that
     const uint32_t n0 = NARROW ? 0 : min(n_own, a.n - G::BN);
-    const uint32_t first = blockIdx.y * a.per * 32, steps = min((a.m - first + 31) / 32, a.per);
+    const uint32_t first = part * a.per * 32, steps = min((a.m - first + 31) / 32, a.per);
     const uint32_t codes_end = (a.k + 15) / 16 * 16, blocks = (a.k + 127) / 128;
 
     struct Stage {
@@ -239,7 +244,6 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
     // What a wavefront has written to LDS is there for the others, and what it has asked for has come
     auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-    Stage st;
     // between two matrix instructions a few of what turns the next half's codes
     auto interleave = [&]() {
 #pragma unroll
@@ -248,12 +252,18 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
             __builtin_amdgcn_sched_group_barrier(0x002, 8 / TN, 0);
         }
     };
-    place(first + (steps - 1) * 32);
-    load(0, st);
-    cut(st);
-    store(0, st);
-    if (steps > 1) place(first);
-    load(1, st);
+    // rows are asked for AHEAD steps before they go to LDS: step j's (from 1 on) are in stage (j - 1) % AHEAD until then
+    Stage st[AHEAD];
+    {
+        Stage zero;
+        place(first + (steps - 1) * 32);
+        load(0, zero);
+        if (steps > 1) place(first);
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) load(j + 1, st[j]);
+        cut(zero);
+        store(0, zero);
+    }
     meet();
     if constexpr (PARTS == 1) {
         // Three halves are on their way: one is multiplied while the next is turned into bfloat16 and the one behind that is read; so a step's
@@ -262,54 +272,49 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
         Kept k_one, k_two;
         read(0, 0, one);
         read(0, 1, two);
-        auto body = [&](uint32_t b, Stage& now, uint32_t ahead) {
-            Half half, next;
-            read(b + 1, 0, half);
-            multiply(one, k_one);
-            convert(two, k_two);
-            interleave();
-            store(b + 2, now);
-            load(b + ahead, now);
-            read(b + 1, 1, next);
-            multiply(two, k_two);
-            convert(half, k_one);
-            interleave();
-            one = half;
-            two = next;
-            meet();
-        };
-        if constexpr (G::THREADS > 256) {                 // rows are asked for two steps ahead
-            Stage other;
-            load(2, other);
-            store(1, st);
-            load(3, st);
-            convert(one, k_one);
-            meet();
-            for (uint32_t b = 0; b < steps; b += 2) {
-                body(b, other, 4);
-                if (b + 1 < steps) body(b + 1, st, 4);
+        store(1, st[0]);
+        load(AHEAD + 1, st[0]);
+        convert(one, k_one);
+        meet();
+        for (uint32_t b0 = 0; b0 < steps; b0 += AHEAD)
+#pragma unroll
+            for (int d = 0; d < AHEAD; d++) {
+                const uint32_t b = b0 + d;
+                if (d && b >= steps) break;
+                Stage& now = st[(d + 1) % AHEAD];
+                Half half, next;
+                read(b + 1, 0, half);
+                multiply(one, k_one);
+                convert(two, k_two);
+                interleave();
+                store(b + 2, now);
+                load(b + 2 + AHEAD, now);
+                read(b + 1, 1, next);
+                multiply(two, k_two);
+                convert(half, k_one);
+                interleave();
+                one = half;
+                two = next;
+                meet();
             }
-        } else {                                          // one step: three work groups share a compute unit then
-            store(1, st);
-            load(2, st);
-            convert(one, k_one);
-            meet();
-            for (uint32_t b = 0; b < steps; b++) body(b, st, 3);
-        }
     } else {                                              // several matrix products to a half hide its reads
         Half half;
         Kept kept;
-        for (uint32_t b = 0; b < steps; b++) {
-            read(b, 0, half);
-            convert(half, kept);
-            multiply(half, kept);
-            store(b + 1, st);                             // the other buffer: its last reads lie before the last barrier
-            read(b, 1, half);
-            convert(half, kept);
-            multiply(half, kept);
-            load(b + 2, st);
-            meet();
-        }
+        for (uint32_t b0 = 0; b0 < steps; b0 += AHEAD)
+#pragma unroll
+            for (int d = 0; d < AHEAD; d++) {
+                const uint32_t b = b0 + d;
+                if (d && b >= steps) break;
+                read(b, 0, half);
+                convert(half, kept);
+                multiply(half, kept);
+                store(b + 1, st[d]);                      // the other buffer: its last reads lie before the last barrier
+                read(b, 1, half);
+                convert(half, kept);
+                multiply(half, kept);
+                load(b + 1 + AHEAD, st[d]);
+                meet();
+            }
     }
     // element e of a square: row 8 (e / 4) + 4 g + e % 4, square j column TK l + j
     const uint32_t k = k0 + (wk * 32 + l) * TK;
@@ -334,7 +339,7 @@ template <class T, int WN, int WK, int TN, int TK, bool NARROW> __global__ __lau
             float x[TK];
 #pragma unroll
             for (int j = 0; j < TK; j++) x[j] = acc[i][j][e];
-            const u64 at = blockIdx.y * a.part + n * a.ld_dw + k;
+            const u64 at = part * a.part + n * a.ld_dw + k;
             if (n >= n_own && n < a.n && k < a.k) {
                 if (a.out_dtype == HE_F32) put(f32_t{}, at, x);
                 else if (a.out_dtype == HE_BF16) put(bf16_t{}, at, x);
@@ -376,12 +381,13 @@ template <class O, int LANES> __global__ __launch_bounds__(256) void weight_join
             if (at + e < k) to[e] = from_float<O>(accumulate ? to_float<O>(to[e]) + x[e] : x[e]);
 }
 
-template <class T, int WN, int WK, int TN, int TK, bool NARROW> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
+template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> static hipError_t launch_weight_grad(const WeightArgs& a, const WeightCut& c, hipStream_t stream) {
     using G = WeightTile<T, WN, WK, TN, TK>;
-    const auto kernel = weight_grad_kernel<T, WN, WK, TN, TK, NARROW>;
+    const auto kernel = weight_grad_kernel<T, WN, WK, TN, TK, AHEAD, NARROW>;
     const hipError_t ready = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
     if (ready != hipSuccess) return ready;
-    kernel<<<dim3((((a.n + G::BN - 1) / G::BN) * ((a.k + G::BK - 1) / G::BK) + 7) / 8 * 8, c.parts), G::THREADS, G::LDS, stream>>>(a);
+    const uint64_t all = (uint64_t)((a.n + G::BN - 1) / G::BN) * ((a.k + G::BK - 1) / G::BK) * a.parts;      // at most 2^20 tiles, and parts only of far fewer
+    kernel<<<(uint32_t)((all + 7) / 8 * 8), G::THREADS, G::LDS, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -403,7 +409,7 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     HE_HIP(ctx, device.status);
     const WeightCut c = weight_cut(p->m, p->n, p->k, p->dtype);
     const bool joined = p->m == 0 || c.parts > 1;
-    WeightArgs a = {p->d_dy, p->d_codes, p->d_exponents, p->d_dw, p->ld_dy, p->ld_codes, p->ld_exponents, p->ld_dw, p->m, p->n, p->k, c.per, 0, p->out_dtype, p->accumulate};
+    WeightArgs a = {p->d_dy, p->d_codes, p->d_exponents, p->d_dw, p->ld_dy, p->ld_codes, p->ld_exponents, p->ld_dw, p->m, p->n, p->k, c.parts, c.per, 0, p->out_dtype, p->accumulate};
     if (joined) {
         a.dw = p->d_work;
         a.ld_dw = weight_pitch(p->k);
@@ -414,9 +420,15 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     hipError_t err = hipSuccess;
     if (p->m) with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
-        if (c.side == 256) err = launch_weight_grad<T, 4, 2, 2, 4, false>(a, c, ctx->stream);
-        else if (p->n >= 128) err = launch_weight_grad<T, 2, 2, 2, 2, false>(a, c, ctx->stream);
-        else err = launch_weight_grad<T, 2, 2, 2, 2, true>(a, c, ctx->stream);
+        constexpr int MANY = Parts<T>::N < 3 ? 4 : 2;     // stages that the registers have room for at two work groups to a compute unit
+        auto small = [&](auto narrow) {
+            constexpr bool N = decltype(narrow)::value;
+            if constexpr (Parts<T>::N == 1)
+                if (!c.ahead) return launch_weight_grad<T, 2, 2, 2, 2, 1, N>(a, c, ctx->stream);
+            return launch_weight_grad<T, 2, 2, 2, 2, MANY, N>(a, c, ctx->stream);
+        };
+        if (c.side == 256) err = launch_weight_grad<T, 4, 2, 2, 4, Parts<T>::N == 1 ? 2 : 1, false>(a, c, ctx->stream);
+        else err = p->n >= 128 ? small(std::false_type{}) : small(std::true_type{});
     });
     HE_HIP(ctx, err);
     if (joined) with_dtype(p->out_dtype, [&](auto o) {
