@@ -267,25 +267,28 @@ template <class T, class P, bool DSUM, int ROW, int V> __global__ __launch_bound
     }
     if (!a.sums) return;
     float* to = a.sums + (u64)blockIdx.x * 2 * a.pitch;
-    if constexpr (SLOTS > 1) {                            // the wavefronts' sums, one after another
-        __shared__ float sums[2][V * ROW * 8];
+    if constexpr (SLOTS > 1) {                            // of a wavefront's rows, then of the wavefronts, in order
+        __shared__ float sums[4][2][V * ROW * 8];
+        const uint32_t wave = threadIdx.x >> 6;
 #pragma unroll
-        for (int k = 0; k < SLOTS; k++) {
-            if (slot == (uint32_t)k)
+        for (int p = 0; p < V; p++)
 #pragma unroll
-                for (int p = 0; p < V; p++)
-                    if (past[p] < 8)
-#pragma unroll
-                        for (int i = 0; i < 8; i++)
-                            if ((uint32_t)i >= past[p]) {
-                                sums[0][base[p] + i] = k ? sums[0][base[p] + i] + dw[p][i] : dw[p][i];
-                                sums[1][base[p] + i] = k ? sums[1][base[p] + i] + db[p][i] : db[p][i];
-                            }
-            __syncthreads();
-        }
+            for (int i = 0; i < 8; i++) {
+                if constexpr (ROW == 16) {
+                    dw[p][i] += __shfl_xor(dw[p][i], 16);
+                    db[p][i] += __shfl_xor(db[p][i], 16);
+                    dw[p][i] += __shfl_xor(dw[p][i], 32);
+                    db[p][i] += __shfl_xor(db[p][i], 32);
+                }
+                if ((threadIdx.x & 63) < ROW && (uint32_t)i >= past[p]) {
+                    sums[wave][0][base[p] + i] = dw[p][i];
+                    sums[wave][1][base[p] + i] = db[p][i];
+                }
+            }
+        __syncthreads();
         for (uint32_t i = threadIdx.x; i < 2 * a.dim; i += GROUP) {
             const uint32_t which = i >= a.dim, column = i - which * a.dim;
-            to[which * a.pitch + column] = sums[which][column];
+            to[which * a.pitch + column] = sums[0][which][column] + sums[1][which][column] + sums[2][which][column] + sums[3][which][column];
         }
     } else
 #pragma unroll
@@ -304,9 +307,9 @@ template <class T, class P, bool DSUM, int ROW, int V> __global__ __launch_bound
 }
 
 // Rows too long for a work group's registers, or shorter than a piece: a row a work group, in two passes, its two means, then its gradient
-template <class T, class P> __global__ __launch_bounds__(256) void layernorm_dx_kernel(LnGradArgs a) {
+template <class T, class P, int THREADS> __global__ __launch_bounds__(THREADS) void layernorm_dx_kernel(LnGradArgs a) {
     using raw = typename T::raw;
-    __shared__ float room[8];
+    __shared__ float room[2 * (THREADS / 64)];
     const u64 row = blockIdx.x;
     const raw *h = (const raw*)a.h + row * a.ld_h, *dy = (const raw*)a.dy + row * a.ld_dy, *dsum = (const raw*)a.dsum + row * a.ld_dsum;
     const typename P::raw* w = (const typename P::raw*)a.weight;
@@ -323,7 +326,7 @@ template <class T, class P> __global__ __launch_bounds__(256) void layernorm_dx_
         }
     };
     float s1 = 0, s2 = 0;
-    for (uint32_t at = threadIdx.x * 8; at < a.dim; at += 2048) {
+    for (uint32_t at = threadIdx.x * 8; at < a.dim; at += THREADS * 8) {
         float n[8], g[8];
         piece(at, n, g);
 #pragma unroll
@@ -332,10 +335,10 @@ template <class T, class P> __global__ __launch_bounds__(256) void layernorm_dx_
             s2 = fmaf(g[i], n[i], s2);
         }
     }
-    group_sum2<4>(s1, s2, room);
+    group_sum2<THREADS / 64>(s1, s2, room);
     s1 /= (float)a.dim;
     s2 /= (float)a.dim;
-    for (uint32_t at = threadIdx.x * 8; at < a.dim; at += 2048) {
+    for (uint32_t at = threadIdx.x * 8; at < a.dim; at += THREADS * 8) {
         float n[8], g[8], more[8];
         piece(at, n, g);
         if (a.dsum) load8<T>(dsum, at, a.dim, more);
@@ -440,7 +443,8 @@ extern "C" int32_t he_layernorm_grad(he_ctx* ctx, const he_layernorm_grad_plan* 
             else launch_layernorm_grad<T, P, false>(a, ctx->stream);
         } else if (a.rows) {                              // sums before dx, which may lie on dy
             if (sums) layernorm_columns_kernel<T><<<dim3((a.dim + 511) / 512, a.parts), 256, 0, ctx->stream>>>(a);
-            layernorm_dx_kernel<T, P><<<a.rows, 256, 0, ctx->stream>>>(a);
+            if (a.dim < 8) layernorm_dx_kernel<T, P, 64><<<a.rows, 64, 0, ctx->stream>>>(a);
+            else layernorm_dx_kernel<T, P, 1024><<<a.rows, 1024, 0, ctx->stream>>>(a);
         }
         if (sums) layernorm_join_kernel<P><<<(2 * a.pitch + 31) / 32, 256, 0, ctx->stream>>>((const float*)p->d_work, a.parts, a.dim, a.pitch, p->d_dweight, p->d_dbias);
     });

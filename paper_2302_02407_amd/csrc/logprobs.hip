@@ -56,8 +56,9 @@ template <class T> __device__ __forceinline__ void write_row(const LogprobArgs& 
 
 // One row, or a part of one, a work group, read once, 16 bytes a lane at a time: every element into its lane's sums against the lane's running maximum,
 // (z - M) c by a difference and a product, so that logits of any size lose nothing.  TOP: pieces with an element that reaches a threshold are also set
-// aside, as top_logits_kernel does (toplogits.hip); what is set aside only has to be put in order, the sums have it already.
-template <class T, int THREADS, int ROOM, bool PARTED> __global__ __launch_bounds__(THREADS, 4) void logprobs_kernel(LogprobArgs a) {
+// aside, as top_logits_kernel does (toplogits.hip); what is set aside only has to be put in order, the sums have it already.  HELD: a row of at most four pieces a
+// lane stays in registers, and one threshold, taken when it is all there, says which elements are put in order.
+template <class T, int THREADS, int ROOM, bool HELD, bool PARTED> __global__ __launch_bounds__(THREADS, 4) void logprobs_kernel(LogprobArgs a) {
     using raw = typename T::raw;
     constexpr int N = Vec<T>::N, WAVES = THREADS / 64;
     constexpr bool TOP = ROOM != 0;
@@ -79,7 +80,7 @@ template <class T, int THREADS, int ROOM, bool PARTED> __global__ __launch_bound
         const uint32_t v = p * THREADS + t;
         const uint32_t base = in.base(v), past = v * N - base;       // elements of it that are another piece's
         Vec<T> x = buf;
-        buf = in.load(v + 2 * THREADS);
+        if (!HELD) buf = in.load(v + 2 * THREADS);
         float e[N];
 #pragma unroll
         for (int i = 0; i < N; i++) e[i] = x[i];
@@ -87,14 +88,14 @@ template <class T, int THREADS, int ROOM, bool PARTED> __global__ __launch_bound
 #pragma unroll
             for (int i = 0; i < N; i++)
                 if ((uint32_t)i < past) {
-                    if (TOP) x.set(i, -INFINITY);
+                    if (TOP && !HELD) x.set(i, -INFINITY);
                     e[i] = -INFINITY;
                 }
         float mx = e[0];
 #pragma unroll
         for (int i = 1; i < N; i++) mx = fmaxf(mx, e[i]);
-        if constexpr (TOP) {
-            high = fmaxf(high, mx);
+        if constexpr (TOP) high = fmaxf(high, mx);
+        if constexpr (TOP && !HELD) {
             if (((p + 1) & (p + 2)) == 0) least = reached_by_all<WAVES>(high, r, full, lane, wave, shared.tw[__builtin_ctz(p + 2) & 1]);
             if (!(mx < least) && (mx != -INFINITY || base < a.k)) {
                 const uint32_t to = atomicAdd(&shared.got, 1u);
@@ -113,10 +114,21 @@ template <class T, int THREADS, int ROOM, bool PARTED> __global__ __launch_bound
             s.less = fmaf(f, fmaxf(d, LEAST_POWER), s.less);
         }
     };
-    Vec<T> one = in.load(t), two = in.load(THREADS + t);
-    for (uint32_t p = 0; p < turns; p += 2) {
-        turn(p, one);
-        if (p + 1 < turns) turn(p + 1, two);
+    Vec<T> held[HELD ? 4 : 2];
+    if constexpr (HELD) {
+#pragma unroll
+        for (uint32_t p = 0; p < 4; p++)
+            if (p < turns) held[p] = in.load(p * THREADS + t);
+#pragma unroll
+        for (uint32_t p = 0; p < 4; p++)
+            if (p < turns) turn(p, held[p]);
+    } else {
+        held[0] = in.load(t);
+        held[1] = in.load(THREADS + t);
+        for (uint32_t p = 0; p < turns; p += 2) {
+            turn(p, held[0]);
+            if (p + 1 < turns) turn(p + 1, held[1]);
+        }
     }
     const float ref = group_max<WAVES>(s.ref, room);
     s = against(s, ref, c);
@@ -128,11 +140,23 @@ template <class T, int THREADS, int ROOM, bool PARTED> __global__ __launch_bound
     }
     if constexpr (TOP) {
         __syncthreads();                                 // all is set aside, and the slots of tw have been read
-        const uint32_t got = shared.got;
+        const uint32_t got = HELD ? 0 : shared.got;
         uint32_t kept = 0;
         bool exact = got > ROOM || d.sum != d.sum;       // a NaN stands above every number, and a threshold does not see it
         if (!exact) {
             least = reached_by_all<WAVES>(high, r, full, lane, wave, shared.tw[0]);
+            if constexpr (HELD)
+#pragma unroll
+                for (uint32_t p = 0; p < 4; p++) {
+                    if (p >= turns) break;
+                    const uint32_t piece = p * THREADS + t, base = in.base(piece), past = piece * N - base;
+#pragma unroll
+                    for (uint32_t i = 0; i < (uint32_t)N; i++)
+                        if (const float v = held[p][i]; !(v < least) && i >= past && (v != -INFINITY || base + i < a.k)) {
+                            const uint32_t to = atomicAdd(&shared.kept, 1u);
+                            if (to < shared.KEEP) shared.keep[to] = place_of(v, from + base + i);
+                        }
+                }
             for (uint32_t i = t; i < got * N; i += THREADS) {
                 const float v = to_float<T>(((const raw*)shared.aside)[i]);
                 const uint32_t which = shared.which[i / N], at = (which & 0xffffff) + i % N;
@@ -270,20 +294,25 @@ extern "C" int32_t he_token_logprobs(he_ctx* ctx, const he_logprobs_plan* p) {
             logprobs_short_kernel<T><<<(p->rows + 255) / 256, 256, 0, ctx->stream>>>(a, p->rows);
             return;
         }
-        auto run = [&](auto threads, auto room) {
+        auto run = [&](auto threads, auto room, auto held) {
             constexpr int THREADS = decltype(threads)::value, ROOM = decltype(room)::value;
+            constexpr bool HELD = decltype(held)::value;
             if (THREADS > 64 && cut.parts > 1) {
-                logprobs_kernel<T, THREADS, ROOM, THREADS != 64><<<dim3(cut.parts, p->rows), THREADS, 0, ctx->stream>>>(a);
+                logprobs_kernel<T, THREADS, ROOM, HELD, THREADS != 64><<<dim3(cut.parts, p->rows), THREADS, 0, ctx->stream>>>(a);
                 logprobs_join_kernel<T><<<p->rows, 256, 0, ctx->stream>>>(a);
-            } else logprobs_kernel<T, THREADS, ROOM, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
+            } else logprobs_kernel<T, THREADS, ROOM, HELD, false><<<p->rows, THREADS, 0, ctx->stream>>>(a);
         };
         using std::integral_constant;
         // Room for what is set aside: of rows in no particular order some k (1 + ln(turns)) pieces are, twice that where the lanes' maxima fall badly
-        // (2048 x 131072 with 512 threads: k = 64 122 us in 1024 places, with 512 it overflowed and took 2355); a row of one wavefront fits whole.
+        // (2048 x 131072 with 512 threads: k = 64 122 us in 1024 places, with 512 it overflowed and took 2355).
         auto go = [&](auto threads) {
-            if (p->k == 0) run(threads, integral_constant<int, 0>{});
-            else if (p->k <= 64) run(threads, integral_constant<int, 1024>{});
-            else run(threads, integral_constant<int, 2048>{});
+            if (p->k == 0) run(threads, integral_constant<int, 0>{}, std::false_type{});
+            else if (p->k <= 64) run(threads, integral_constant<int, 1024>{}, std::false_type{});
+            else run(threads, integral_constant<int, 2048>{}, std::false_type{});
+        };
+        auto hold = [&](auto threads) {
+            if (p->k == 0) run(threads, integral_constant<int, 0>{}, std::true_type{});
+            else run(threads, integral_constant<int, 1>{}, std::true_type{});
         };
         // Several work groups to a compute unit, one of which reads while another puts in order: 2048 x 131072 bf16, k = 8, takes 107 us with 512 threads, 110 with
         // 256 and 123 with 1024, 4096 x 50021 100, 95 and 132, 8192 x 20000 97, 84 and 146.  From k = 65 on thresholds of few wavefronts take long: 512 then
@@ -291,9 +320,9 @@ extern "C" int32_t he_token_logprobs(he_ctx* ctx, const he_logprobs_plan* p) {
         const uint64_t bytes = (uint64_t)cut.len * dtype_bytes(p->dtype);
         const bool few = p->k <= 32 || p->vocab <= 128;
         if (bytes > 131072 || (bytes > 32768 && p->k > 64)) go(integral_constant<int, 512>{});
-        else if (bytes > 4096 || !few || (bytes > 1024 && p->rows < 1024)) go(integral_constant<int, 256>{});
-        else if (p->k == 0) run(integral_constant<int, 64>{}, integral_constant<int, 0>{});
-        else run(integral_constant<int, 64>{}, integral_constant<int, 256>{});
+        else if (bytes > 16384) go(integral_constant<int, 256>{});
+        else if (bytes > 4096 || !few || (bytes > 1024 && p->rows < 1024)) hold(integral_constant<int, 256>{});
+        else hold(integral_constant<int, 64>{});
     });
     HE_LAUNCHED(ctx);
     return HE_OK;
