@@ -136,6 +136,7 @@ static inline const char* refuse_poly(const he_poly_plan* p) {
 // Work groups of 256 threads, 16 to a block of 128 columns.  What sums nothing has one for every sixteen blocks (16384 x 8192 bf16, degree 3: 112 us; 2048 that go on: 142).  Sums
 // want few, as many as are there at a time: the gradients of that take 127 us with 1024, 129 with 2048 and 177 with 512; of 777 x 10007 f16, degree 7, 19, 24 and 20.
 #define HE_POLY_GROUPS 1024u
+#define HE_GROUPS_MAX (1u << 23)   // of 256 threads: 2^31, a launch's must stay below 2^32
 static inline uint32_t poly_groups(uint32_t rows, uint32_t dim, uint32_t most) {
     const uint64_t groups = ((uint64_t)rows * blocks_of(dim) + 15) / 16;
     return groups < most ? (uint32_t)groups : most;

@@ -109,7 +109,7 @@ extern "C" int32_t he_poly_q8(he_ctx* ctx, const he_poly_plan* p) {
     HE_HIP(ctx, device.status);
     const PolyArgs a = {p->d_u, p->d_coefs, p->d_y, p->d_codes, p->d_exponents, p->ld_u, p->ld_y, p->ld_codes, p->ld_exponents, p->rows, p->dim, p->n_coefs, blocks_of(p->dim),
                         inverse_of(blocks_of(p->dim))};
-    const uint32_t groups = poly_groups(p->rows, p->dim, ~0u);
+    const uint32_t groups = poly_groups(p->rows, p->dim, HE_GROUPS_MAX);
     with_dtype(p->dtype, [&](auto t) {
         if (p->d_y) poly_q8_kernel<decltype(t), true><<<groups, 256, 0, ctx->stream>>>(a);
         else poly_q8_kernel<decltype(t), false><<<groups, 256, 0, ctx->stream>>>(a);
@@ -216,7 +216,7 @@ extern "C" int32_t he_poly_grad_q8(he_ctx* ctx, const he_poly_grad_plan* p) {
     HE_REFUSE(ctx, "he_poly_grad_q8", refuse_poly_grad(p));
     const OnDevice device(ctx);
     HE_HIP(ctx, device.status);
-    const uint32_t groups = p->rows ? poly_groups(p->rows, p->dim, p->d_dcoefs ? HE_POLY_GROUPS : ~0u) : 0;
+    const uint32_t groups = p->rows ? poly_groups(p->rows, p->dim, p->d_dcoefs ? HE_POLY_GROUPS : HE_GROUPS_MAX) : 0;
     const PolyGradArgs a = {p->d_codes, p->d_exponents, p->d_coefs, p->d_dy, p->d_du, p->d_dcoefs ? (double*)p->d_work : nullptr, p->ld_codes, p->ld_exponents, p->ld_dy, p->ld_du,
                             p->rows, p->dim, p->n_coefs, blocks_of(p->dim), inverse_of(blocks_of(p->dim))};
     if (groups) with_dtype(p->dtype, [&](auto t) {

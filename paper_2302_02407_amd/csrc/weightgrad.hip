@@ -354,7 +354,7 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
 template <class O, int LANES> __global__ __launch_bounds__(256) void weight_join_kernel(const float* parts, uint32_t n_parts, u64 part, uint32_t ld_part, typename O::raw* dw, u64 ld_dw, uint32_t k, uint32_t accumulate) {
     constexpr int GROUP = 256 / LANES;
     __shared__ v4f sums[LANES][GROUP];
-    const u64 i = ((u64)blockIdx.x * GROUP + threadIdx.x % GROUP) * 4;
+    const u64 i = (((u64)blockIdx.y * gridDim.x + blockIdx.x) * GROUP + threadIdx.x % GROUP) * 4;
     const uint32_t lane = threadIdx.x / GROUP;
     v4f x = {0, 0, 0, 0};
     if (i < part)
@@ -433,11 +433,12 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     HE_HIP(ctx, err);
     if (joined) with_dtype(p->out_dtype, [&](auto o) {
         using O = decltype(o);
-        const u64 all = (u64)p->n * a.ld_dw;              // below 2^34: fewer than 2^31 threads
+        const u64 all = (u64)p->n * a.ld_dw;              // at most 2^34
         const uint32_t parts = p->m ? c.parts : 0;
         auto go = [&](auto lanes) {
             constexpr int LANES = decltype(lanes)::value;
-            weight_join_kernel<O, LANES><<<(all + 1024 / LANES - 1) / (1024 / LANES), 256, 0, ctx->stream>>>(
+            const u64 groups = (all + 1024 / LANES - 1) / (1024 / LANES), side = groups < HE_GROUPS_MAX ? groups : HE_GROUPS_MAX;
+            weight_join_kernel<O, LANES><<<dim3((uint32_t)side, (uint32_t)((groups + side - 1) / side)), 256, 0, ctx->stream>>>(
                 (const float*)p->d_work, parts, all, (uint32_t)a.ld_dw, (typename O::raw*)p->d_dw, p->ld_dw, p->k, p->accumulate);
         };
         if (parts > 8) go(std::integral_constant<int, 8>{});

@@ -101,6 +101,17 @@ def test_rows_that_are_hard(ctx, dim):
             assert (n <= (min(math.sqrt(dim), 2.0 ** -46 * c * 300 / math.sqrt(eps)) if eps else math.sqrt(dim)) * 1.01 + 1e-4 * (1 + (b / w).abs())).all()
 
 
+@pytest.mark.parametrize("dim", [100, 1000, 4096, 9000])
+def test_rows_whose_spread_is_a_few_roundings(ctx, dim):
+    """A mean of 2^20 to 2^24 and numbers that differ by 1 or 2: the rounding of the sum of them is as large as what they differ by."""
+    g = T.rng(dim)
+    x = 2.0 ** torch.arange(20, 25)[:, None].float() + torch.randint(0, 3, (5, dim), generator=g).float() * torch.tensor([1.0, 1, 1, 1, 2])[:, None]
+    w = torch.randn(dim, generator=g)
+    check_forward(run(ctx, x, None, w, None, 1e-5), x, None, w, None, 1e-5)
+    dy = torch.randn((5, dim), generator=g)
+    check_grad(run_grad(ctx, x, 1e-5, dy, w, None, torch.float32), x, 1e-5, dy, w, None, torch.float32)
+
+
 def test_what_is_not_a_number_stays_in_its_row(ctx):
     x = torch.randn((5, 700), generator=T.rng(1))
     x[1, 3], x[2, 699], x[3, 0] = math.nan, math.inf, -math.inf

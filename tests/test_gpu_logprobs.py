@@ -105,6 +105,22 @@ def test_hard_rows(ctx, dtype, vocab):
             check(run(ctx, part, 1.5, None, k), part, 1.5, None, k)
 
 
+@pytest.mark.parametrize("vocab", [520, 1000, 1023])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_short_rows(ctx, dtype, vocab):
+    """From 1024 rows on a wavefront takes one of up to 4 KB; k above 32 four."""
+    few = hard_rows(vocab, dtype)
+    few = torch.cat([few, torch.randn((53, vocab), generator=T.rng(vocab)).to(dtype)])
+    z = few.repeat(16, 1)
+    logp, _, entropy = T.distribution(few, 1.5)
+    index = T.top_order(few, 40)
+    for k in (1, 32, 40):
+        out = run(ctx, z, 1.5, None, k, vocab + 1, 1)
+        assert torch.equal(out["index"].cpu().long(), index[:, :k].repeat(16, 1))
+        assert near(out["values"], logp.gather(1, index[:, :k]).repeat(16, 1))
+        assert ((out["entropy"].cpu().double() - entropy.repeat(16)).abs() <= 1e-5 * (2 + 2 * entropy.repeat(16))).all()
+
+
 @pytest.mark.parametrize("rows", [1, 3])
 def test_a_large_vocabulary(ctx, rows):
     """2^20 logits, the largest; order compared with a sort."""

@@ -109,6 +109,14 @@ def test_what_is_not_finite_stays_in_its_row_and_column(ctx):
     assert torch.equal(~got.isfinite(), bad) and (got[3, :128] == math.inf).all()
 
 
+def test_a_block_marked_as_not_finite_is_none_whatever_its_codes(ctx):
+    codes, exponents = T.keep(torch.randn((40, 300), generator=T.rng(7)))
+    exponents[11, 1] = 255
+    for dtype in TYPES:
+        got = run(ctx, torch.ones((40, 20), dtype=dtype), codes, exponents, torch.float32)
+        assert torch.equal(got.isnan(), (torch.arange(300) // 128 == 1).expand(20, 300)) and got[:, :128].isfinite().all()
+
+
 def test_long_sums_with_the_same_bits(ctx):
     g = T.rng(3)
     codes, exponents = T.keep(torch.randn((20000, 70), generator=g))
