@@ -26,16 +26,31 @@ template <> struct Parts<bf16_t> { static constexpr int N = 1; };
 template <> struct Parts<f16_t> { static constexpr int N = 2; };
 template <> struct Parts<f32_t> { static constexpr int N = 3; };
 
-// A number's bfloat16 parts, in the upper halves: 8 significant bits each, cut off; nothing but itself of an infinity
-template <int PARTS> __device__ __forceinline__ void parts_of(float x, uint32_t (&w)[PARTS]) {
-    w[0] = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
-    float rest = x - __builtin_bit_cast(float, w[0]);
-    if (__builtin_isinf(x)) rest = 0.0f;
+// The upper halves of two numbers of 32 bits side by side
+__device__ __forceinline__ uint32_t uppers(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+__device__ __forceinline__ uint32_t uppers(float lo, float hi) { return uppers(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)); }
+// Two neighbours' bfloat16 parts, pair j of a piece: 8 significant bits each, cut off
+__device__ __forceinline__ void parts_of(const Eight<f32_t>& y, int j, uint32_t (&w)[3]) {
+    const uint32_t word[2] = {y.v[j / 2].w[2 * (j % 2)], y.v[j / 2].w[2 * (j % 2) + 1]};
+    float mid[2], low[2];
 #pragma unroll
-    for (int q = 1; q < PARTS; q++) {
-        w[q] = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
-        rest -= __builtin_bit_cast(float, w[q]);
+    for (int i = 0; i < 2; i++) {
+        const float x = __builtin_bit_cast(float, word[i]);
+        mid[i] = x - __builtin_bit_cast(float, word[i] & 0xffff0000u);
+        if (__builtin_isinf(x)) mid[i] = 0.0f;               // nothing but itself of an infinity
+        low[i] = mid[i] - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, mid[i]) & 0xffff0000u);
     }
+    w[0] = uppers(word[0], word[1]);
+    w[1] = uppers(mid[0], mid[1]);
+    w[2] = uppers(low[0], low[1]);
+}
+// Of 11 significant bits the last three are the second part.  Of an infinity that would be no number: 256, above any other, which beside an infinity is nothing.
+__device__ __forceinline__ void parts_of(const Eight<f16_t>& y, int j, uint32_t (&w)[2]) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const uint32_t word = y.v[0].w[j];
+    const h2 x = __builtin_bit_cast(h2, word), high = __builtin_bit_cast(h2, word & 0xfff8fff8u), low = __builtin_elementwise_min(x - high, h2{256, 256});
+    w[0] = uppers((float)high[0], (float)high[1]);
+    w[1] = uppers((float)low[0], (float)low[1]);
 }
 
 // A work group owns BN columns of dy by BK columns of what is kept and goes through the rows 32 at a time.
@@ -161,11 +176,10 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
                 uint32_t w[PARTS][4];
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    uint32_t lo[PARTS], hi[PARTS];
-                    parts_of(st.y[f][2 * j], lo);
-                    parts_of(st.y[f][2 * j + 1], hi);
+                    uint32_t pair[PARTS];
+                    parts_of(st.y[f], j, pair);
 #pragma unroll
-                    for (int q = 0; q < PARTS; q++) w[q][j] = __builtin_amdgcn_perm(hi[q], lo[q], 0x07060302u);
+                    for (int q = 0; q < PARTS; q++) w[q][j] = pair[q];
                 }
 #pragma unroll
                 for (int q = 0; q < PARTS; q++) *(uint4*)(to + q * G::PLANE) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);

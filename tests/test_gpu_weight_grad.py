@@ -101,6 +101,11 @@ def test_numbers_of_all_sizes(ctx):
 def test_what_is_not_finite_stays_in_its_row_and_column(ctx):
     g = T.rng(2)
     dy, u = torch.randn((50, 40), generator=g), torch.randn((50, 300), generator=g).abs() + 0.1
+    for dtype in TYPES:
+        half = dy.to(dtype, copy=True)
+        half[7, 3], half[8, 4], half[9, 5] = math.inf, math.nan, -math.inf
+        got = run(ctx, half, *T.keep(u), torch.float32)
+        assert (got[3] == math.inf).all() and got[4].isnan().all() and (got[5] == -math.inf).all() and got[6:].isfinite().all()
     dy[7, 3], dy[8, 4], u[9, 200] = math.inf, math.nan, math.nan
     codes, exponents = T.keep(u)
     got = run(ctx, dy, codes, exponents, torch.float32)
