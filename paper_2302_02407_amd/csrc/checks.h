@@ -167,7 +167,7 @@ static inline const char* refuse_poly_grad(const he_poly_grad_plan* p, bool quer
 
 #define HE_SIDE_MAX (1u << 17)
 
-// Tiles of `side` rows by as many columns of dw, the sum over the rows of dy in `parts` parts of `per` steps of 32 rows, joined by a second kernel
+// Tiles of `side` rows by as many columns of dw, or of 64 by 256, the sum over the rows of dy in `parts` parts of `per` steps of 32 rows, joined by a second kernel
 struct WeightCut {
     uint32_t side, parts, per;
     bool ahead;                // small tiles of bf16, at most two to a compute unit: rows are asked for four steps ahead, for which three have no registers (65536 x 256 x 256: 28 us, 30)
@@ -181,10 +181,10 @@ static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k, int32_t d
     WeightCut best = {128, 1, (uint32_t)steps, false};
     if (steps == 0) return best;
     uint64_t least = ~0ull;
-    for (uint32_t side = 128; side <= 256; side += 128) {
-        if (side == 256 && n < 256) break;
-        const uint64_t tiles = (uint64_t)((n + side - 1) / side) * ((k + side - 1) / side);
-        static const uint32_t wants[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    for (uint32_t side = n > 64 ? 128 : 64; side <= 256; side *= 2) {
+        if (side == 256 ? n < 256 : side == 128 && n <= 64) break;
+        const uint64_t wide = side == 64 ? 256 : side, tiles = ((n + side - 1) / side) * ((k + wide - 1) / wide);
+        static const uint32_t wants[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
         for (const uint32_t want : wants) {
             if (want > 1 && steps < 4 * want) break;
             const uint64_t per = (steps + want - 1) / want, parts = (steps + per - 1) / per, each = (tiles * parts + 255) / 256;

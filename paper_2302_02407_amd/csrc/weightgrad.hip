@@ -75,13 +75,16 @@ typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 // takes 1019), matrix instructions 55% of its cycles, vector instructions 42%, most of them conversions, which run beside those only in part.  Steps on the way:
 // read and multiplied in turn 1256, in the pipeline below 1124, loads by pointers 1095, asked for two steps ahead 1040.  Wavefronts of 128 x 64, which convert half as much,
 // read codes two bytes a lane: 1190 where this took 1095, for LDS instructions.  Four wavefronts of 128 x 128 do not fit the registers.  Smaller tiles,
-// 128 x 128 by four wavefronts of 64 x 64, two or three to a unit, where few large ones are there: 4096 x 2048 x 2048 63 us.
+// 128 x 128 by four wavefronts of 64 x 64, two or three to a unit, where few large ones are there: 4096 x 2048 x 2048
+// 63 us; 64 x 256 by four of 64 x 64 for up to 64 columns of dy: 22070 x 25 x 4773 f16 44 us, in tiles of 128 x 128 76.
 template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __global__ __launch_bounds__(64 * WN * WK, 2) void weight_grad_kernel(WeightArgs a) {
     using raw = typename T::raw;
     using G = WeightTile<T, WN, WK, TN, TK>;
     using codes_t = std::conditional_t<TK == 4, uint32_t, uint16_t>;         // a lane's columns of a row
     constexpr int PARTS = G::PARTS;
     extern __shared__ __align__(1024) uint8_t lds[];
+    // a piece's place in row r, so that four rows' lie in different banks: a row is all 64 banks, or half of them
+    auto turned = [](uint32_t p, uint32_t r) { return G::BN >= 128 ? p ^ 4 * (r & 3) : p ^ 4 * (r >> 1 & 1); };
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane & 31, g = lane >> 5;
     const uint32_t wn = wave / WK, wk = wave % WK;
     // All tiles of a part, then those of the next: a die takes an eighth of that, and its cache holds the rows that the tiles of a part share.  (With the parts on
@@ -176,7 +179,7 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
 #pragma unroll
                 for (int j = 0; j < WORDS; j++) st.y[f].v[j / 4].w[j % 4] = w[j];
             }
-            uint8_t* to = buf + r * (G::BN * 2) + ((p ^ (4 * (r & 3))) * 16);
+            uint8_t* to = buf + r * (G::BN * 2) + turned(p, r) * 16;
             if constexpr (PARTS == 1) *(uint4*)to = make_uint4(st.y[f].v[0].w[0], st.y[f].v[0].w[1], st.y[f].v[0].w[2], st.y[f].v[0].w[3]);
             else {
                 uint32_t w[PARTS][4];
@@ -208,7 +211,7 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
     uint32_t y_at[TN], x_at[2];
 #pragma unroll
     for (int q = 0; q < TN; q++)
-        y_at[q] = (8 * g + (lane & 15) / 4) * (G::BN * 2) + (((wn * TN * 4 + 4 * q + (lane >> 4 & 1) * 2 + (lane & 3) / 2) ^ 4 * ((lane & 15) / 4)) * 16) + (lane & 1) * 8;
+        y_at[q] = (8 * g + (lane & 15) / 4) * (G::BN * 2) + turned(wn * TN * 4 + 4 * q + (lane >> 4 & 1) * 2 + (lane & 3) / 2, (lane & 15) / 4) * 16 + (lane & 1) * 8;
 #pragma unroll
     for (int i = 0; i < 2; i++) x_at[i] = G::X + (((8 * g + i) * G::BK + (wk * 32 + l) * TK) ^ (g * 128));
     auto read = [&](uint32_t step, int h, Half& f) {
@@ -371,7 +374,8 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
 
 // Sums the parts, in a fixed order: four elements a thread, LANES of which take every LANES-th part of the same four.  Parts lie as dw does, their rows
 // ld_part apart, a multiple of 4.
-template <class O, int LANES> __global__ __launch_bounds__(256) void weight_join_kernel(const float* parts, uint32_t n_parts, u64 part, uint32_t ld_part, typename O::raw* dw, u64 ld_dw, uint32_t k, uint32_t accumulate) {
+template <class O, int LANES> __global__ __launch_bounds__(256)
+void weight_join_kernel(const float* parts, uint32_t n_parts, u64 part, uint32_t ld_part, typename O::raw* dw, u64 ld_dw, uint32_t k, uint32_t accumulate) {
     constexpr int GROUP = 256 / LANES;
     __shared__ v4f sums[LANES][GROUP];
     const u64 i = (((u64)blockIdx.y * gridDim.x + blockIdx.x) * GROUP + threadIdx.x % GROUP) * 4;
@@ -441,14 +445,18 @@ extern "C" int32_t he_weight_grad_q8(he_ctx* ctx, const he_weight_grad_plan* p) 
     if (p->m) with_dtype(p->dtype, [&](auto t) {
         using T = decltype(t);
         constexpr int MANY = Parts<T>::N < 3 ? 4 : 2;     // stages that the registers have room for at two work groups to a compute unit
-        auto small = [&](auto narrow) {
+        auto small = [&](auto wn, auto narrow) {
+            constexpr int WN = decltype(wn)::value;
             constexpr bool N = decltype(narrow)::value;
             if constexpr (Parts<T>::N == 1)
-                if (!c.ahead) return launch_weight_grad<T, 2, 2, 2, 2, 1, N>(a, c, ctx->stream);
-            return launch_weight_grad<T, 2, 2, 2, 2, MANY, N>(a, c, ctx->stream);
+                if (!c.ahead) return launch_weight_grad<T, WN, 4 / WN, 2, 2, 1, N>(a, c, ctx->stream);
+            return launch_weight_grad<T, WN, 4 / WN, 2, 2, MANY, N>(a, c, ctx->stream);
         };
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
         if (c.side == 256) err = launch_weight_grad<T, 4, 2, 2, 4, Parts<T>::N == 1 ? 2 : 1, false>(a, c, ctx->stream);
-        else err = p->n >= 128 ? small(std::false_type{}) : small(std::true_type{});
+        else if (c.side == 64) err = small(one, std::true_type{});
+        else err = p->n >= 128 ? small(two, std::false_type{}) : small(two, std::true_type{});
     });
     HE_HIP(ctx, err);
     if (joined) with_dtype(p->out_dtype, [&](auto o) {

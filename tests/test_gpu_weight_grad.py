@@ -58,6 +58,16 @@ def test_weight_grad(ctx, dtype, m, n, k):
     check(run(ctx, dy, codes, exponents, out, 1, 1, onto), dy, codes, exponents, onto)
 
 
+# tiles of 64 by 256: one and several, ends of both sides, sums in one part and in many
+@pytest.mark.parametrize("m,n,k", [(40, 64, 256), (33, 63, 257), (700, 1, 1000), (65, 7, 513), (300, 9, 255), (5000, 33, 700), (20000, 64, 130), (9000, 65, 260)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_columns(ctx, dtype, m, n, k):
+    g = T.rng(m + n + k)
+    codes, exponents = T.keep(torch.randn((m, k), generator=g) * torch.exp(torch.randn((m, 1), generator=g)))
+    dy = torch.randn((m, n), generator=g).to(dtype)
+    check(run(ctx, dy, codes, exponents, torch.float32, 5, 3), dy, codes, exponents)
+
+
 @pytest.mark.parametrize("m,n,k", [(40, 50, 60), (500, 260, 257), (3000, 130, 70), (9000, 20, 20)])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_whole_numbers_are_exact(ctx, dtype, m, n, k):

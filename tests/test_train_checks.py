@@ -195,7 +195,7 @@ int main() {
                 const WeightCut c = weight_cut(m, n, k, t);
                 const uint32_t steps = (m + 31) / 32;
                 if (c.parts < 1 || c.parts > 65535 || c.per < 1 || (uint64_t)(c.parts - 1) * c.per >= steps || (uint64_t)c.parts * c.per < steps) { bad++; printf("cut of %u %u %u\n", m, n, k); }
-                if (c.side != 128 && (c.side != 256 || n < 256)) { bad++; printf("tile of %u %u %u\n", m, n, k); }
+                if (c.side != (n > 64 ? 128 : 64) && (c.side != 256 || n < 256)) { bad++; printf("tile of %u %u %u\n", m, n, k); }
                 }
             }
     if (weight_cut(0, 5, 7, HE_F32).parts != 1 || weight_cut(0, 5, 7, HE_F32).per != 0) { bad++; printf("cut of no rows\n"); }
