@@ -214,7 +214,7 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
         y_at[q] = (8 * g + (lane & 15) / 4) * (G::BN * 2) + turned(wn * TN * 4 + 4 * q + (lane >> 4 & 1) * 2 + (lane & 3) / 2, (lane & 15) / 4) * 16 + (lane & 1) * 8;
 #pragma unroll
     for (int i = 0; i < 2; i++) x_at[i] = G::X + (((8 * g + i) * G::BK + (wk * 32 + l) * TK) ^ (g * 128));
-    auto read = [&](uint32_t step, int h, Half& f) {
+    auto read_x = [&](uint32_t step, int h, Half& f) {
         const uint32_t buf = (step & 1) * G::BYTES;
 #pragma unroll
         for (int u = 0; u < 4; u++)
@@ -222,6 +222,9 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
             for (int i = 0; i < 2; i++) f.x[2 * u + i] = *(const codes_t*)(lds + buf + x_at[i] + (16 * h + 2 * u) * G::BK);
 #pragma unroll
         for (int i = 0; i < 2; i++) f.s[i] = *(const v4f*)(lds + buf + G::S + (wk * TK / 4 * 32 + 16 * h + 8 * g + 4 * i) * 4);
+    };
+    auto read_y = [&](uint32_t step, int h, Half& f) {
+        const uint32_t buf = (step & 1) * G::BYTES;
 #pragma unroll
         for (int q = PARTS - 1; q >= 0; q--)
 #pragma unroll
@@ -229,6 +232,10 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
 #pragma unroll
                 for (int t = 0; t < 2; t++)
                     f.y[q][i][t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)((lds_ptr)lds + buf + y_at[i] + (q * 32 + 16 * h + 4 * t) * (G::BN * 2)));
+    };
+    auto read = [&](uint32_t step, int h, Half& f) {
+        read_x(step, h, f);
+        read_y(step, h, f);
     };
     v16f acc[TN][TK];
 #pragma unroll
@@ -320,23 +327,31 @@ template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __glo
                 two = next;
                 meet();
             }
-    } else {                                              // several matrix products to a half hide its reads
+    } else {
+        // Several matrix products to a half: the next one is read and turned while they run, and the registers hold no third (60294 x 663 x 6360 f16 1030 -> 980 us, 16384
+        // x 4096 x 4096 f32 1248 -> 1200, 1374 TFLOP/s of its three products; small tiles lose their third work group to a compute unit for it and still gain, 1000 x 500 x
+        // 4000 f32 37 -> 33; 8192 x 200 x 8000 f16 88 -> 89)
         Half half;
-        Kept kept;
+        Kept kept, other;
+        read(0, 0, half);
+        convert(half, kept);
         for (uint32_t b0 = 0; b0 < steps; b0 += AHEAD)
 #pragma unroll
             for (int d = 0; d < AHEAD; d++) {
                 const uint32_t b = b0 + d;
                 if (d && b >= steps) break;
-                read(b, 0, half);
-                convert(half, kept);
+                Half next;
+                read(b, 1, next);
                 multiply(half, kept);
+                convert(next, other);
+                interleave();
                 store(b + 1, st[d]);                      // the other buffer: its last reads lie before the last barrier
-                read(b, 1, half);
-                convert(half, kept);
-                multiply(half, kept);
                 load(b + 1 + AHEAD, st[d]);
                 meet();
+                read(b + 1, 0, half);
+                multiply(next, other);
+                convert(half, kept);
+                interleave();
             }
     }
     // element e of a square: row 8 (e / 4) + 4 g + e % 4, square j column TK l + j
