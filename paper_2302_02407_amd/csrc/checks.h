@@ -174,8 +174,8 @@ struct WeightCut {
 };
 // The cut that costs least, by what was measured of steps and joins (bf16; in fifths of a step of a compute unit's three small tiles, 0.19 us): a step of a
 // unit takes 5.5 with a tile of 256 x 256, and 3, 4, 5 with one, two, three of 128 x 128; a step of f16 1.4 times that and one of f32 2 times, their matrix
-// products being two and three (between 1.2 and 1.6, and 1.6 and 2.3, cuts or times of few shapes change).  The second launch takes 16 and a part 8 bytes an element at 4.5 TB/s.  Measured against the best of five rules of thumb
-// on eleven shapes from 500 x 100 x 100 to 65536 x 256 x 256; shapes between go by the same line.
+// products being two and three (between 1.2 and 1.6, and 1.6 and 2.3, cuts or times of few shapes change).  The second launch takes 16 and a part 8 bytes an
+// element at 4.5 TB/s.  Measured against the best of five rules of thumb on eleven shapes from 500 x 100 x 100 to 65536 x 256 x 256; shapes between go by the same line.
 static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k, int32_t dtype) {
     const uint64_t steps = (m + 31) / 32, kind = dtype == HE_BF16 ? 10 : dtype == HE_F16 ? 14 : 20;
     WeightCut best = {128, 1, (uint32_t)steps, false};

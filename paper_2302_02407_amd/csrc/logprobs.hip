@@ -59,7 +59,7 @@ template <class T> __device__ __forceinline__ void write_row(const LogprobArgs& 
 // aside, as top_logits_kernel does (toplogits.hip); what is set aside only has to be put in order, the sums have it already.  HELD: a row of at most four pieces a
 // lane stays in registers, and one threshold, taken when it is all there, says which elements are put in order.
 //
-// 2048 x 131072 bf16, k = 8: 105 us (5.1 TB/s of one reading), vector instructions 95% of its cycles under the counters, 13.4 an element, one exponential among them;
+// 2048 x 131072 bf16, k = 8: 106 us (5.0 TB/s of one reading), vector instructions 96% of its cycles under the counters, 13.4 an element, one exponential among them;
 // as two passes, order and sums, 413.  8192 x 500, k = 30, 20 us, without HELD 30.
 template <class T, int THREADS, int ROOM, bool HELD, bool PARTED> __global__ __launch_bounds__(THREADS, 4) void logprobs_kernel(LogprobArgs a) {
     using raw = typename T::raw;

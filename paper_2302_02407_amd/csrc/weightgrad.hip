@@ -71,8 +71,8 @@ typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 // holds columns 4 l .. 4 l + 3, so that results are written 16 bytes a lane.  Rows r and r + 8 go to the two halves of a wavefront
 // and are 128 bytes, half of the banks, apart: no conflicts (counted).
 //
-// Tiles of 256 x 256 by eight wavefronts of 64 x 128: 16384 x 8192 x 4096 bf16 to f32 985 us (1116 TFLOP/s; a library product of two bfloat16 matrices that lie so
-// takes 1019), matrix instructions 55% of its cycles, vector instructions 42%, most of them conversions, which run beside those only in part.  Steps on the way:
+// Tiles of 256 x 256 by eight wavefronts of 64 x 128: 16384 x 8192 x 4096 bf16 to f32 979 us (1123 TFLOP/s; a library product of two bfloat16 matrices that lie so
+// takes 1019), matrix instructions 55% of its cycles, vector instructions 42% (counted).  Steps on the way:
 // read and multiplied in turn 1256, in the pipeline below 1124, loads by pointers 1095, asked for two steps ahead 1040.  Wavefronts of 128 x 64, which convert half as much,
 // read codes two bytes a lane: 1190 where this took 1095, for LDS instructions.  Four wavefronts of 128 x 128 do not fit the registers.  Smaller tiles,
 // 128 x 128 by four wavefronts of 64 x 64, two or three to a unit, where few large ones are there: 4096 x 2048 x 2048
