@@ -235,11 +235,11 @@ static inline const char* logits_sizes(uint32_t rows, uint32_t vocab, int32_t dt
 struct LogprobCut {
     uint32_t parts, len;
 };
-// Few long rows are cut in up to 32 parts of at least 8 KiB, which are joined by a second launch (128
-// x 131072 bf16, k = 8, in four parts 17.8 us, whole 20.1; 1 x 131072, k = 20, in 32 parts 11.3)
+// Few long rows are cut in up to 32 parts of at least 8 KiB, which are joined by a second launch (128 x 131072 bf16, k = 8, in four parts 17.8 us,
+// whole 20.1; 1 x 131072, k = 20, in 32 parts 11.3)
 static inline LogprobCut logprobs_cut(uint32_t rows, uint32_t vocab, int32_t dtype) {
     const uint32_t piece = 8192 / dtype_bytes(dtype);
-        uint32_t parts = rows ? 512 / rows : 1;
+    uint32_t parts = rows ? 512 / rows : 1;
     if (parts > vocab / piece) parts = vocab / piece;
     if (parts > 32) parts = 32;
     if (parts < 4) return {1, vocab};
