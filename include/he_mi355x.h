@@ -558,7 +558,7 @@ typedef struct {
 int32_t he_poly_q8(he_ctx* ctx, const he_poly_plan* plan);
 
 /* From the gradient dy by y, at the values v that are kept: du = dy * sum of i coefs[i] v^(i-1), dcoefs[i] = sum over all elements of dy * v^i
- * (may be NULL; 0 where there are no rows; its sums are held in 64 bits across pieces of a few dozen elements).  d_du may be d_dy with the same ld. */
+ * (may be NULL; 0 where there are no rows; its sums are held in 64 bits across pieces of eight elements).  d_du may be d_dy with the same ld. */
 typedef struct {
     uint32_t rows, dim, n_coefs;   /* n_coefs from 1 to HE_POLY_MAX */
     int32_t dtype;                 /* of dy and du */

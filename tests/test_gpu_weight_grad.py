@@ -96,6 +96,18 @@ def test_whole_numbers_of_large_gradients(ctx, dtype, m, n, k):
     assert torch.equal(run(ctx, dy, codes, exponents, torch.float32, 0, 0, onto), want + onto)
 
 
+@pytest.mark.parametrize("m,n,k", [(20011, 777, 1001), (2069, 4050, 4060)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_whole_numbers_of_long_sums_in_large_tiles(ctx, dtype, m, n, k):
+    """Many steps a tile, in parts (40 steps each, 26 the last) and whole (65): sums below m * 20 * 16 < 2^24."""
+    g = T.rng(m)
+    dy, v = torch.randint(-20, 21, (m, n), generator=g).to(dtype), torch.randint(-8, 9, (m, k), generator=g).float()
+    codes, exponents = T.keep(v)
+    exponents[::3] += 1
+    want = dy.float().T @ T.kept(codes, exponents).float()
+    assert torch.equal(run(ctx, dy, codes, exponents, torch.float32, 1, 1), want)
+
+
 def test_numbers_of_all_sizes(ctx):
     """32 bits of dy count, far powers of what is kept too: one product a sum, which is added up from three parts of it, so off by at most 3 2^-24 of itself
     and by what is below the smallest normal numbers; what 32 bits do not hold is infinite."""
