@@ -65,7 +65,8 @@ template <int FROM> __device__ __forceinline__ void horner(const Coefs& k, uint3
 
 // Sixteen lanes a block of 128 columns, eight elements each: they find the largest among themselves.  A block at a time and many wavefronts: two or four at a
 // time, their loads together, are no faster (16384 x 8192 bf16, degree 3, when work groups went on from block to block: 142 us, 143 and 146; gradients 145, 198 and 196, for
-// want of registers).  Memory is what bounds it: 112 us, 6.0 TB/s; gradients 127 us, 5.3 TB/s.
+// want of registers).  Memory is what bounds it: 112 us, 6.0 TB/s; gradients 127 us, 5.3 TB/s (148 with
+// the next block asked for ahead: its registers leave fewer wavefronts).
 template <class T, bool Y> __global__ __launch_bounds__(256) void poly_q8_kernel(PolyArgs a) {
     using raw = typename T::raw;
     const uint32_t lane = threadIdx.x & 15, all = a.rows * a.blocks;
