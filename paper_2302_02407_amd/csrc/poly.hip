@@ -174,7 +174,7 @@ template <class T, int SUMS> __global__ __launch_bounds__(256) void poly_grad_ke
             if (j + 1 < SUMS) total[j + 1] += t;
             if (j + 2 < SUMS)
 #pragma unroll
-                for (int i = 0; i < 8; i++) g[i] *= v[i] * v[i];
+                for (int i = 0; i < 8; i++) g[i] = g[i] * v[i] * v[i];        // not g v^2: a square of its own 32 bits need not hold
         }
     }
     if constexpr (SUMS > 0) {

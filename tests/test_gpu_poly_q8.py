@@ -154,6 +154,22 @@ def test_many_rows_with_the_same_bits(ctx):
         assert all(torch.equal(a, b) for a, b in zip(r, runs[0]))
 
 
+# powers of two of values and gradients: squares above and below what 32 bits hold, dy v^i not; None: padding, a gradient of 0
+@pytest.mark.parametrize("value,gradient", [(66, -100), (100, -120), (-74, 110), (100, None)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sums_of_values_whose_squares_32_bits_do_not_hold(ctx, dtype, value, gradient):
+    g = T.rng(7)
+    v, dy = torch.randn((9, 300), generator=g), torch.randn((9, 300), generator=g)
+    v[::2] *= 2.0 ** value
+    if gradient is None:
+        dy[::2] = 0
+    else:
+        v, dy = v[::2], dy[::2] * 2.0 ** gradient
+    codes, exponents = T.keep(v)
+    for n in (2, 3):                                          # slopes of up to two terms: numbers of 32 bits
+        check_grad(run_grad(ctx, codes, exponents, coefs_of(n), dy.to(dtype)), codes, exponents, coefs_of(n), dy.to(dtype))
+
+
 def test_far_rows(ctx):
     rows, dim, pitch = 18, 300, 1 << 28                                # 17 * 2^28 elements: past 2^32
     g = T.rng(6)
