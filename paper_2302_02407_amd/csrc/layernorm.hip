@@ -335,6 +335,9 @@ template <class T, class P, int THREADS> __global__ __launch_bounds__(THREADS) v
             n[i] = (n[i] - stats.x - stats.y) * stats.z;
             if (w) g[i] *= f[i];
         }
+        if (at + 8 > a.dim)                               // past the row's end: 0 of g times what -mean / sqrt(v + eps) is, which may be no number
+#pragma unroll
+            for (int i = 0; i < 8; i++) n[i] = at + i < a.dim ? n[i] : 0.0f;
     };
     float s1 = 0, s2 = 0;
     for (uint32_t at = threadIdx.x * 8; at < a.dim; at += THREADS * 8) {

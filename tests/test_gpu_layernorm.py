@@ -179,6 +179,19 @@ def test_grad_of_hard_rows(ctx):
     assert (got[0] == 0).all() and (got[1] == 0).all()
 
 
+@pytest.mark.parametrize("dim", [1, 5, 7, 13, 300, 5001, 20001])
+def test_grad_of_constants_far_out(ctx, dim):
+    """A mean times 1/sqrt(eps) that 32 bits do not hold, n being 0 everywhere; statistics as given."""
+    g, c, r = T.rng(dim), torch.tensor([3.3e38, -1.1e36, 2.5]), 2.0 ** 10
+    dy, w = torch.randn((3, dim), generator=g), torch.randn(dim, generator=g)
+    stats = torch.stack([c, torch.zeros(3), torch.full((3,), r), torch.zeros(3)], dim=1).cuda()
+    dx, dw = torch.empty((3, dim), device="cuda"), torch.empty(dim, device="cuda")
+    ctx.he_layernorm_grad(c[:, None].expand(3, dim).contiguous().cuda(), stats, dy.cuda(), dx, weight=w.cuda(), dweight=dw)
+    t = dy.double() * w.double()
+    mean, size = t.mean(dim=1, keepdim=True), r * (t.abs() + t.abs().mean(dim=1, keepdim=True))
+    assert ((dx.cpu().double() - r * (t - mean)).abs() <= 2.0 ** -15 * size).all() and (dw == 0).all()
+
+
 def test_gradient_against_differences(ctx):
     """Central differences of sum(y t): the third derivative of a normed row of variance about 1 is below 40 |t|, a value's rounding 2^-17 of its size."""
     rows, dim, h = 2, 9, 2.0 ** -6
