@@ -51,28 +51,32 @@ template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds
     }
     auto total = [&](float v) { return ROW == 16 ? row_sum(v) : group_sum<WAVES ? WAVES : 1>(v, room); };
     float mean = total(s) / (float)dim, low, var;
-    auto spread = [&](float center) {                     // the variance, and what the mean and `center` lack
-        float d1 = 0, d2 = 0;
+    // The variance, and what the mean lacks.  Where that is not far below the row's spread, the mean is rounded again with it and both are taken again: a constant then is its own
+    // mean, and of numbers that differ by their last bits the variance is at least the square of what the nearest number lacks.
+    auto spread = [&]() {
+#pragma unroll 1
+        for (int turn = 0;; turn++) {
+            float d1 = 0, d2 = 0;
 #pragma unroll
-        for (int p = 0; p < V; p++) {
-            const int left = (int)dim - (int)((p * ROW + t) * 8);
+            for (int p = 0; p < V; p++) {
+                const int left = (int)dim - (int)((p * ROW + t) * 8);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float d = i < left ? h[p][i] - mean - center : 0.0f;
-                d1 += d;
-                d2 = fmaf(d, d, d2);
+                for (int i = 0; i < 8; i++) {
+                    const float d = i < left ? h[p][i] - mean : 0.0f;
+                    d1 += d;
+                    d2 = fmaf(d, d, d2);
+                }
             }
+            group_sum2<WAVES>(d1, d2, room);
+            low = d1 / (float)dim;
+            var = d2 / (float)dim - low * low;
+            var = var < 0.0f ? 0.0f : var;                // a NaN stays one
+            const float nearer = mean + low;
+            if (turn == 2 || !(low * low > 0.015625f * var) || nearer == mean) break;
+            mean = nearer;
         }
-        group_sum2<WAVES>(d1, d2, room);
-        const float more = d1 / (float)dim;
-        low = center + more;
-        var = d2 / (float)dim - more * more;
-        var = var < 0.0f ? 0.0f : var;                    // a NaN stays one
-        return more * more > 0.015625f * var;
     };
-    // Where the mean's rounding is not far below the row's spread, the difference of the two is taken again from what is now known (but for rows that fill the
-    // registers, of more than 32768 columns)
-    if (spread(0.0f) && V < 8) spread(low);
+    spread();
     float r = inverse_root(var + a.eps);
     float4 stats = {mean, low, r, 0};
     if (!(var < 0x1p126f)) {                              // squares, or the sum, that 32 bits do not hold: by a power of two
@@ -90,7 +94,7 @@ template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds
 #pragma unroll
                 for (int i = 0; i < 8; i++) s += h[p][i] = ldexpf(h[p][i], -e);
             mean = total(s) / (float)dim;
-            spread(0.0f);
+            spread();
             r = inverse_root(var + ldexpf(a.eps, -2 * e));
             stats = {ldexpf(mean, e), ldexpf(low, e), ldexpf(r, -e), 0};
         }

@@ -112,6 +112,26 @@ def test_rows_whose_spread_is_a_few_roundings(ctx, dim):
     check_grad(run_grad(ctx, x, 1e-5, dy, w, None, torch.float32), x, 1e-5, dy, w, None, torch.float32)
 
 
+def nearly_constant(dim, size):
+    """A constant whose sum rounds alike everywhere, and one element that differs by its last bit: far less than the mean's rounding."""
+    c = (torch.tensor([1.2345678, 1.4142135, 1.9999998, 1.0000001]) * size)[:, None].expand(4, dim).contiguous()
+    c[:, dim // 3] = torch.nextafter(c[:, 0], c[:, 0] * 2)
+    return c
+
+
+@pytest.mark.parametrize("dim", [50, 900, 5000, 20001])
+def test_nearly_constant_rows_whose_sum_leaves_32_bits(ctx, dim):
+    x, w = nearly_constant(dim, 2.0 ** 127), torch.randn(dim, generator=T.rng(dim))
+    check_forward(run(ctx, x, None, w, None, 1e-5), x, None, w, None, 1e-5)
+
+
+@pytest.mark.parametrize("dim", [300, 5000, 20001, 32776, 40001, 65536])
+def test_nearly_constant_rows(ctx, dim):
+    x, w = nearly_constant(dim, 2.0 ** 20), torch.randn(dim, generator=T.rng(dim))
+    for eps in (0.0, 1e-5):
+        check_forward(run(ctx, x, None, w, None, eps), x, None, w, None, eps)
+
+
 def test_what_is_not_a_number_stays_in_its_row(ctx):
     x = torch.randn((5, 700), generator=T.rng(1))
     x[1, 3], x[2, 699], x[3, 0] = math.nan, math.inf, -math.inf
