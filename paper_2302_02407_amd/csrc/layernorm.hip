@@ -95,8 +95,9 @@ template <class T, class P, bool RES, int ROW, int V> __global__ __launch_bounds
                 for (int i = 0; i < 8; i++) s += h[p][i] = ldexpf(h[p][i], -e);
             mean = total(s) / (float)dim;
             spread();
-            r = inverse_root(var + ldexpf(a.eps, -2 * e));
-            stats = {ldexpf(mean, e), ldexpf(low, e), ldexpf(r, -e), 0};
+            // of a constant eps is all that is left, which has no power; another row's variance is at least 2^-70 beside it
+            r = inverse_root(var == 0.0f ? a.eps : var + ldexpf(a.eps, -2 * e));
+            stats = {ldexpf(mean, e), ldexpf(low, e), var == 0.0f ? r : ldexpf(r, -e), 0};
         }
     }
     if (a.stats && t == 0) a.stats[row] = stats;

@@ -112,6 +112,25 @@ def test_rows_whose_spread_is_a_few_roundings(ctx, dim):
     check_grad(run_grad(ctx, x, 1e-5, dy, w, None, torch.float32), x, 1e-5, dy, w, None, torch.float32)
 
 
+@pytest.mark.parametrize("dim", [2, 5, 64, 700, 1000, 3000, 5001, 12000, 20000, 40001, 65536])
+def test_constant_rows(ctx, dim):
+    """No spread, whatever the size: a sum that 32 bits do not hold, or one whose rounding times 1/sqrt(eps) is far from 0."""
+    g = T.rng(dim)
+    c = torch.tensor([3.3e38, -3.4e38, 2.0 ** 120 * 1.37, 1.1e15, -7.3e27, -3.25, 0.1])
+    x, w, b, dy = c[:, None].expand(7, dim).contiguous(), torch.randn(dim, generator=g), torch.randn(dim, generator=g), torch.randn((7, dim), generator=g)
+    for eps in (1e-5, 3.0, 1e-12, 0.0):
+        y, _, stats = run(ctx, x, None, w, b, eps)
+        s, r = stats.cpu().double(), 1 / math.sqrt(float(torch.tensor(eps))) if eps else 0.0
+        assert torch.equal(y.cpu(), b.expand(7, dim))
+        assert torch.equal(s[:, 0] + s[:, 1], c.double()) and ((s[:, 2] - r).abs() <= 2.0 ** -22 * r).all() and (s[:, 3] == 0).all()
+        d = torch.randn((7, dim), generator=g)
+        dx, dw, db = run_grad(ctx, x, eps, dy, w, d, torch.float32)
+        t = dy.double() * w.double()                          # dx = (g - mean g) / sqrt(eps) + dsum
+        mean, size = t.mean(dim=1, keepdim=True), r * (t.abs() + t.abs().mean(dim=1, keepdim=True)) + d.double().abs()
+        assert ((dx.cpu().double() - (r * (t - mean) + d.double())).abs() <= 2.0 ** -15 * size + 2.0 ** -149).all()
+        assert (dw == 0).all() and ((db.cpu().double() - dy.double().sum(dim=0)).abs() <= 2.0 ** -15 * dy.double().abs().sum(dim=0)).all()
+
+
 def nearly_constant(dim, size):
     """A constant whose sum rounds alike everywhere, and one element that differs by its last bit: far less than the mean's rounding."""
     c = (torch.tensor([1.2345678, 1.4142135, 1.9999998, 1.0000001]) * size)[:, None].expand(4, dim).contiguous()
