@@ -163,6 +163,13 @@ extern "C" int32_t he_layernorm(he_ctx* ctx, const he_layernorm_plan* p) {
 
 // ---- gradients
 
+// n from a row's statistics.  By halves: the difference of two numbers of 32 bits may be none, half of it is, with the same rounding.
+struct Normed {
+    float mean, low, by;
+    __device__ __forceinline__ Normed(const float4& stats) : mean(-0.5f * stats.x), low(0.5f * stats.y), by(2.0f * stats.z) {}
+    __device__ __forceinline__ float operator()(float h) const { return (fmaf(h, 0.5f, mean) - low) * by; }
+};
+
 struct LnGradArgs {
     const void *h, *dy, *dsum, *weight;
     const float4* stats;
@@ -223,7 +230,8 @@ template <class T, class P, bool DSUM, int ROW, int V> __global__ __launch_bound
     for (; row < a.rows; row += step, turn ^= 1) {
         if (!AHEAD) load(row, now);
         else if (row + step < a.rows) load(row + step, next);
-        const float mean = now.stats.x, low = now.stats.y, r = now.stats.z;
+        const Normed normed(now.stats);
+        const float r = now.stats.z;
         float s1 = 0, s2 = 0;
 #pragma unroll
         for (int p = 0; p < V; p++) {
@@ -233,7 +241,7 @@ template <class T, class P, bool DSUM, int ROW, int V> __global__ __launch_bound
                     if ((uint32_t)i < past[p]) now.dy[p].v[i / Vec<T>::N].set(i % Vec<T>::N, 0.0f);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float d = now.dy[p][i], n = (now.h[p][i] - mean - low) * r, g = d * weight[p][i];
+                const float d = now.dy[p][i], n = normed(now.h[p][i]), g = d * weight[p][i];
                 dw[p][i] = fmaf(d, n, dw[p][i]);
                 db[p][i] += d;
                 s1 += g;
@@ -265,7 +273,7 @@ template <class T, class P, bool DSUM, int ROW, int V> __global__ __launch_bound
             if (DSUM && !AHEAD) now.dsum[p].load((const raw*)a.dsum + (u64)row * a.ld_dsum + base[p]);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float n = (now.h[p][i] - mean - low) * r, g = now.dy[p][i] * weight[p][i];
+                const float n = normed(now.h[p][i]), g = now.dy[p][i] * weight[p][i];
                 y[i] = fmaf(r, g - s1 - n * s2, DSUM ? now.dsum[p][i] : 0.0f);
             }
             if (past[p] == 0) {
@@ -330,6 +338,7 @@ template <class T, class P, int THREADS> __global__ __launch_bounds__(THREADS) v
     const raw *h = (const raw*)a.h + row * a.ld_h, *dy = (const raw*)a.dy + row * a.ld_dy, *dsum = (const raw*)a.dsum + row * a.ld_dsum;
     const typename P::raw* w = (const typename P::raw*)a.weight;
     const float4 stats = a.stats[row];
+    const Normed normed(stats);
     auto piece = [&](uint32_t at, float* n, float* g) {
         load8<T>(h, at, a.dim, n);
         load8<T>(dy, at, a.dim, g);
@@ -337,7 +346,7 @@ template <class T, class P, int THREADS> __global__ __launch_bounds__(THREADS) v
         if (w) load8<P>(w, at, a.dim, f);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            n[i] = (n[i] - stats.x - stats.y) * stats.z;
+            n[i] = normed(n[i]);
             if (w) g[i] *= f[i];
         }
         if (at + 8 > a.dim)                               // past the row's end: 0 of g times what -mean / sqrt(v + eps) is, which may be no number
@@ -379,10 +388,10 @@ template <class T> __global__ __launch_bounds__(256) void layernorm_columns_kern
             float n[8], g[8];
             load8<T>((const raw*)a.h + row * a.ld_h, at, a.dim, n);
             load8<T>((const raw*)a.dy + row * a.ld_dy, at, a.dim, g);
-            const float4 stats = a.stats[row];
+            const Normed normed(a.stats[row]);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                dw[i] = fmaf(g[i], (n[i] - stats.x - stats.y) * stats.z, dw[i]);
+                dw[i] = fmaf(g[i], normed(n[i]), dw[i]);
                 db[i] += g[i];
             }
         }

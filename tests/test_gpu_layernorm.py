@@ -218,6 +218,19 @@ def test_grad_of_hard_rows(ctx):
     assert (got[0] == 0).all() and (got[1] == 0).all()
 
 
+@pytest.mark.parametrize("dim", [5, 20, 200, 500, 900, 1500, 4000, 8000, 12000, 20000])
+@pytest.mark.parametrize("dtype,params", T.PAIRS[:2])
+def test_grad_of_rows_as_wide_as_their_type(ctx, dtype, params, dim):
+    """Differences from the mean that 32 bits do not hold."""
+    g = T.rng(dim)
+    h, dy, w = torch.full((5, dim), -3e38), torch.randn((5, dim), generator=g).to(dtype), torch.randn(dim, generator=g).to(params)
+    h[torch.arange(5), torch.arange(5) * dim // 5] = 3.2e38
+    h[3] = -h[3]
+    ds = (1e-38 * torch.randn((5, dim), generator=g)).to(dtype)
+    for ds_ in (None, ds):
+        check_grad(run_grad(ctx, h.to(dtype), 1e-5, dy, w, ds_, params), h.to(dtype), 1e-5, dy, w, ds_, params)
+
+
 @pytest.mark.parametrize("dim", [1, 5, 7, 13, 300, 5001, 20001])
 def test_grad_of_constants_far_out(ctx, dim):
     """A mean times 1/sqrt(eps) that 32 bits do not hold, n being 0 everywhere; statistics as given."""
