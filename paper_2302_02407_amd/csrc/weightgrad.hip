@@ -44,13 +44,19 @@ __device__ __forceinline__ void parts_of(const Eight<f32_t>& y, int j, uint32_t 
     w[1] = uppers(mid[0], mid[1]);
     w[2] = uppers(low[0], low[1]);
 }
-// Of 11 significant bits the last three are the second part.  Of an infinity that would be no number: 256, above any other, which beside an infinity is nothing.
+// Of 11 significant bits the last three are the second part, of numbers of 32 bits, in which every NaN has the highest of its bits.  Of an infinity it would be no number: 256, above any
+// other, which beside an infinity is nothing.
 __device__ __forceinline__ void parts_of(const Eight<f16_t>& y, int j, uint32_t (&w)[2]) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    const uint32_t word = y.v[0].w[j];
-    const h2 x = __builtin_bit_cast(h2, word), high = __builtin_bit_cast(h2, word & 0xfff8fff8u), low = __builtin_elementwise_min(x - high, h2{256, 256});
-    w[0] = uppers((float)high[0], (float)high[1]);
-    w[1] = uppers((float)low[0], (float)low[1]);
+    const h2 pair = __builtin_bit_cast(h2, y.v[0].w[j]);
+    float x[2], low[2];
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        x[i] = (float)pair[i];
+        low[i] = fminf(x[i] - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[i]) & 0xffff0000u), 256.0f);
+    }
+    w[0] = uppers(x[0], x[1]);
+    w[1] = uppers(low[0], low[1]);
 }
 
 // A work group owns BN columns of dy by BK columns of what is kept and goes through the rows 32 at a time.

@@ -136,6 +136,18 @@ def test_what_is_not_finite_stays_in_its_row_and_column(ctx):
     assert torch.equal(~got.isfinite(), bad) and (got[3, :128] == math.inf).all()
 
 
+def test_every_f16_nan_stays_one(ctx):
+    """Whichever of its bits are set, the lowest three alone too."""
+    bits = torch.tensor([0x7c01, 0x7c02, 0x7c04, 0x7c07, 0x7c08, 0x7e00, 0x7fff]).repeat(2) - torch.tensor([0] * 7 + [0x8000] * 7)
+    dy = torch.randn((20, 16), generator=T.rng(8)).half()
+    for n, b in enumerate(bits.tolist()):
+        dy[n, n:n + 1].view(torch.int16).fill_(b)
+    assert dy.isnan().sum() == 14
+    codes, exponents = T.keep(torch.randn((20, 300), generator=T.rng(9)).abs() + 0.1)
+    got = run(ctx, dy, codes, exponents, torch.float32)
+    assert got[:14].isnan().all() and got[14:].isfinite().all()
+
+
 def test_a_block_marked_as_not_finite_is_none_whatever_its_codes(ctx):
     codes, exponents = T.keep(torch.randn((40, 300), generator=T.rng(7)))
     exponents[11, 1] = 255
