@@ -44,8 +44,8 @@ __device__ __forceinline__ void parts_of(const Eight<f32_t>& y, int j, uint32_t 
     w[1] = uppers(mid[0], mid[1]);
     w[2] = uppers(low[0], low[1]);
 }
-// Of 11 significant bits the last three are the second part, of numbers of 32 bits, in which every NaN has the highest of its bits.  Of an infinity it would be no number: 256, above any
-// other, which beside an infinity is nothing.
+// Of 11 significant bits the last three are the second part, of numbers of 32 bits, in which every NaN has the highest of its bits.  Of an infinity it is that of the largest number of its
+// sign, which beside an infinity is nothing.
 __device__ __forceinline__ void parts_of(const Eight<f16_t>& y, int j, uint32_t (&w)[2]) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
     const h2 pair = __builtin_bit_cast(h2, y.v[0].w[j]);
@@ -53,7 +53,8 @@ __device__ __forceinline__ void parts_of(const Eight<f16_t>& y, int j, uint32_t 
 #pragma unroll
     for (int i = 0; i < 2; i++) {
         x[i] = (float)pair[i];
-        low[i] = fminf(x[i] - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x[i]) & 0xffff0000u), 256.0f);
+        const float finite = __builtin_amdgcn_fmed3f(x[i], -65504.0f, 65504.0f);
+        low[i] = finite - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, finite) & 0xffff0000u);
     }
     w[0] = uppers(x[0], x[1]);
     w[1] = uppers(low[0], low[1]);

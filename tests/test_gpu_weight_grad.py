@@ -148,6 +148,19 @@ def test_every_f16_nan_stays_one(ctx):
     assert got[:14].isnan().all() and got[14:].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinities_beside_large_powers(ctx, dtype):
+    """An infinity times any kept value but 0 is an infinity of the product's sign."""
+    dy, v = torch.zeros((20, 16), dtype=dtype), torch.randn((20, 300), generator=T.rng(10))
+    v = (v + v.sign()) * 2.0 ** torch.arange(29, 129, 5)[:, None].float()
+    for n in range(16):
+        dy[n + 4, n] = -math.inf if n % 2 else math.inf
+    codes, exponents = T.keep(v)
+    got = run(ctx, dy, codes, exponents, torch.float32)
+    for n in range(16):
+        assert torch.equal(got[n], v[n + 4] * float(dy[n + 4, n]))
+
+
 def test_a_block_marked_as_not_finite_is_none_whatever_its_codes(ctx):
     codes, exponents = T.keep(torch.randn((40, 300), generator=T.rng(7)))
     exponents[11, 1] = 255
