@@ -102,11 +102,11 @@ def polynomial(ctx, u, coefs):
 
 class _LinearQ8(torch.autograd.Function):
     @staticmethod
-    def forward(run, x, weight, ctx):
+    def forward(run, x, weight, ctx, mixed):
         _same_stream(ctx)
         run.ctx, run.kept = ctx, run.needs_input_grad[1]
         run.save_for_backward(weight, *(keep_q8(ctx, x) if run.kept else ()))
-        return F.linear(x, weight)
+        return F.linear(x, weight.to(x.dtype) if mixed else weight)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -117,12 +117,16 @@ class _LinearQ8(torch.autograd.Function):
         if run.kept:
             dweight = torch.empty(weight.shape, dtype=weight.dtype, device=weight.device)
             run.ctx.he_weight_grad_q8(dy, *kept, dweight)
-        return dy @ weight if run.needs_input_grad[0] else None, dweight, None
+        return dy @ weight.to(dy.dtype) if run.needs_input_grad[0] else None, dweight, None, None
 
 
 def linear_q8(ctx, x, weight):
-    """x times weight [n][k] transposed, by the library's product; x is kept in 8 bits for the weight's gradient."""
-    return _LinearQ8.apply(_own_rows(x), weight, ctx).view(*x.shape[:-1], weight.shape[0])
+    """x times weight [n][k] transposed, by the library's product; x is kept in 8 bits for the weight's gradient.  Under autocast x and the product are of its type, and the weight's gradient,
+    of the weight's own, is not rounded to that."""
+    rows, mixed = _own_rows(x), torch.is_autocast_enabled("cuda") and x.dtype != torch.float64
+    if mixed:                                                 # here and not by autocast, which would keep the weight's copy, made without a gradient, for others in its region
+        rows = rows.to(torch.get_autocast_dtype("cuda"))
+    return _LinearQ8.apply(rows, weight, ctx, mixed).view(*x.shape[:-1], weight.shape[0])
 
 
 class _TokenLogprobs(torch.autograd.Function):

@@ -118,6 +118,41 @@ def test_what_is_not_asked_for(ctx):
     assert e.grad.shape == (0, 64)
 
 
+@pytest.mark.parametrize("low", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("inside", [True, False])
+def test_layer_in_mixed_precision(ctx, low, inside):
+    """Parameters of 32 bits under autocast: the product in 16 bits, the weight's gradient in 32, whether the backward pass runs in the region or behind it; a second use of the weight there
+    by torch's own product has its gradient too."""
+    from paper_2302_02407_amd.training import linear_q8
+    g, m, n, k = T.rng(6), 37, 50, 200
+    x, w, wr = torch.randn((m, k), generator=g), torch.randn((n, k), generator=g) / 16, torch.randn((m, n), generator=g)
+    px, pw = x.cuda().requires_grad_(), w.cuda().requires_grad_()
+    with torch.autocast("cuda", dtype=low):
+        u = linear_q8(ctx, px, pw)
+        assert u.dtype == low
+        if inside:
+            u.backward(wr.to(low).cuda())
+    if not inside:
+        u.backward(wr.to(low).cuda())
+    assert px.grad.dtype == pw.grad.dtype == torch.float32
+    a, b, d = x.to(low).double(), w.to(low).double(), wr.to(low).double()
+    near(u, a @ b.T, a.abs() @ b.abs().T, low, (k + 16) * 2.0 ** -24)
+    near(px.grad, d @ b, d.abs() @ b.abs(), low, (n + 16) * 2.0 ** -24)
+    kept = T.kept(*T.keep(x.to(low).float()))
+    near(pw.grad, d.T @ kept, d.abs().T @ kept.abs(), torch.float32, (m + 16) * 2.0 ** -24)
+    pw.grad = None
+    with torch.autocast("cuda", dtype=low):
+        linear_q8(ctx, px, pw.detach()).sum().backward()
+        u = linear_q8(ctx, px, pw)
+        (u.sum() + torch.nn.functional.linear(px, pw).sum()).backward()
+    one = pw.grad.clone()
+    pw.grad = None
+    with torch.autocast("cuda", dtype=low):
+        linear_q8(ctx, px, pw).sum().backward()
+    layer = pw.grad.clone()
+    near(one - layer, a.sum(dim=0).expand(n, k), a.abs().sum(dim=0).expand(n, k) + layer.cpu().double().abs(), low, (m + 16) * 2.0 ** -24)
+
+
 def test_another_stream_is_refused(ctx):
     from paper_2302_02407_amd.training import layer_norm
     x = torch.zeros((4, 64), device="cuda")
