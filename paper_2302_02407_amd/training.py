@@ -117,7 +117,8 @@ class _LinearQ8(torch.autograd.Function):
         if run.kept:
             dweight = torch.empty(weight.shape, dtype=weight.dtype, device=weight.device)
             run.ctx.he_weight_grad_q8(dy, *kept, dweight)
-        return dy @ weight.to(dy.dtype) if run.needs_input_grad[0] else None, dweight, None, None
+        with torch.autocast("cuda", enabled=False):           # the forward pass says in which type
+            return dy @ weight.to(dy.dtype) if run.needs_input_grad[0] else None, dweight, None, None
 
 
 def linear_q8(ctx, x, weight):

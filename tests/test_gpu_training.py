@@ -153,6 +153,18 @@ def test_layer_in_mixed_precision(ctx, low, inside):
     near(one - layer, a.sum(dim=0).expand(n, k), a.abs().sum(dim=0).expand(n, k) + layer.cpu().double().abs(), low, (m + 16) * 2.0 ** -24)
 
 
+def test_layer_behind_a_region_of_mixed_precision(ctx):
+    """A forward pass of 32 bits has a backward pass of 32 bits, also where that runs under autocast."""
+    from paper_2302_02407_amd.training import linear_q8
+    g = T.rng(7)
+    x, w, d = torch.randn((20, 64), generator=g).cuda().requires_grad_(), torch.randn((30, 64), generator=g).cuda(), torch.randn((20, 30), generator=g).cuda()
+    u = linear_q8(ctx, x, w)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        u.backward(d)
+    a, b = d.cpu().double(), w.cpu().double()
+    near(x.grad, a @ b, a.abs() @ b.abs(), torch.float32, 46 * 2.0 ** -24)
+
+
 def test_another_stream_is_refused(ctx):
     from paper_2302_02407_amd.training import layer_norm
     x = torch.zeros((4, 64), device="cuda")
