@@ -580,7 +580,8 @@ int32_t he_work_poly_grad_q8(const he_ctx* ctx, const he_poly_grad_plan* plan, u
 
 /* dw[n][k] = sum over m of dy[m][n] * v[m][k], v the values that are kept; with `accumulate` that is added to what dw holds.  Products are
  * exact (dy is taken as the sum of as many bfloat16 numbers as its type needs: where that leaves 2^-126 behind, it is lost) and summed
- * in 32 bits.  With m = 0 dw becomes 0, or stays.  dw must not overlap an operand or d_work. */
+ * in 32 bits.  With m = 0 dw becomes 0, or stays.  dw must not overlap an operand or d_work.  Scratch memory: where few
+ * tiles would leave compute units idle, sums over parts of the rows, each 4 n k bytes (k to a multiple of 4), up to 2^30 bytes in all. */
 typedef struct {
     uint32_t m, n, k;              /* m up to 2^21, n and k up to 2^17 */
     int32_t dtype;                 /* of dy */

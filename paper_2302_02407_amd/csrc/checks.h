@@ -166,16 +166,19 @@ static inline const char* refuse_poly_grad(const he_poly_grad_plan* p, bool quer
 // ---- a weight's gradient from an input kept in 8 bits
 
 #define HE_SIDE_MAX (1u << 17)
+#define HE_WORK_MAX (1ull << 30)   // bytes of a weight gradient's scratch memory
 
 // Tiles of `side` rows by as many columns of dw, or of 64 by 256, the sum over the rows of dy in `parts` parts of `per` steps of 32 rows, joined by a second kernel
 struct WeightCut {
     uint32_t side, parts, per;
     bool ahead;                // small tiles of bf16, at most two to a compute unit: rows are asked for four steps ahead, for which three have no registers (65536 x 256 x 256: 28 us, 30)
 };
+static inline uint64_t weight_pitch(uint32_t k) { return (k + 3) & ~3u; }
 // The cut that costs least, by what was measured of steps and joins (bf16; in fifths of a step of a compute unit's three small tiles, 0.19 us): a step of a
 // unit takes 5.5 with a tile of 256 x 256, and 3, 4, 5 with one, two, three of 128 x 128; a step of f16 1.4 times that and one of f32 2 times, their matrix
 // products being two and three (between 1.2 and 1.6, and 1.6 and 2.3, cuts or times of few shapes change).  The second launch takes 16 and a part 8 bytes an
 // element at 4.5 TB/s.  Measured against the best of five rules of thumb on eleven shapes from 500 x 100 x 100 to 65536 x 256 x 256; shapes between go by the same line.
+// No more parts than HE_WORK_MAX has room for, which binds only from some 10^12 products on.
 static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k, int32_t dtype) {
     const uint64_t steps = (m + 31) / 32, kind = dtype == HE_BF16 ? 10 : dtype == HE_F16 ? 14 : 20;
     WeightCut best = {128, 1, (uint32_t)steps, false};
@@ -188,6 +191,7 @@ static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k, int32_t d
         for (const uint32_t want : wants) {
             if (want > 1 && steps < 4 * want) break;
             const uint64_t per = (steps + want - 1) / want, parts = (steps + per - 1) / per, each = (tiles * parts + 255) / 256;
+            if (parts > 1 && parts * n * weight_pitch(k) * 4 > HE_WORK_MAX) break;
             const uint64_t step = side == 256 ? 11 * each : 2 * (each / 3 * 5 + (each % 3 ? each % 3 + 2 : 0));
             const uint64_t cost = per * step * kind + (parts > 1 ? 320 + parts * n * k / 5350 : 0);          // in twentieths
             if (cost < least) least = cost, best = {side, (uint32_t)parts, (uint32_t)per, each <= 2};
@@ -195,7 +199,6 @@ static inline WeightCut weight_cut(uint32_t m, uint32_t n, uint32_t k, int32_t d
     }
     return best;
 }
-static inline uint64_t weight_pitch(uint32_t k) { return (k + 3) & ~3u; }
 static inline uint64_t weight_grad_work(const he_weight_grad_plan* p) {
     if (!p->m || !p->n || !p->k) return 0;
     const WeightCut c = weight_cut(p->m, p->n, p->k, p->dtype);

@@ -216,6 +216,40 @@ def test_refusals(tmp_path):
     assert r.returncode == 0, r.stdout
 
 
+BOUND = r"""
+#include <stdio.h>
+#include "checks.h"
+
+int main() {
+    int bad = 0;
+    for (int32_t t = 0; t < 3; t++)
+        for (uint64_t m = 1; m <= 1 << 21; m = m * 7 / 4 + 1)
+            for (uint64_t n = 1; n <= 1 << 17; n = n * 5 / 4 + 1)
+                for (uint64_t k = 1; k <= 1 << 17; k = k * 5 / 4 + 1) {
+                    he_weight_grad_plan p = {};
+                    p.m = m, p.n = n, p.k = k, p.dtype = t;
+                    const uint64_t bytes = weight_grad_work(&p), parts = weight_cut(m, n, k, t).parts;
+                    if (bytes > 1ull << 30 || bytes != (parts > 1 ? parts * n * ((k + 3) / 4 * 4) * 4 : 0)) bad++;
+                }
+    printf("%d bad\n", bad);
+    return bad != 0;
+}
+"""
+
+
+def on_host(tmp_path, program):
+    """What a program says that is compiled for the host with the header of checks."""
+    src, exe = tmp_path / "program.cc", tmp_path / "program"
+    src.write_text(program)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", os.path.join(ROOT, "paper_2302_02407_amd", "csrc"), str(src), "-o", str(exe)], check=True, timeout=120)
+    return subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
+
+
+def test_scratch_memory_of_a_weight_gradient_has_a_bound(tmp_path):
+    r = on_host(tmp_path, BOUND)
+    assert r.returncode == 0, r.stdout
+
+
 def test_every_operator_is_exported():
     for f in ("he_layernorm", "he_layernorm_grad", "he_poly_q8", "he_poly_grad_q8", "he_weight_grad_q8", "he_token_logprobs", "he_token_logprobs_grad",
               "he_work_layernorm_grad", "he_work_poly_grad_q8", "he_work_weight_grad_q8", "he_work_token_logprobs"):
