@@ -238,13 +238,16 @@ static inline const char* logits_sizes(uint32_t rows, uint32_t vocab, int32_t dt
 struct LogprobCut {
     uint32_t parts, len;
 };
+#define HE_JOIN_PARTS 32               // at most so many parts: lanes and room of the kernel that joins them
 // Few long rows are cut in up to 32 parts of at least 8 KiB, which are joined by a second launch (128 x 131072 bf16, k = 8, in four parts 17.8 us,
 // whole 20.1; 1 x 131072, k = 20, in 32 parts 11.3)
+// Every part, the last too, has to have at least HE_TOP_MAX elements, the first k of which are put in order, and more than 4 KiB, what a launch of single wavefronts, which knows no
+// parts, takes.
 static inline LogprobCut logprobs_cut(uint32_t rows, uint32_t vocab, int32_t dtype) {
     const uint32_t piece = 8192 / dtype_bytes(dtype);
     uint32_t parts = rows ? 512 / rows : 1;
     if (parts > vocab / piece) parts = vocab / piece;
-    if (parts > 32) parts = 32;
+    if (parts > HE_JOIN_PARTS) parts = HE_JOIN_PARTS;
     if (parts < 4) return {1, vocab};
     const uint32_t len = ((vocab + parts - 1) / parts + 15) & ~15u;
     return {(vocab + len - 1) / len, len};

@@ -190,12 +190,11 @@ template <class T, int THREADS, int ROOM, bool HELD, bool PARTED> __global__ __l
     }
 }
 
-#define JOIN_PARTS 32              // at most so many parts
 // The parts of a row, joined by a work group: totals, and of the parts' places those that can be among the first k.  Every part has its own first k in order, so
 // with r = ceil(k / parts) the smallest of the parts' r-th places is one that k places reach, and so is any part's k-th.  1 x 131072 bf16, k = 20: 6.6 us for the parts and 5.3
 // for this.
 template <class T> __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a) {
-    __shared__ u64 keep[JOIN_PARTS * HE_TOP_MAX], bound[2];
+    __shared__ u64 keep[HE_JOIN_PARTS * HE_TOP_MAX], bound[2];
     __shared__ uint32_t kept;
     const u64 row = blockIdx.x;
     const uint32_t t = threadIdx.x, lane = t & 63;

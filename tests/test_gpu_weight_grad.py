@@ -108,6 +108,25 @@ def test_whole_numbers_of_long_sums_in_large_tiles(ctx, dtype, m, n, k):
     assert torch.equal(run(ctx, dy, codes, exponents, torch.float32, 1, 1), want)
 
 
+# m, n, k, and of bfloat16 the tile's columns of dy, the parts of the sum, whether rows are asked for further ahead: test_train_checks compares these with the cut
+LAUNCHES = [(1000, 10, 40000, 64, 4, 0), (2048, 100, 40000, 128, 2, 0), (4096, 2048, 2048, 128, 3, 0), (1000, 200, 40000, 128, 1, 0), (40, 100, 100000, 128, 1, 0), (70, 50, 40000, 64, 1, 1),
+            (70, 100, 40000, 128, 1, 1), (5000, 33, 700, 64, 32, 1), (3000, 130, 70, 128, 16, 1), (9000, 65, 260, 128, 57, 1), (2069, 4050, 4060, 256, 1, 1), (20011, 777, 1001, 256, 16, 1)]
+
+
+@pytest.mark.parametrize("m,n,k", [row[:3] for row in LAUNCHES])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_whole_numbers_by_every_launch(ctx, dtype, m, n, k):
+    """Sums below m * 20 * 16 < 2^24: exact."""
+    g = torch.Generator("cuda").manual_seed(m + n)
+    dy = torch.randint(-20, 21, (m, n), generator=g, device="cuda").to(dtype)
+    v, exponents = torch.randint(-8, 9, (m, k), generator=g, device="cuda").float(), torch.full((m, -(-k // 128)), 127, dtype=torch.uint8, device="cuda")
+    codes = v.to(R.F8)
+    exponents[::3] += 1
+    v[::3] *= 2
+    want = (dy.double().T @ v.double()).float().cpu()
+    assert torch.equal(run(ctx, dy, codes, exponents, torch.float32, 1, 1), want)
+
+
 def test_numbers_of_all_sizes(ctx):
     """32 bits of dy count, far powers of what is kept too: one product a sum, which is added up from three parts of it, so off by at most 3 2^-24 of itself
     and by what is below the smallest normal numbers; what 32 bits do not hold is infinite."""

@@ -250,6 +250,56 @@ def test_scratch_memory_of_a_weight_gradient_has_a_bound(tmp_path):
     assert r.returncode == 0, r.stdout
 
 
+PARTED = r"""
+#include <stdio.h>
+#include "checks.h"
+
+int main() {
+    int bad = 0;
+    for (int32_t t = 0; t < 3; t++)
+        for (uint32_t rows = 1; rows <= 600; rows++)
+            for (uint32_t vocab = 1; vocab <= HE_VOCAB_MAX; vocab += 1 + vocab / 97) {
+                const LogprobCut c = logprobs_cut(rows, vocab, t);
+                const uint64_t last = vocab - (uint64_t)(c.parts - 1) * c.len;
+                // every element in one part, and the last part not empty
+                if (c.parts < 1 || (uint64_t)(c.parts - 1) * c.len >= vocab || (uint64_t)c.parts * c.len < vocab) bad++;
+                // as many as the join takes; in each as many as can be asked for, and more than a wavefront's launch has
+                if (c.parts > 1 && (c.parts > HE_JOIN_PARTS || last < HE_TOP_MAX || c.len < HE_TOP_MAX || (uint64_t)c.len * dtype_bytes(t) <= 4096 || c.len % 16)) bad++;
+            }
+    printf("%d bad\n", bad);
+    return bad != 0;
+}
+"""
+
+
+def test_parts_of_a_row_of_logits(tmp_path):
+    r = on_host(tmp_path, PARTED)
+    assert r.returncode == 0, r.stdout
+
+
+CUTS = r"""
+#include <stdio.h>
+#include "checks.h"
+
+int main() {
+    const uint32_t want[][6] = {%s};                     // m, n, k, tile, parts, whether rows are asked for further ahead
+    int bad = 0;
+    for (auto& w : want) {
+        const WeightCut c = weight_cut(w[0], w[1], w[2], HE_BF16);
+        if (c.side != w[3] || c.parts != w[4] || c.ahead != (w[5] != 0)) { bad++; printf("%%u %%u %%u: %%u %%u %%d\n", w[0], w[1], w[2], c.side, c.parts, c.ahead); }
+    }
+    return bad != 0;
+}
+"""
+
+
+def test_sizes_that_take_every_launch_of_a_weight_gradient(tmp_path):
+    """Those that the tests on the GPU go by: kinds of tiles of bfloat16, whole and in parts, with rows asked for one step and four steps ahead."""
+    from test_gpu_weight_grad import LAUNCHES
+    r = on_host(tmp_path, CUTS % ", ".join("{%d, %d, %d, %d, %d, %d}" % row for row in LAUNCHES))
+    assert r.returncode == 0, r.stdout
+
+
 def test_every_operator_is_exported():
     for f in ("he_layernorm", "he_layernorm_grad", "he_poly_q8", "he_poly_grad_q8", "he_weight_grad_q8", "he_token_logprobs", "he_token_logprobs_grad",
               "he_work_layernorm_grad", "he_work_poly_grad_q8", "he_work_weight_grad_q8", "he_work_token_logprobs"):
