@@ -170,6 +170,35 @@ def test_sums_of_values_whose_squares_32_bits_do_not_hold(ctx, dtype, value, gra
         check_grad(run_grad(ctx, codes, exponents, coefs_of(n), dy.to(dtype)), codes, exponents, coefs_of(n), dy.to(dtype))
 
 
+def check_sums(got, codes, exponents, coefs, dy):
+    """The coefficients' gradients alone: a slope there need not be a number of 32 bits."""
+    _, dc, _, size = T.poly_grad(T.kept(codes, exponents), coefs, dy)
+    off, bound = (got[1].cpu().double() - dc).abs(), 2.0 ** -19 * size + T.rounding(dc, torch.float32)
+    assert (off <= bound).all(), float((off / bound).max())
+
+
+@pytest.mark.parametrize("n", [4, 5, 6, 7, 9])
+@pytest.mark.parametrize("high", [1, 57, 100, 126])
+def test_sums_of_higher_powers_beside_padding(ctx, n, high):
+    """Blocks of padding among others, several of them a wavefront's."""
+    g = T.rng(n)
+    v, dy = torch.randn((40, 300), generator=g), torch.randn((40, 300), generator=g)
+    pad = torch.arange(40) % 3 == 1
+    v[pad], dy[pad] = v[pad].clamp(-3, 3) * 2.0 ** high, 0.0
+    codes, exponents = T.keep(v)
+    check_sums(run_grad(ctx, codes, exponents, coefs_of(n), dy), codes, exponents, coefs_of(n), dy)
+
+
+# on both sides of the powers whose squares are normal numbers
+@pytest.mark.parametrize("value,gradient", [(61, -146), (63, -149), (-44, 0), (-46, 0), (-60, 120), (-70, 120)])
+def test_sums_of_fourth_powers_far_out(ctx, value, gradient):
+    g = T.rng(8)
+    v = (1 + torch.rand((9, 300), generator=g) / 2) * (2.0 * torch.randint(0, 2, (9, 300), generator=g) - 1) * 2.0 ** value
+    dy = torch.randint(-2 ** 9, 2 ** 9, (9, 300), generator=g).float() * 2.0 ** (gradient if gradient < 0 else gradient - 9)
+    codes, exponents = T.keep(v)
+    check_sums(run_grad(ctx, codes, exponents, coefs_of(5), dy), codes, exponents, coefs_of(5), dy)
+
+
 def test_far_rows(ctx):
     rows, dim, pitch = 18, 300, 1 << 28                                # 17 * 2^28 elements: past 2^32
     g = T.rng(6)
