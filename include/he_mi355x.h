@@ -485,7 +485,8 @@ int32_t he_distill_grad(he_ctx* ctx, const he_distill_plan* plan);
  *  - Rows kept in 8 bits: e4m3 codes, and for each 128 columns (the last of what is left) one byte b: a value is its code times
  *    2^(b-127).  2^(b-127) is the smallest power from 2^-110 on at which the block's largest value is at most 448; values are
  *    divided by it, exactly, and rounded to nearest even.  So a value is a number of 16 bits (bfloat16), exactly, and off by at most
- *    2^-4 of itself or 2^-10 of the power.  A block of zeros has b = 118 (2^-9).  A block that holds an infinity or a NaN has b = 255 and codes 0x7f: all its values are NaN.
+ *    2^-4 of itself or 2^-10 of the power; from 1.9375 * 2^127 on it is kept as 2^128, which is infinite where it is read.  A block of zeros
+ *    has b = 118 by convention.  A block that holds an infinity or a NaN has b = 255 and codes 0x7f: all its values are NaN.
  *    Rows of codes start at multiples of 16 bytes (pointer and ld), and the columns up to the next multiple of 16 are there, as above. */
 
 /* h = x + residual, rounded to dtype (without a residual h = x); mean and variance v of h's row, y = (h - mean) / sqrt(v + eps) * weight +
@@ -558,7 +559,8 @@ typedef struct {
 int32_t he_poly_q8(he_ctx* ctx, const he_poly_plan* plan);
 
 /* From the gradient dy by y, at the values v that are kept: du = dy * sum of i coefs[i] v^(i-1), dcoefs[i] = sum over all elements of dy * v^i
- * (may be NULL; 0 where there are no rows; its sums are held in 64 bits across pieces of eight elements).  d_du may be d_dy with the same ld. */
+ * (may be NULL; 0 where there are no rows; its sums are held in 64 bits across pieces of eight elements, where a dy of 0 adds nothing whatever number v is).  The slope beside dy
+ * in du is a number of 32 bits: where it leaves them du is infinite, or beside a dy of 0 a NaN.  d_du may be d_dy with the same ld. */
 typedef struct {
     uint32_t rows, dim, n_coefs;   /* n_coefs from 1 to HE_POLY_MAX */
     int32_t dtype;                 /* of dy and du */
@@ -583,7 +585,7 @@ int32_t he_work_poly_grad_q8(const he_ctx* ctx, const he_poly_grad_plan* plan, u
  * in 32 bits.  With m = 0 dw becomes 0, or stays.  dw must not overlap an operand or d_work.  Scratch memory: where few
  * tiles would leave compute units idle, sums over parts of the rows, each 4 n k bytes (k to a multiple of 4), up to 2^30 bytes in all. */
 typedef struct {
-    uint32_t m, n, k;              /* m up to 2^21, n and k up to 2^17 */
+    uint32_t m, n, k;              /* m up to 2^21, n and k up to 2^17 (rows that he_poly_q8 writes: k up to 65536) */
     int32_t dtype;                 /* of dy */
     int32_t out_dtype;             /* of dw */
     uint32_t accumulate;
@@ -608,7 +610,9 @@ int32_t he_work_weight_grad_q8(const he_ctx* ctx, const he_weight_grad_plan* pla
  *   d_stats     the largest logit that counts, the sum of exp((z - that) / tau), the entropy, and 0: what he_token_logprobs_grad reads.
  * Each may be NULL (d_tokens and d_logp: both or neither; d_values and d_index with k > 0, both or neither; at least one is there).  Which
  * logits count as -infinity is as in he_top_logits.  A row of nothing else has log probabilities of -infinity, entropy 0 and a sum of 0.  A row that
- * holds a NaN, or a logit from 2^126 min(1, tau) up, has no distribution: log probability, entropy and values are NaN, the order stands. */
+ * holds a NaN, or a logit from 2^126 min(1, tau) up, has no distribution: log probability, entropy and values are NaN, the order stands.
+ * Rows with very many equal finite logits at the k-th place are slow, since they are read nine times: all equal, or but for a few masked by a finite number (2048 x 131072
+ * bf16, k = 8, five others a row: 6.0 ms in place of 0.11; he_top_logits too).  A mask of -infinity is not slow. */
 typedef struct {
     uint32_t rows, vocab, k;       /* vocab from 1 to 2^20, k <= min(vocab, HE_TOP_MAX) */
     int32_t dtype;

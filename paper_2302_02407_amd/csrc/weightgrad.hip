@@ -83,7 +83,7 @@ typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 // read and multiplied in turn 1256, in the pipeline below 1124, loads by pointers 1095, asked for two steps ahead 1040.  Wavefronts of 128 x 64, which convert half as much,
 // read codes two bytes a lane: 1190 where this took 1095, for LDS instructions.  Four wavefronts of 128 x 128 do not fit the registers.  Smaller tiles,
 // 128 x 128 by four wavefronts of 64 x 64, two or three to a unit, where few large ones are there: 4096 x 2048 x 2048
-// 63 us; 64 x 256 by four of 64 x 64 for up to 64 columns of dy: 22070 x 25 x 4773 f16 44 us, in tiles of 128 x 128 76.
+// 63 us; 64 x 256 by four of 64 x 64 for up to 64 columns of dy: 22070 x 25 x 4773 f16 39 us, in tiles of 128 x 128 76 when this took 44.
 template <class T, int WN, int WK, int TN, int TK, int AHEAD, bool NARROW> __global__ __launch_bounds__(64 * WN * WK, 2) void weight_grad_kernel(WeightArgs a) {
     using raw = typename T::raw;
     using G = WeightTile<T, WN, WK, TN, TK>;

@@ -122,8 +122,8 @@ class _LinearQ8(torch.autograd.Function):
 
 
 def linear_q8(ctx, x, weight):
-    """x times weight [n][k] transposed, by the library's product; x is kept in 8 bits for the weight's gradient.  Under autocast x and the product are of its type, and the weight's gradient,
-    of the weight's own, is not rounded to that."""
+    """x times weight [n][k <= 65536] transposed, by the library's product; x is kept in 8 bits for the weight's gradient.  Under autocast x and the product are of its type, and the weight's
+    gradient, of the weight's own, is not rounded to that."""
     rows, mixed = _own_rows(x), torch.is_autocast_enabled("cuda") and x.dtype != torch.float64
     if mixed:                                                 # here and not by autocast, which would keep the weight's copy, made without a gradient, for others in its region
         rows = rows.to(torch.get_autocast_dtype("cuda"))
