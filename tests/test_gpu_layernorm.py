@@ -77,6 +77,19 @@ def test_forward(ctx, dtype, params, rows, dim):
         check_forward(run(ctx, x, r_, w_, b_, 1e-5, dim + n, n, over), x, r_, w_, b_, 1e-5)
 
 
+@pytest.mark.parametrize("dim,each", [(100, 8), (250, 16), (500, 8), (1000, 16), (2000, 8), (4000, 16), (8000, 16), (16000, 16), (30000, 32), (60000, 64)])
+def test_roundings_of_32_bits(ctx, dim, each):
+    """A thread adds `each` numbers, then 6 joins in a wavefront and up to 16 of wavefronts: that many roundings and one more of the mean's lack, against the mean of |n|, at most 1; half of them
+    and 6 of n, of its size; two of the result."""
+    x, _, w, b = inputs(7, dim, torch.float32, torch.float32, dim, False)
+    y, _, _ = run(ctx, x, None, w, b, 1e-5)
+    n, _ = T.norm(x, 1e-5)
+    want = n * w.double() + b.double()
+    bound = 2.0 ** -24 * (((each + 24) / 2 + 6) * (n * w).abs() + (each + 23) * w.double().abs() + 2 * ((n * w).abs() + b.double().abs())) + 2.0 ** -149
+    off = (y.cpu().double() - want).abs()
+    assert (off <= bound).all(), float((off / bound).max())
+
+
 @pytest.mark.parametrize("dim", [5, 64, 1000, 3000, 20000])
 def test_rows_that_are_hard(ctx, dim):
     g = T.rng(dim)
